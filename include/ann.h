@@ -49,6 +49,9 @@ extern "C" {
 #define ANN_MAX_DEGREE 64u
 #define ANN_MAX_ENTRIES 64u
 #define ANN_STATIC_SCRATCH_BYTES (8u << 20) /* see ann_search_batch_static */
+#define ANN_MAX_NORM_DIM (1u << 20)         /* see ann_layer_norm */
+#define ANN_MAX_SCORE_DIM 4096u             /* see ann_row_logprobs */
+#define ANN_MAX_ALTERNATIVES 64u            /* see ann_row_logprobs */
 
 typedef struct ann_index ann_index; /* opaque; device memory owned by the library */
 
@@ -62,6 +65,9 @@ typedef enum {
 } ann_status;
 
 typedef enum { ANN_L2 = 0, ANN_IP = 1 } ann_metric;
+
+/* Element types of the operators on hidden states and embeddings (ann_layer_norm, ann_row_logprobs). */
+typedef enum { ANN_F32 = 0, ANN_F16 = 1, ANN_BF16 = 2 } ann_type;
 
 /* ann_index_desc.flags */
 #define ANN_DESC_HOST_POINTERS 1u /* every array in the descriptor is in HOST memory */
@@ -486,6 +492,122 @@ ann_status ann_rerank_adaptive(ann_index *index, const float *q, uint32_t nq, co
  */
 ann_status ann_bruteforce_topk(const float *x, uint64_t n, uint32_t d, const float *q, uint32_t nq, uint32_t k,
                                uint32_t metric, uint32_t *out_ids, float *out_dist, void *stream);
+
+/*
+ * The head of a model over a table of rows: what an encoder does last (layer
+ * norm) and what it is trained with and weighed by (probabilities of rows under
+ * the softmax of all rows' scores), each with its gradient.  These calls only
+ * enqueue work on the caller's stream: they allocate nothing, wait for nothing
+ * and keep nothing between calls, and may be captured into a graph.  Where a call
+ * needs scratch memory the caller brings it (`workspace`, of at least the
+ * bytes that the function named *_workspace returns for the same sizes; its
+ * contents do not matter and need not be kept; 16-byte aligned); calls that may overlap need one
+ * each.  Row strides count elements and are at least the row length.  Elements are
+ * ann_type; any alignment that the type itself asks for works (16 bytes, also of
+ * the stride, is fastest).  Sums and statistics are fp32 or wider and results are
+ * rounded once to the type they are returned in, except where a comment says otherwise.
+ * The same call gives the same bits again.
+ */
+
+/*
+ * Layer norm of n rows of `dim` elements:
+ *   y = (x - mean) * rstd * weight + bias,  rstd = 1 / sqrt(mean((x - mean)^2) + eps).
+ *   type         of x and y; weight_type: of weight and bias, `type` or ANN_F32.
+ *   weight, bias [dim], each NULL allowed (ones, zeros).
+ *   mean, rstd   [n] fp32, for the backward pass; NULL allowed.
+ * y may be x (same stride).  n = 0 does nothing.  dim <= ANN_MAX_NORM_DIM.
+ * Errors: ANN_EINVAL (NULL x or y, dim == 0, unknown type, a stride shorter than a
+ * row, eps negative or NaN), ANN_ECAPACITY.
+ */
+ann_status ann_layer_norm(const void *x, uint64_t n, uint32_t dim, uint64_t x_stride, uint32_t type, const void *weight,
+                          const void *bias, uint32_t weight_type, float eps, void *y, uint64_t y_stride, float *mean,
+                          float *rstd, void *stream);
+
+/*
+ * Gradients of ann_layer_norm from dy, x and the forward pass' mean and rstd.
+ *   dx             [n] rows of `type`; may be dy (same stride).
+ *   dweight, dbias [dim] of weight_type, summed over the rows in fp32 in a fixed
+ *                  order; NULL where not wanted (both NULL: no workspace needed).
+ * n = 0 writes zeros to dweight and dbias.  Errors as ann_layer_norm, and a
+ * workspace that is NULL, unaligned or too small (ANN_EINVAL).
+ */
+ann_status ann_layer_norm_backward(const void *dy, uint64_t dy_stride, const void *x, uint64_t x_stride, uint64_t n,
+                                   uint32_t dim, uint32_t type, const void *weight, uint32_t weight_type,
+                                   const float *mean, const float *rstd, void *dx, uint64_t dx_stride, void *dweight,
+                                   void *dbias, void *workspace, uint64_t workspace_bytes, void *stream);
+uint64_t ann_layer_norm_backward_workspace(uint64_t n, uint32_t dim);
+
+/*
+ * The scores of nq queries against n rows, s[i][j] = scale * <q_i, x_j> + bias_j.
+ * They are never stored: the calls below take them as they are computed.
+ *   q, rows    [nq], [n] rows of d elements of `type` with their strides;
+ *              d <= ANN_MAX_SCORE_DIM, n and nq < 2^31.
+ *   scale      an inverse temperature; finite.
+ *   row_bias   [n] fp32, NULL allowed: zeros.  A row whose bias is -infinity is left
+ *              out of every query's softmax, whatever its elements hold.  (Squared
+ *              distances instead of inner products: scale = 2 / t and bias_j =
+ *              -|x_j|^2 / t give the softmax of -|q - x|^2 / t.)
+ *   targets    [nq] the row whose log probability is asked for; ANN_PAD_ID (or any id
+ *              that is not below n): none.  NULL: none for any query.
+ * Products of 16-bit elements are exact and summed in fp32; fp32 elements are
+ * taken as three bf16 parts (six of the nine products; what is left out is below
+ * 2^-23 of the product).
+ */
+typedef struct {
+  const void *q, *rows;
+  uint64_t n, q_stride, row_stride;
+  uint32_t nq, d, type;
+  float scale;
+  const float *row_bias;
+  const uint32_t *targets;
+} ann_row_scores;
+
+/*
+ * Log probabilities of given rows under the softmax over all rows, the softmax'
+ * entropy and its k largest alternatives:
+ *   lse[i]       = log sum_j exp(s[i][j])
+ *   logprob[i]   = s[i][targets[i]] - lse[i]; 0 where no row is given, -infinity
+ *                  where the row given is left out
+ *   entropy[i]   = lse[i] - sum_j p[i][j] s[i][j], p the probabilities
+ *   alt_ids      [nq][k] the rows with the largest scores, in descending order; the
+ *                order is that of the scores as fp64 sums (up to the rounding of
+ *                those), equal scores in ascending order of their ids; ANN_PAD_ID
+ *                behind the last row that is not left out.
+ *   alt_logprobs [nq][k] their log probabilities (-infinity with ANN_PAD_ID).
+ * logprob and lse are required; entropy may be NULL; alt_ids and alt_logprobs
+ * both or neither (k = 0: both NULL).  k <= ANN_MAX_ALTERNATIVES.  A query with no row left (all biases
+ * -infinity, or n = 0): lse -infinity, entropy 0, logprob -infinity (0 where no
+ * row is given), no alternatives.  A score of a row that is not
+ * left out that is not finite (or, times log2 e, not) leaves that query's statistics NaN or infinite, and only
+ * its; a row whose score is NaN is no alternative.  nq = 0 does nothing.
+ * Errors: ANN_EINVAL (NULL arguments, unknown type, d == 0, strides, scale,
+ * alternatives without k or the reverse, workspace), ANN_ECAPACITY (d, k, n, nq).
+ */
+ann_status ann_row_logprobs(const ann_row_scores *scores, uint32_t k, float *logprob, float *entropy, float *lse,
+                            uint32_t *alt_ids, float *alt_logprobs, void *workspace, uint64_t workspace_bytes,
+                            void *stream);
+uint64_t ann_row_logprobs_workspace(uint32_t nq, uint64_t n, uint32_t d, uint32_t type, uint32_t k);
+
+/*
+ * Gradients of  sum_i g_logprob[i] * logprob[i] + g_entropy[i] * entropy[i]
+ * from the forward pass' lse and entropy; with G = the gradient of the scores,
+ *   G[i][j] = g_logprob[i] ([j = targets[i]] - p[i][j]) - g_entropy[i] p[i][j] (s[i][j] - lse[i] + entropy[i])
+ *   dq[i]    = scale * sum_j G[i][j] x_j         drows[j] = scale * sum_i G[i][j] q_i
+ *   drow_bias[j] = sum_i G[i][j]
+ * g_logprob or g_entropy may be NULL (zeros; entropy is needed with g_entropy
+ * only); dq, drows (of `type`, with their strides) and drow_bias ([n] fp32) each may be NULL where not wanted.
+ * G is rounded to 16 bits before its products with 16-bit rows and queries (bf16: to
+ * bf16; f16: to f16 after a power of two that brings the largest weight to
+ * 2^13 .. 2^14), and taken as three bf16 parts with fp32 ones; drow_bias sums it in fp32.
+ * Queries without a given row take no part with their g_logprob; rows left out get
+ * zero.  A query whose lse is -infinity (no row left) gets zero.
+ * Errors as ann_row_logprobs.
+ */
+ann_status ann_row_logprobs_backward(const ann_row_scores *scores, const float *lse, const float *entropy,
+                                     const float *g_logprob, const float *g_entropy, void *dq, uint64_t dq_stride,
+                                     void *drows, uint64_t drows_stride, float *drow_bias, void *workspace,
+                                     uint64_t workspace_bytes, void *stream);
+uint64_t ann_row_logprobs_backward_workspace(uint32_t nq, uint64_t n, uint32_t d, uint32_t type);
 
 /*
  * The number of expansions per step that mode 1 uses when

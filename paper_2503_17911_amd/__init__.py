@@ -20,8 +20,10 @@ LIB_PATH = Path(os.environ.get("ANN_LIBRARY_PATH") or (_PKG / "lib" / "libann_gf
 
 PAD_ID = 0xFFFFFFFF
 L2, IP = 0, 1
+F32, F16, BF16 = 0, 1, 2
 MAX_EF, MAX_DEGREE, MAX_ENTRIES = 512, 64, 64
 STATIC_SCRATCH_BYTES = 8 << 20
+MAX_NORM_DIM, MAX_SCORE_DIM, MAX_ALTERNATIVES = 1 << 20, 4096, 64
 DESC_HOST_POINTERS = 1
 DESC_UNIT_NORM_L2_KEYS = 2
 DESC_QUERY_15BIT = 4
@@ -31,7 +33,9 @@ _STATUS_NAMES = ["ANN_OK", "ANN_EINVAL", "ANN_ENOMEM", "ANN_EDEVICE", "ANN_EUNSU
 EXPORTED_SYMBOLS = ["ann_sq_train", "ann_sq_train_truncated", "ann_sq_encode", "ann_upload_index", "ann_free_index", "ann_trim_memory", "ann_query_prep",
                     "ann_search_batch", "ann_rescore", "ann_rerank", "ann_rerank_adaptive", "ann_bruteforce_topk", "ann_build_entry_table",
                     "ann_entry_scan", "ann_build_prs", "ann_build_prs_ratio", "ann_build_row_norms", "ann_schedule_queries", "ann_reserve_workspace",
-                    "ann_search_batch_static", "ann_default_expansions_per_step", "ann_last_error", "ann_version"]
+                    "ann_search_batch_static", "ann_layer_norm", "ann_layer_norm_backward", "ann_row_logprobs", "ann_row_logprobs_backward",
+                    "ann_layer_norm_backward_workspace", "ann_row_logprobs_workspace", "ann_row_logprobs_backward_workspace",
+                    "ann_default_expansions_per_step", "ann_last_error", "ann_version"]
 
 
 class AnnError(RuntimeError):
@@ -63,6 +67,12 @@ class SearchParams(ctypes.Structure):
                 ("reuse_folded_queries", ctypes.c_uint32), ("ef_per_query", ctypes.c_void_p)]
 
 
+class RowScores(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("rows", ctypes.c_void_p), ("n", ctypes.c_uint64), ("q_stride", ctypes.c_uint64),
+                ("row_stride", ctypes.c_uint64), ("nq", ctypes.c_uint32), ("d", ctypes.c_uint32), ("type", ctypes.c_uint32),
+                ("scale", ctypes.c_float), ("row_bias", ctypes.c_void_p), ("targets", ctypes.c_void_p)]
+
+
 def _load_library() -> ctypes.CDLL:
     if not LIB_PATH.exists():
         raise ImportError(f"{LIB_PATH} is missing: build the HIP library first "
@@ -89,8 +99,17 @@ def _load_library() -> ctypes.CDLL:
     lib.ann_build_entry_table.argtypes = [vp, u32, vp]
     lib.ann_entry_scan.argtypes = [vp, vp, u32, u32, vp, vp]
     lib.ann_schedule_queries.argtypes = [vp, u32, u32, vp, vp]
-    for name in EXPORTED_SYMBOLS[:-3]:
+    lib.ann_layer_norm.argtypes = [vp, u64, u32, u64, u32, vp, vp, u32, ctypes.c_float, vp, u64, vp, vp, vp]
+    lib.ann_layer_norm_backward.argtypes = [vp, u64, vp, u64, u64, u32, u32, vp, u32, vp, vp, vp, u64, vp, vp, vp, u64, vp]
+    lib.ann_row_logprobs.argtypes = [ctypes.POINTER(RowScores), u32, vp, vp, vp, vp, vp, vp, u64, vp]
+    lib.ann_row_logprobs_backward.argtypes = [ctypes.POINTER(RowScores), vp, vp, vp, vp, vp, u64, vp, u64, vp, vp, u64, vp]
+    for name in EXPORTED_SYMBOLS[:-6]:
         getattr(lib, name).restype = i32
+    lib.ann_layer_norm_backward_workspace.argtypes = [u64, u32]
+    lib.ann_row_logprobs_workspace.argtypes = [u32, u64, u32, u32, u32]
+    lib.ann_row_logprobs_backward_workspace.argtypes = [u32, u64, u32, u32]
+    for name in EXPORTED_SYMBOLS[-6:-3]:
+        getattr(lib, name).restype = u64
     lib.ann_default_expansions_per_step.argtypes = [u32, u32]
     lib.ann_default_expansions_per_step.restype = u32
     lib.ann_last_error.restype = ctypes.c_char_p
@@ -242,3 +261,46 @@ def ann_entry_scan(index, q, nq, n_entry, out_entry_ids, stream=None):
 
 def ann_bruteforce_topk(x, n, d, q, nq, k, metric, out_ids, out_dist, stream=None):
     _check(_lib.ann_bruteforce_topk(_ptr(x), n, d, _ptr(q), nq, k, metric, _ptr(out_ids), _ptr(out_dist), stream))
+
+
+def ann_layer_norm(x, n, dim, x_stride, type, weight, bias, weight_type, eps, y, y_stride, mean=None, rstd=None, stream=None):
+    _check(_lib.ann_layer_norm(_ptr(x), n, dim, x_stride, type, _ptr(weight), _ptr(bias), weight_type, eps, _ptr(y), y_stride,
+                               _ptr(mean), _ptr(rstd), stream))
+
+
+def ann_layer_norm_backward_workspace(n, dim) -> int:
+    return int(_lib.ann_layer_norm_backward_workspace(n, dim))
+
+
+def ann_layer_norm_backward(dy, dy_stride, x, x_stride, n, dim, type, weight, weight_type, mean, rstd, dx, dx_stride, dweight=None,
+                            dbias=None, workspace=None, workspace_bytes=0, stream=None):
+    _check(_lib.ann_layer_norm_backward(_ptr(dy), dy_stride, _ptr(x), x_stride, n, dim, type, _ptr(weight), weight_type, _ptr(mean),
+                                        _ptr(rstd), _ptr(dx), dx_stride, _ptr(dweight), _ptr(dbias), _ptr(workspace), workspace_bytes,
+                                        stream))
+
+
+def _row_scores(q, nq, q_stride, rows, n, row_stride, d, type, scale, row_bias, targets):
+    return ctypes.byref(RowScores(q=_ptr(q), rows=_ptr(rows), n=n, q_stride=q_stride, row_stride=row_stride, nq=nq, d=d, type=type,
+                                  scale=scale, row_bias=_ptr(row_bias), targets=_ptr(targets)))
+
+
+def ann_row_logprobs_workspace(nq, n, d, type, k=0) -> int:
+    return int(_lib.ann_row_logprobs_workspace(nq, n, d, type, k))
+
+
+def ann_row_logprobs(q, nq, q_stride, rows, n, row_stride, d, type, *, logprob, lse, scale=1.0, row_bias=None, targets=None, k=0,
+                     entropy=None, alt_ids=None, alt_logprobs=None, workspace=None, workspace_bytes=0, stream=None):
+    _check(_lib.ann_row_logprobs(_row_scores(q, nq, q_stride, rows, n, row_stride, d, type, scale, row_bias, targets), k, _ptr(logprob),
+                                 _ptr(entropy), _ptr(lse), _ptr(alt_ids), _ptr(alt_logprobs), _ptr(workspace), workspace_bytes, stream))
+
+
+def ann_row_logprobs_backward_workspace(nq, n, d, type) -> int:
+    return int(_lib.ann_row_logprobs_backward_workspace(nq, n, d, type))
+
+
+def ann_row_logprobs_backward(q, nq, q_stride, rows, n, row_stride, d, type, *, lse, scale=1.0, row_bias=None, targets=None, entropy=None,
+                              g_logprob=None, g_entropy=None, dq=None, dq_stride=0, drows=None, drows_stride=0, drow_bias=None,
+                              workspace=None, workspace_bytes=0, stream=None):
+    _check(_lib.ann_row_logprobs_backward(_row_scores(q, nq, q_stride, rows, n, row_stride, d, type, scale, row_bias, targets), _ptr(lse),
+                                          _ptr(entropy), _ptr(g_logprob), _ptr(g_entropy), _ptr(dq), dq_stride, _ptr(drows), drows_stride,
+                                          _ptr(drow_bias), _ptr(workspace), workspace_bytes, stream))
