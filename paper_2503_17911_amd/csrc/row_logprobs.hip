@@ -33,6 +33,48 @@ __device__ __forceinline__ void join(Stats &a, const Stats &b) {
   a.m = m;
 }
 
+// A lane's running statistics of one query.  The scores of a tile are summed by themselves and the tiles' sums
+// with what the last addition lost: over a million rows plain sums erred by 4.6e-6, ten times the rounding of the scores.
+struct Running {
+  float m = -3.402823466e38f, l = 0.0f, t = 0.0f, l_lost = 0.0f, t_lost = 0.0f;
+
+  static __device__ __forceinline__ void add(float &sum, float &lost, float v) {
+    v -= lost;
+    const float next = sum + v;
+    lost = (next - sum) - v;
+    sum = next;
+  }
+  // N scores and the largest of them.  MASKED: they are whole, and -infinity means a row left out; otherwise a score
+  // is s * scale, with c = scale log2 e.
+  template <bool MASKED, int N>
+  __device__ __forceinline__ void take(const float (&s)[N], float top, float c) {
+    const float next = fmaxf(m, top), step = fmaxf(m - next, kNothing), f = __builtin_amdgcn_exp2f(step * kLog2e);
+    // (for the same maximum: f = 1, step = 0, and these change nothing)
+    t = f * __builtin_fmaf(step, l, t), t_lost *= f;
+    l *= f, l_lost *= f;
+    m = next;
+    float sum = 0.0f, weighed = 0.0f;
+    const float m2 = m * kLog2e;
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+      if constexpr (MASKED) {
+        const float y = s[r] == -INFINITY ? kNothing : s[r] - m;
+        const float p = __builtin_amdgcn_exp2f(y * kLog2e);
+        sum += p;
+        weighed = __builtin_fmaf(p, y, weighed);
+      } else {
+        const float y = __builtin_fmaf(s[r], c, -m2);
+        const float p = __builtin_amdgcn_exp2f(y);
+        sum += p;
+        weighed = __builtin_fmaf(p, y, weighed);
+      }
+    }
+    add(l, l_lost, sum);
+    add(t, t_lost, MASKED ? weighed : weighed * kLn2);
+  }
+  __device__ __forceinline__ Stats stats() const { return {m, l, t}; }
+};
+
 // Rows of a group of 64: a wavefront's of a tile.  Of a group of 16: those of one half of the lanes in a block of 32.
 __host__ __device__ constexpr uint32_t group_count(uint32_t n, int group) { return group == 64 ? (n + 63) / 64 : (n + 31) / 32 * 2; }
 
@@ -51,9 +93,7 @@ __global__ __launch_bounds__(256) void row_scores_kernel(ScoreTable g, uint32_t 
   const Lines<T> X = {(const T *)g.rows, g.row_stride, g.n, g.d}, Q = {(const T *)g.q, g.q_stride, g.nq, g.d};
   const uint32_t n_groups = GROUP ? group_count(g.n, GROUP) : 0;
   const float c = g.scale * kLog2e;
-  Stats st[2];
-#pragma unroll
-  for (int j = 0; j < 2; ++j) st[j] = {-3.402823466e38f, 0.0f, 0.0f};
+  Running run[2];
   for (uint32_t tile = first; tile < last; ++tile) {
     const uint32_t row0 = tile * kTile;
     const bool whole = row0 + kTile <= g.n;
@@ -102,27 +142,10 @@ __global__ __launch_bounds__(256) void row_scores_kernel(ScoreTable g, uint32_t 
             }
           }
         }
-        const float m = fmaxf(st[j].m, fmaxf(top[0], top[1]));
-        const float step = fmaxf(st[j].m - m, kNothing), f = __builtin_amdgcn_exp2f(step * kLog2e);
-        float l = f * st[j].l, t = f * __builtin_fmaf(step, st[j].l, st[j].t), t2 = 0.0f;
-        const float m2 = m * kLog2e;
+        float all[32];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            if constexpr (MASKED) {
-              const float y = acc[i][j][r] == -INFINITY ? kNothing : acc[i][j][r] - m;
-              const float p = __builtin_amdgcn_exp2f(y * kLog2e);
-              l += p;
-              t = __builtin_fmaf(p, y, t);
-            } else {
-              const float y = __builtin_fmaf(acc[i][j][r], c, -m2);
-              const float p = __builtin_amdgcn_exp2f(y);
-              l += p;
-              t2 = __builtin_fmaf(p, y, t2);
-            }
-          }
-        st[j] = {m, l, MASKED ? t : __builtin_fmaf(t2, kLn2, t)};
+        for (int r = 0; r < 32; ++r) all[r] = acc[r / 16][j][r % 16];
+        run[j].template take<MASKED>(all, fmaxf(top[0], top[1]), c);
       }
     };
     if (BIAS || !whole)
@@ -132,9 +155,10 @@ __global__ __launch_bounds__(256) void row_scores_kernel(ScoreTable g, uint32_t 
   }
   // the two halves of a wavefront, then the two wavefronts that share queries
   __shared__ Stats other[2][64];
-  __syncthreads();
+  Stats st[2];
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
+    st[j] = run[j].stats();
     const LanePair m = lane_pair<false>(__float_as_uint(st[j].m)), l = lane_pair<false>(__float_as_uint(st[j].l)), t = lane_pair<false>(__float_as_uint(st[j].t));
     Stats a = {__uint_as_float(m.low), __uint_as_float(l.low), __uint_as_float(t.low)};
     const Stats b = {__uint_as_float(m.high), __uint_as_float(l.high), __uint_as_float(t.high)};
@@ -150,6 +174,242 @@ __global__ __launch_bounds__(256) void row_scores_kernel(ScoreTable g, uint32_t 
       const uint32_t q = qt * kTile + nw + j * 32 + lane;
       if (q < g.nq) stats[(uint64_t)split * g.nq + q] = make_float4(st[j].m, st[j].l, st[j].t, 0.0f);
     }
+  }
+}
+
+// Few queries: the rows are read once, straight into registers, and multiplied by blocks of 16 queries that
+// wait in LDS as the 16x16x32 instruction takes them.  Bound by reading the rows.  A wavefront takes 64 rows at a time, four
+// blocks of 16, and kSteps slices of 32 columns of them per round; the next round's are on their way meanwhile.  Row m of block b
+// of a pair is row 8 (m / 4) + 4 b + m % 4 of the pair's 32, so that blocks are the same groups of 16 as above.  The rows' norms
+// (for score_room) are summed on the way.
+constexpr int kStreamThreads = 512;
+constexpr int kStreamRows = 64;         // to a wavefront at a time
+constexpr uint32_t kStreamGroups = 256; // workgroups: one to a compute unit, eight wavefronts each
+constexpr uint32_t kStreamLds = 152u << 10;  // of the 160 KiB, for queries
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ f32x4 small_step(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 small_step(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+__device__ __forceinline__ float add_squares(const Unit<bf16_t> &u, float sum) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    const bf16x2 v = {u.v[e], u.v[e + 1]};
+    sum = __builtin_amdgcn_fdot2_f32_bf16(v, v, sum, false);
+  }
+  return sum;
+}
+__device__ __forceinline__ float add_squares(const Unit<f16_t> &u, float sum) {
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    const f16x2 v = {u.v[e], u.v[e + 1]};
+    sum = __builtin_amdgcn_fdot2(v, v, sum, false);
+  }
+  return sum;
+}
+__device__ __forceinline__ float add_squares(const Unit<float> &u, float sum) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(u.v[e], u.v[e], sum);
+  return sum;
+}
+
+template <typename T>
+constexpr int kSteps = sizeof(T) == 4 ? 2 : 4;  // 64 registers of rows on their way
+
+// NB: blocks of 16 queries.
+template <typename T, int NB, bool BIAS, int GROUP>
+__global__ __launch_bounds__(kStreamThreads) void row_stream_kernel(ScoreTable g, float4 *__restrict__ stats, float *__restrict__ group_max,
+                                                                    float *__restrict__ norms) {
+  typedef Operand16<T> O;
+  typedef typename O::E E;
+  constexpr int kWaves = kStreamThreads / kWave, S = kSteps<T>;
+  extern __shared__ __attribute__((aligned(16))) char dynamic[];  // [steps][parts][NB] pieces of 64 lanes x 16 bytes; later the wavefronts' statistics
+  const uint32_t steps = (g.d + 31) / 32, rounds = (steps + S - 1) / S;
+  const int lane = lane_id(), wave = (int)threadIdx.x / kWave, part = lane / 16;
+  for (uint32_t at = threadIdx.x; at < steps * NB * 64; at += kStreamThreads) {
+    const uint32_t q = at / 64 % NB * 16 + at % 16, step = at / (64 * NB), k = step * 32 + at % 64 / 16 * 8;
+    Unit<T> u;
+    load_unit(u, (const T *)g.q + q * g.q_stride + k, q < g.nq ? (int64_t)g.d - k : 0);
+#pragma unroll
+    for (int p = 0; p < O::kParts; ++p) *(uint4 *)(dynamic + (((uint64_t)step * O::kParts + p) * NB * 64 + at % (64 * NB)) * 16) = unit_part(u, p);
+  }
+  __syncthreads();
+  // blocks of 64 rows in turn to the wavefronts of the workgroup, which has a run of them to itself
+  const uint32_t blocks = (g.n + kStreamRows - 1) / kStreamRows;
+  const uint32_t first = (uint32_t)((uint64_t)blocks * blockIdx.x / gridDim.x), last = (uint32_t)((uint64_t)blocks * (blockIdx.x + 1) / gridDim.x);
+  const uint32_t n_groups = GROUP ? group_count(g.n, GROUP) : 0;
+  const float c = g.scale * kLog2e;
+  const T *rows = (const T *)g.rows;
+  const int in_block = lane % 16 / 4 * 8 + lane % 4;  // the lane's row of a pair's 32, of its first block
+  Unit<T> now[S][4], next[S][4];
+  // (rows behind the last are the last once more: they do not count; slices behind the last are not used)
+  const auto fetch = [&](Unit<T>(&u)[S][4], uint32_t block, uint32_t round) {
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      uint32_t row = block * kStreamRows + b / 2 * 32 + b % 2 * 4 + in_block;
+      row = row < g.n ? row : g.n - 1;
+      const T *x = rows + row * g.row_stride;
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        const uint32_t k = (round * S + s) * 32 + part * 8;
+        if ((round * S + s + 1) * 32 <= g.d)
+          load_unit(u[s][b], x + k, 8);
+        else
+          load_unit(u[s][b], x + k, (int64_t)g.d - k);
+      }
+    }
+  };
+  Running run[NB];
+  f32x4 acc[NB][4];
+  float squares[4] = {0.0f, 0.0f, 0.0f, 0.0f}, largest = 0.0f;
+  uint32_t block = first + wave, round = 0;
+  if (block < last) fetch(next, block, 0);
+  while (block < last) {
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) now[s][b] = next[s][b];
+    const bool ends = round + 1 == rounds;
+    const uint32_t next_block = ends ? block + kWaves : block, next_round = ends ? 0 : round + 1;
+    if (next_block < last) fetch(next, next_block, next_round);
+    if (round == 0) {
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) acc[j][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      if (round * S + s >= steps) break;
+      E q[O::kParts][NB];
+      const char *at = dynamic + (uint64_t)(round * S + s) * O::kParts * NB * 1024 + lane * 16;
+#pragma unroll
+      for (int p = 0; p < O::kParts; ++p)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) q[p][j] = *(const E *)(at + (p * NB + j) * 1024);
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        if constexpr (GROUP != 0) squares[b] = add_squares(now[s][b], squares[b]);
+        E x[O::kParts];
+#pragma unroll
+        for (int p = 0; p < O::kParts; ++p) x[p] = __builtin_bit_cast(E, unit_part(now[s][b], p));
+#pragma unroll
+        for (int sum = O::kParts - 1; sum >= 0; --sum)
+#pragma unroll
+          for (int p = 0; p <= sum; ++p)
+#pragma unroll
+            for (int j = 0; j < NB; ++j) acc[j][b] = small_step(x[p], q[sum - p][j], acc[j][b]);
+      }
+    }
+    if (ends) {
+      const uint32_t row0 = block * kStreamRows;
+      const bool whole = row0 + kStreamRows <= g.n;
+      if constexpr (GROUP != 0) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const uint32_t row = row0 + b / 2 * 32 + b % 2 * 4 + in_block;
+          const bool out = BIAS && g.bias && row < g.n && g.bias[row] == -INFINITY;
+          if (!out) largest = fmaxf(largest, squares[b]);
+          squares[b] = 0.0f;
+        }
+      }
+      float bias[16];
+      if (BIAS || !whole) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const uint32_t row = row0 + r / 8 * 32 + part * 8 + r % 8;  // (r / 4: the block)
+          bias[r] = row < g.n ? (BIAS && g.bias ? g.bias[row] : 0.0f) : -INFINITY;
+        }
+      }
+      const auto finish = [&](auto masked) {
+        constexpr bool MASKED = decltype(masked)::value;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+          float s[16], top[4];
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int i = b * 4 + r;
+              s[i] = acc[j][b][r];
+              if constexpr (MASKED) s[i] = bias[i] == -INFINITY ? -INFINITY : __builtin_fmaf(s[i], g.scale, bias[i]);
+              top[b] = r ? fmaxf(top[b], s[i]) : s[i];
+            }
+            if constexpr (!MASKED) top[b] *= g.scale;
+          }
+          const float all = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+          if constexpr (GROUP != 0) {
+            const uint32_t q = j * 16 + lane % 16;
+            const auto over_parts = [](float v) {  // the other lanes' of the same query
+              LanePair p = lane_pair<true>(__float_as_uint(v));
+              v = fmaxf(__uint_as_float(p.low), __uint_as_float(p.high));
+              p = lane_pair<false>(__float_as_uint(v));
+              return fmaxf(__uint_as_float(p.low), __uint_as_float(p.high));
+            };
+            float *out = group_max + (uint64_t)q * n_groups;
+            if constexpr (GROUP == 64) {
+              const float most = over_parts(all);
+              if (lane < 16 && q < g.nq) out[block] = most;
+            } else {
+#pragma unroll
+              for (int b = 0; b < 4; ++b) {
+                const float most = over_parts(top[b]);
+                if (part == b && q < g.nq && block * 4 + b < n_groups) out[block * 4 + b] = most;
+              }
+            }
+          }
+          run[j].template take<MASKED>(s, all, c);
+        }
+      };
+      if (BIAS || !whole)
+        finish(std::true_type());
+      else
+        finish(std::false_type());
+    }
+    block = next_block, round = next_round;
+  }
+  // lanes that share a query, then wavefronts
+  __syncthreads();
+  Stats *room = (Stats *)dynamic;  // [kWaves][NB * 16]
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    Stats a = run[j].stats();
+#pragma unroll
+    for (int far = 16; far < 64; far *= 2) {
+      const Stats b = {__int_as_float(xor_lane_i32(__float_as_int(a.m), far)), __int_as_float(xor_lane_i32(__float_as_int(a.l), far)),
+                       __int_as_float(xor_lane_i32(__float_as_int(a.t), far))};
+      join(a, b);
+    }
+    if (lane < 16) room[wave * NB * 16 + j * 16 + lane] = a;
+  }
+  __shared__ float most[kWaves];
+  if constexpr (GROUP != 0) {
+    // a row's norm is the sum of its four lanes' shares, at most the sum of their largest
+    float v = largest;
+    v = fmaxf(v, __int_as_float(dpp_i32<kDppQuadXor1>(__float_as_int(v))));
+    v = fmaxf(v, __int_as_float(dpp_i32<kDppQuadXor2>(__float_as_int(v))));
+    v = fmaxf(v, __int_as_float(dpp_i32<kDppRowHalfMirror>(__float_as_int(v))));
+    v = fmaxf(v, __int_as_float(dpp_i32<kDppRowMirror>(__float_as_int(v))));
+    LanePair p = lane_pair<true>(__float_as_uint(v));
+    v = __uint_as_float(p.low) + __uint_as_float(p.high);
+    p = lane_pair<false>(__float_as_uint(v));
+    v = __uint_as_float(p.low) + __uint_as_float(p.high);
+    if (lane == 0) most[wave] = v;
+  }
+  __syncthreads();
+  if (threadIdx.x < NB * 16 && threadIdx.x < g.nq) {
+    Stats a = room[threadIdx.x];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) join(a, room[w * NB * 16 + threadIdx.x]);
+    stats[(uint64_t)blockIdx.x * g.nq + threadIdx.x] = make_float4(a.m, a.l, a.t, 0.0f);
+  }
+  if (GROUP != 0 && threadIdx.x == 0) {
+    float v = most[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) v = fmaxf(v, most[w]);
+    norms[blockIdx.x] = v;
   }
 }
 
@@ -302,8 +562,9 @@ __global__ __launch_bounds__(kFinishThreads) void row_finish_kernel(FinishArgs a
     const float *gm = a.group_max + (uint64_t)i * n_groups;
     float x_norm = 0.0f, top = -INFINITY;
     for (uint32_t c = tid; c < a.norm_runs; c += kFinishThreads) x_norm = fmaxf(x_norm, a.norms[c]);
-    x_norm = sqrtf(block_max(x_norm, room32));
-    const float q_norm = sqrtf((float)block_sum((double)qsq, room, wave));
+    const float lost = (float)g.d * 0x1p-126f;  // squares below the smallest normal number may have gone
+    x_norm = sqrtf(block_max(x_norm, room32) + lost);
+    const float q_norm = sqrtf((float)block_sum((double)qsq, room, wave) + lost);
     for (uint32_t c = tid; c < n_groups; c += kFinishThreads) top = fmaxf(top, gm[c]);
     // The k-th largest of the lanes' maxima: at least k groups reach it.
     tops[tid] = top;
@@ -378,24 +639,39 @@ __global__ __launch_bounds__(kFinishThreads) void row_finish_kernel(FinishArgs a
 struct ForwardPlan {
   uint32_t q_tiles = 0, splits = 0, norm_runs = 0;
   int group = 0;
+  int blocks = 0;  // of 16 queries, if the rows are streamed
   uint64_t stats_at = 0, groups_at = 0, norms_at = 0;
   Parts parts;
 };
 
-static ForwardPlan forward_plan(uint32_t nq, uint64_t n, uint32_t d, uint32_t k) {
+// Bytes of queries in LDS that the streaming kernel would take.
+static uint64_t stream_lds(int blocks, uint32_t d, uint32_t type) {
+  const uint64_t queries = (d + 31) / 32 * (type == ANN_F32 ? 3ull : 1ull) * blocks * 1024, stats = sizeof(Stats) * 16ull * blocks * (kStreamThreads / kWave);
+  return queries > stats ? queries : stats;
+}
+
+static ForwardPlan forward_plan(uint32_t nq, uint64_t n, uint32_t d, uint32_t type, uint32_t k) {
   ForwardPlan p;
   if (nq == 0 || n == 0) return p;
-  p.q_tiles = (nq + kTile - 1) / kTile;
-  const uint32_t row_tiles = (uint32_t)((n + kTile - 1) / kTile);
-  uint32_t want = (kSplitTarget + p.q_tiles - 1) / p.q_tiles;
-  want = (want + 7) / 8 * 8;
-  p.splits = want < row_tiles ? want : row_tiles;
+  // (four blocks of fp32 queries and the rows' parts are more registers than a wavefront has)
+  const int blocks = nq <= 16 ? 1 : nq <= 32 ? 2 : 4;
+  if (nq <= (type == ANN_F32 ? 32 : 64) && stream_lds(blocks, d, type) <= kStreamLds) {
+    p.blocks = blocks;
+    const uint64_t most = (n + kStreamRows - 1) / kStreamRows;
+    p.splits = most < kStreamGroups ? (uint32_t)most : kStreamGroups;
+  } else {
+    p.q_tiles = (nq + kTile - 1) / kTile;
+    const uint32_t row_tiles = (uint32_t)((n + kTile - 1) / kTile);
+    uint32_t want = (kSplitTarget + p.q_tiles - 1) / p.q_tiles;
+    want = (want + 7) / 8 * 8;
+    p.splits = want < row_tiles ? want : row_tiles;
+  }
   // What a group costs: 8 n / group bytes per query written and read, and about k group d elements read again.
   if (k) p.group = 4 * n >= 1024ull * k * d ? 64 : 16;
   p.stats_at = p.parts.take((uint64_t)p.splits * nq * sizeof(float4));
   if (k) {
     p.groups_at = p.parts.take((uint64_t)nq * group_count((uint32_t)n, p.group) * sizeof(float));
-    p.norm_runs = (uint32_t)((n + 15) / 16 < kNormRuns ? (n + 15) / 16 : kNormRuns);
+    p.norm_runs = p.blocks ? p.splits : (uint32_t)((n + 15) / 16 < kNormRuns ? (n + 15) / 16 : kNormRuns);
     p.norms_at = p.parts.take(p.norm_runs * sizeof(float));
   }
   return p;
@@ -407,10 +683,28 @@ static ann_status forward(const ann_row_scores &s, uint32_t k, const ForwardPlan
   if (s.n) {
     float4 *stats = (float4 *)(ws + p.stats_at);
     float *groups = (float *)(ws + p.groups_at), *norms = (float *)(ws + p.norms_at);
-    const uint32_t grid = p.q_tiles * ((p.splits + 7) / 8 * 8);
     const bool bias = g.bias || g.scale < 0.0f;
+    hipError_t refused = hipSuccess;
     const auto run = [&](auto with_bias, auto group) {
-      row_scores_kernel<T, decltype(with_bias)::value, decltype(group)::value><<<grid, 256, 0, st>>>(g, p.q_tiles, p.splits, stats, groups);
+      constexpr bool BIAS = decltype(with_bias)::value;
+      constexpr int GROUP = decltype(group)::value;
+      if (!p.blocks) {
+        row_scores_kernel<T, BIAS, GROUP><<<p.q_tiles * ((p.splits + 7) / 8 * 8), 256, 0, st>>>(g, p.q_tiles, p.splits, stats, groups);
+        if (GROUP) row_norms_kernel<T><<<p.norm_runs, 256, 0, st>>>(g, norms);
+        return;
+      }
+      const auto stream = [&](auto blocks) {
+        const auto kernel = row_stream_kernel<T, decltype(blocks)::value, BIAS, GROUP>;
+        const uint32_t lds = (uint32_t)stream_lds(p.blocks, g.d, s.type);
+        if (lds > 64u << 10) refused = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (refused == hipSuccess) kernel<<<p.splits, kStreamThreads, lds, st>>>(g, stats, groups, norms);
+      };
+      if (p.blocks == 1)
+        stream(std::integral_constant<int, 1>());
+      else if (p.blocks == 2)
+        stream(std::integral_constant<int, 2>());
+      else if constexpr (sizeof(T) == 2)
+        stream(std::integral_constant<int, 4>());
     };
     const auto run_group = [&](auto with_bias) {
       if (p.group == 0)
@@ -424,11 +718,8 @@ static ann_status forward(const ann_row_scores &s, uint32_t k, const ForwardPlan
       run_group(std::true_type());
     else
       run_group(std::false_type());
+    ANN_HIP(refused);
     ANN_HIP(hipGetLastError());
-    if (k) {
-      row_norms_kernel<T><<<p.norm_runs, 256, 0, st>>>(g, norms);
-      ANN_HIP(hipGetLastError());
-    }
     f.stats = stats, f.group_max = groups, f.norms = norms, f.splits = p.splits, f.norm_runs = p.norm_runs;
   }
   const uint32_t lds = (g.d + 7) / 8 * 8 * sizeof(float);
@@ -466,9 +757,9 @@ ann_status check_workspace(const char *what, const void *workspace, uint64_t byt
 
 using namespace ann;
 
-extern "C" uint64_t ann_row_logprobs_workspace(uint32_t nq, uint64_t n, uint32_t d, uint32_t, uint32_t k) {
+extern "C" uint64_t ann_row_logprobs_workspace(uint32_t nq, uint64_t n, uint32_t d, uint32_t type, uint32_t k) {
   if (n >= (1ull << 31) || nq >= (1u << 31) || k > ANN_MAX_ALTERNATIVES) return 0;
-  return forward_plan(nq, n, d, k).parts.bytes;
+  return forward_plan(nq, n, d, type, k).parts.bytes;
 }
 
 extern "C" ann_status ann_row_logprobs(const ann_row_scores *scores, uint32_t k, float *logprob, float *entropy, float *lse, uint32_t *alt_ids,
@@ -479,7 +770,7 @@ extern "C" ann_status ann_row_logprobs(const ann_row_scores *scores, uint32_t k,
   if (!logprob || !lse) return fail(ANN_EINVAL, "ann_row_logprobs: logprob or lse is NULL");
   if ((k != 0) != (alt_ids != nullptr) || (k != 0) != (alt_logprobs != nullptr))
     return fail(ANN_EINVAL, "ann_row_logprobs: alt_ids and alt_logprobs go with k > 0, k = %u", k);
-  const ForwardPlan p = forward_plan(scores->nq, scores->n, scores->d, k);
+  const ForwardPlan p = forward_plan(scores->nq, scores->n, scores->d, scores->type, k);
   if (ann_status s = check_workspace("ann_row_logprobs", workspace, workspace_bytes, p.parts.bytes)) return s;
   FinishArgs f = {};
   f.g = score_table(*scores);
