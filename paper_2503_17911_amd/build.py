@@ -18,11 +18,14 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # reference bit for bit; fused multiply-adds are written explicitly (fmaf).
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off", "-I", str(INCLUDE), "-I", str(CSRC),
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument"]
+# Sources whose kernels work on the matrix instructions' results with ordinary ones: accumulators in ordinary
+# registers (else every element is copied out of the accumulation registers first).
+OWN_FLAGS = {s: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for s in ("row_logprobs.hip", "row_logprobs_grad.hip")}
 
 
 def _compile(src: str) -> Path:
     obj = LIBDIR / (src + ".o")
-    cmd = [HIPCC, *FLAGS, "-c", str(CSRC / src), "-o", str(obj)]
+    cmd = [HIPCC, *FLAGS, *OWN_FLAGS.get(src, []), "-c", str(CSRC / src), "-o", str(obj)]
     r = subprocess.run(cmd, capture_output=True, text=True)
     err = "\n".join(l for l in r.stderr.splitlines() if "packed-fp32-ops" not in l)
     if r.returncode != 0:

@@ -18,7 +18,7 @@
 namespace ann {
 
 constexpr uint32_t kNormRuns = 512;     // workgroups that look for the largest row norm
-constexpr uint32_t kSplitTarget = 1536; // workgroups of the product kernel: two rounds of three to a compute unit
+constexpr uint32_t kSplitTarget = 6144; // workgroups of the product kernel: two rounds of three to a compute unit
 constexpr float kNothing = -1000.0f;    // an exponent whose power is zero, and finite
 
 struct Stats {
@@ -33,26 +33,31 @@ __device__ __forceinline__ void join(Stats &a, const Stats &b) {
   a.m = m;
 }
 
-// A lane's running statistics of one query.  The scores of a tile are summed by themselves and the tiles' sums
-// with what the last addition lost: over a million rows plain sums erred by 4.6e-6, ten times the rounding of the scores.
+// A lane's running statistics of one query: l = sum exp(s - m), t = sum exp(s - m) (s - m).  The reference m need not be the
+// largest score: it is raised when one lies kSlack above it, which is seldom, and nothing is scaled in between.  The scores of a tile are
+// summed by themselves and the tiles' sums with what the last addition lost: over a million rows plain sums erred by
+// 4.6e-6, ten times the rounding of the scores.
+constexpr float kSlack = 20.0f;  // exp(20) times 2^31 rows is far from fp32's end
 struct Running {
   float m = -3.402823466e38f, l = 0.0f, t = 0.0f, l_lost = 0.0f, t_lost = 0.0f;
 
+  __device__ __forceinline__ bool behind(float top) const { return top > m + kSlack; }
+  __device__ __forceinline__ void raise(float top) {
+    const float next = behind(top) ? top : m, step = fmaxf(m - next, kNothing), f = __builtin_amdgcn_exp2f(step * kLog2e);
+    t = f * __builtin_fmaf(step, l, t), t_lost *= f;
+    l *= f, l_lost *= f;
+    m = next;
+  }
   static __device__ __forceinline__ void add(float &sum, float &lost, float v) {
     v -= lost;
     const float next = sum + v;
     lost = (next - sum) - v;
     sum = next;
   }
-  // N scores and the largest of them.  MASKED: they are whole, and -infinity means a row left out; otherwise a score
+  // N scores, none of which lies far above m.  MASKED: they are whole, and -infinity means a row left out; otherwise a score
   // is s * scale, with c = scale log2 e.
   template <bool MASKED, int N>
-  __device__ __forceinline__ void take(const float (&s)[N], float top, float c) {
-    const float next = fmaxf(m, top), step = fmaxf(m - next, kNothing), f = __builtin_amdgcn_exp2f(step * kLog2e);
-    // (for the same maximum: f = 1, step = 0, and these change nothing)
-    t = f * __builtin_fmaf(step, l, t), t_lost *= f;
-    l *= f, l_lost *= f;
-    m = next;
+  __device__ __forceinline__ void take(const float (&s)[N], float c) {
     float sum = 0.0f, weighed = 0.0f;
     const float m2 = m * kLog2e;
 #pragma unroll
@@ -77,6 +82,54 @@ struct Running {
 
 // Rows of a group of 64: a wavefront's of a tile.  Of a group of 16: those of one half of the lanes in a block of 32.
 __host__ __device__ constexpr uint32_t group_count(uint32_t n, int group) { return group == 64 ? (n + 63) / 64 : (n + 31) / 32 * 2; }
+
+// A block of 32 rows x 32 queries, rows down the registers and queries along the lanes.  MASKED: bias[32] (LDS) is added, -infinity
+// where a row does not count.  Returns the lane's largest score (16 rows').
+template <bool MASKED>
+__device__ __forceinline__ float largest_of(f32x16 &acc, const float *bias, float scale) {
+  if constexpr (MASKED) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float b = bias[block_row(r)];
+      acc[r] = b == -INFINITY ? -INFINITY : __builtin_fmaf(acc[r], scale, b);
+    }
+  }
+  float top = acc[0];
+#pragma unroll
+  for (int r = 1; r < 16; ++r) top = fmaxf(top, acc[r]);
+  return MASKED ? top : top * scale;
+}
+template <bool MASKED>
+__device__ __forceinline__ void take_block(const f32x16 &acc, Running &run, float c) {
+  float s[16];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s[r] = acc[r];
+  run.template take<MASKED>(s, c);
+}
+
+// Writes the largest scores of the groups of 64 rows from row0, of which the lane has seen the halves of two blocks.
+template <int GROUP>
+__device__ __forceinline__ void put_groups(float top0, float top1, uint32_t q, uint32_t nq, uint32_t row0, uint32_t n_groups, float *__restrict__ group_max) {
+  const int lane = lane_id();
+  float *out = group_max + (uint64_t)q * n_groups;
+  if constexpr (GROUP == 64) {
+    const LanePair p = lane_pair<false>(__float_as_uint(fmaxf(top0, top1)));
+    const float all = fmaxf(__uint_as_float(p.low), __uint_as_float(p.high));
+    if (lane < 32 && q < nq && row0 / 64 < n_groups) out[row0 / 64] = all;
+  } else if constexpr (GROUP == 16) {
+    const uint32_t at = row0 / 16 + lane / 32;
+    if (q < nq && at < n_groups) out[at] = top0;
+    if (q < nq && at + 2 < n_groups) out[at + 2] = top1;
+  }
+}
+
+// The statistics of the two lanes, 32 apart, that share a query.
+__device__ __forceinline__ Stats join_halves(const Stats &s) {
+  const LanePair m = lane_pair<false>(__float_as_uint(s.m)), l = lane_pair<false>(__float_as_uint(s.l)), t = lane_pair<false>(__float_as_uint(s.t));
+  Stats a = {__uint_as_float(m.low), __uint_as_float(l.low), __uint_as_float(t.low)};
+  join(a, {__uint_as_float(m.high), __uint_as_float(l.high), __uint_as_float(t.high)});
+  return a;
+}
 
 // BIAS: rows may be left out, or the scale is negative.
 template <typename T, bool BIAS, int GROUP>
@@ -107,45 +160,23 @@ __global__ __launch_bounds__(256) void row_scores_kernel(ScoreTable g, uint32_t 
     }
     const auto finish = [&](auto masked) {
       constexpr bool MASKED = decltype(masked)::value;
+      float top[2][2];
+      bool behind = false;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        float top[2];
-        if constexpr (MASKED) {
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < 2; ++i) top[i][j] = largest_of<MASKED>(acc[i][j], row_bias + mw + i * 32, g.scale);
+        behind |= run[j].behind(fmaxf(top[0][j], top[1][j]));
+      }
+      if (__any(behind)) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const float bias = row_bias[mw + i * 32 + block_row(r)];
-              acc[i][j][r] = bias == -INFINITY ? -INFINITY : __builtin_fmaf(acc[i][j][r], g.scale, bias);
-            }
-        }
+        for (int j = 0; j < 2; ++j) run[j].raise(fmaxf(top[0][j], top[1][j]));
+      }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          top[i] = acc[i][j][0];
+      for (int j = 0; j < 2; ++j) {
+        put_groups<GROUP>(top[0][j], top[1][j], qt * kTile + nw + j * 32 + lane % 32, g.nq, row0 + mw, n_groups, group_max);
 #pragma unroll
-          for (int r = 1; r < 16; ++r) top[i] = fmaxf(top[i], acc[i][j][r]);
-          if constexpr (!MASKED) top[i] *= g.scale;
-        }
-        if constexpr (GROUP != 0) {
-          const uint32_t q = qt * kTile + nw + j * 32 + lane % 32;
-          if constexpr (GROUP == 64) {
-            const float both = fmaxf(top[0], top[1]);
-            const LanePair p = lane_pair<false>(__float_as_uint(both));
-            const float all = fmaxf(__uint_as_float(p.low), __uint_as_float(p.high));
-            const uint32_t at = (row0 + mw) / 64;
-            if (lane < 32 && q < g.nq && at < n_groups) group_max[(uint64_t)q * n_groups + at] = all;
-          } else {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const uint32_t at = (row0 + mw + i * 32) / 32 * 2 + lane / 32;
-              if (q < g.nq && at < n_groups) group_max[(uint64_t)q * n_groups + at] = top[i];
-            }
-          }
-        }
-        float all[32];
-#pragma unroll
-        for (int r = 0; r < 32; ++r) all[r] = acc[r / 16][j][r % 16];
-        run[j].template take<MASKED>(all, fmaxf(top[0], top[1]), c);
+        for (int i = 0; i < 2; ++i) take_block<MASKED>(acc[i][j], run[j], c);
       }
     };
     if (BIAS || !whole)
@@ -158,13 +189,8 @@ __global__ __launch_bounds__(256) void row_scores_kernel(ScoreTable g, uint32_t 
   Stats st[2];
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    st[j] = run[j].stats();
-    const LanePair m = lane_pair<false>(__float_as_uint(st[j].m)), l = lane_pair<false>(__float_as_uint(st[j].l)), t = lane_pair<false>(__float_as_uint(st[j].t));
-    Stats a = {__uint_as_float(m.low), __uint_as_float(l.low), __uint_as_float(t.low)};
-    const Stats b = {__uint_as_float(m.high), __uint_as_float(l.high), __uint_as_float(t.high)};
-    join(a, b);
-    st[j] = a;
-    if (wave >= 2 && lane < 32) other[wave % 2][j * 32 + lane] = a;
+    st[j] = join_halves(run[j].stats());
+    if (wave >= 2 && lane < 32) other[wave % 2][j * 32 + lane] = st[j];
   }
   __syncthreads();
   if (wave < 2 && lane < 32) {
@@ -174,6 +200,140 @@ __global__ __launch_bounds__(256) void row_scores_kernel(ScoreTable g, uint32_t 
       const uint32_t q = qt * kTile + nw + j * 32 + lane;
       if (q < g.nq) stats[(uint64_t)split * g.nq + q] = make_float4(st[j].m, st[j].l, st[j].t, 0.0f);
     }
+  }
+}
+
+// Short rows of 16 bits, KS slices of 16 columns: the queries stay in registers, as the matrix instruction takes them, 64 to a
+// wavefront, and tiles of 64 rows pass by in LDS.  With 128 columns a score costs 256 operations on the matrix cores and
+// an exponential with four more instructions, so the end of a block counts as much as its product: the product of a block of 32 rows and
+// the end of the one before it are one stretch of code, so that the matrix cores work meanwhile.  What is left is bound by the
+// instructions of the end, so addresses are kept cheap: lines of LDS are 16 bytes apart from a power of two (eight
+// lines read side by side hit all banks, and every piece lies at a constant distance), and offsets within a tile are 32 bits.
+constexpr int kShortRows = 64, kShortQueries = 256;
+constexpr uint64_t kShortStride = 1u << 24;  // longest row stride
+
+template <typename T, int KS, bool BIAS, int GROUP>
+__global__ __launch_bounds__(256, 2) void row_scores_short_kernel(ScoreTable g, uint32_t q_tiles, uint32_t splits, float4 *__restrict__ stats,
+                                                                  float *__restrict__ group_max) {
+  typedef typename Operand16<T>::E E;
+  constexpr int kSlots = 2 * KS, kLine = KS * 32 + 16, kUnits = (kShortRows * kSlots + 255) / 256;
+  __shared__ __attribute__((aligned(16))) char lds[2][kShortRows * kLine];
+  __shared__ float row_bias[4][kShortRows];  // (of a tile: written while some wavefront may still read that of two tiles before)
+  // workgroup b runs on die b mod 8: a die takes all queries through its own part of the rows
+  const uint32_t b8 = blockIdx.x / 8, qt = b8 % q_tiles, split = b8 / q_tiles * 8 + blockIdx.x % 8;
+  if (split >= splits) return;
+  const uint32_t tiles = (g.n + kShortRows - 1) / kShortRows;
+  const uint32_t first = (uint32_t)((uint64_t)tiles * split / splits), last = (uint32_t)((uint64_t)tiles * (split + 1) / splits);
+  const int wave = (int)threadIdx.x / kWave, lane = lane_id();
+  const T *rows = (const T *)g.rows;
+  const uint32_t n_groups = GROUP ? group_count(g.n, GROUP) : 0, q = qt * kShortQueries + wave * 64 + lane % 32;  // (and q + 32)
+  const float c = g.scale * kLog2e;
+  E query[2][KS];
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) {
+      const uint32_t k = kk * 16 + lane / 32 * 8;
+      Unit<T> u;
+      load_unit(u, (const T *)g.q + (q + j * 32) * g.q_stride + k, q + j * 32 < g.nq ? (int64_t)g.d - k : 0);
+      query[j][kk] = __builtin_bit_cast(E, u);
+    }
+  Unit<T> u[kUnits];
+  uint32_t from[kUnits], to[kUnits];
+#pragma unroll
+  for (int i = 0; i < kUnits; ++i) {
+    const uint32_t at = threadIdx.x + 256 * i, line = at / kSlots, slot = at % kSlots;
+    from[i] = (line * (uint32_t)g.row_stride + slot * 8) * sizeof(T);
+    to[i] = line * kLine + slot * 16;
+  }
+  constexpr bool kEven = kUnits * 256 == kShortRows * kSlots;  // every lane has as many units
+  const auto fetch = [&](uint32_t tile) {
+    const char *base = (const char *)(rows + (uint64_t)tile * kShortRows * g.row_stride);
+    if (KS * 16 == g.d && (tile + 1) * kShortRows <= g.n) {
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i)
+        if (kEven || threadIdx.x + 256 * i < kShortRows * kSlots) load_unit(u[i], (const T *)(base + from[i]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) {
+        const uint32_t at = threadIdx.x + 256 * i, row = tile * kShortRows + at / kSlots, k = at % kSlots * 8;
+        if (kEven || at < kShortRows * kSlots) load_unit(u[i], (const T *)(base + from[i]), row < g.n ? (int64_t)g.d - k : 0);
+      }
+    }
+  };
+  // Tile into LDS, the next one on its way.  (One barrier per tile: whoever writes this half again has met the others at the next tile's.)
+  const auto enter = [&](uint32_t tile) {
+    char *at = lds[tile & 1];
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i)
+      if (kEven || threadIdx.x + 256 * i < kShortRows * kSlots) *(uint4 *)(at + to[i]) = unit_part(u[i], 0);
+    const uint32_t row = tile * kShortRows + threadIdx.x;
+    if ((BIAS || tile * kShortRows + kShortRows > g.n) && threadIdx.x < kShortRows)
+      row_bias[tile & 3][threadIdx.x] = row < g.n ? (BIAS && g.bias ? g.bias[row] : 0.0f) : -INFINITY;
+    __syncthreads();
+    if (tile + 1 < last) fetch(tile + 1);
+  };
+  const auto product = [&](f32x16(&acc)[2], uint32_t tile, int half) {
+    const char *at = lds[tile & 1] + lane % 32 * kLine + lane / 32 * 16;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[j][r] = 0.0f;
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) {
+      const E x = *(const E *)(at + half * 32 * kLine + kk * 32);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) acc[j] = matrix_step(x, query[j][kk], acc[j]);
+    }
+  };
+  Running run[2];
+  float top[2][2];  // of either half of a tile
+  // The scores of a half of a tile are taken on while `also` (the next half's product) is formed.
+  const auto end = [&](f32x16(&past)[2], uint32_t tile, int half, auto also) {
+    const auto with = [&](auto masked) {
+      constexpr bool MASKED = decltype(masked)::value;
+      bool behind = false;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        top[half][j] = largest_of<MASKED>(past[j], row_bias[tile & 3] + half * 32, g.scale);
+        behind |= run[j].behind(top[half][j]);
+      }
+      if (__any(behind)) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) run[j].raise(top[half][j]);
+      }
+      also();
+#pragma unroll
+      for (int j = 0; j < 2; ++j) take_block<MASKED>(past[j], run[j], c);
+    };
+    if (BIAS || tile * kShortRows + kShortRows > g.n)
+      with(std::true_type());
+    else
+      with(std::false_type());
+    if (GROUP != 0 && half) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) put_groups<GROUP>(top[0][j], top[1][j], q + j * 32, g.nq, tile * kShortRows, n_groups, group_max);
+    }
+  };
+  if (first < last) {
+    f32x16 upper[2], lower[2];
+    fetch(first);
+    enter(first);
+    product(upper, first, 0);
+    for (uint32_t tile = first; tile < last; ++tile) {
+      end(upper, tile, 0, [&] { product(lower, tile, 1); });
+      if (tile + 1 < last) {
+        enter(tile + 1);
+        end(lower, tile, 1, [&] { product(upper, tile + 1, 0); });
+      } else {
+        end(lower, tile, 1, [] {});
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const Stats s = join_halves(run[j].stats());
+    if (lane < 32 && q + j * 32 < g.nq) stats[(uint64_t)split * g.nq + q + j * 32] = make_float4(s.m, s.l, s.t, 0.0f);
   }
 }
 
@@ -360,7 +520,8 @@ __global__ __launch_bounds__(kStreamThreads) void row_stream_kernel(ScoreTable g
               }
             }
           }
-          run[j].template take<MASKED>(s, all, c);
+          if (__any(run[j].behind(all))) run[j].raise(all);
+          run[j].template take<MASKED>(s, c);
         }
       };
       if (BIAS || !whole)
@@ -450,9 +611,11 @@ __device__ __forceinline__ float score_room(uint32_t d, bool parts, float q_norm
   return ((parts ? 6.0f : 1.0f) * (float)d + 64.0f) * 0x1p-23f * size + 0x1p-22f * (fabsf(largest) + size);
 }
 
-constexpr int kFinishThreads = 256;
-constexpr uint32_t kGroupRange = 4096;  // groups that are looked through at a time
-constexpr uint32_t kBest = 1024;        // candidates that are kept at a time
+constexpr uint32_t kListed = 1024;      // groups that are taken up at a time
+constexpr uint32_t kBest = 512;         // scored candidates that are kept at a time
+constexpr uint32_t kFewQueries = 512;   // fewer get a workgroup of 1,024 lanes each
+constexpr uint32_t kInFlight = 8;       // groups' scores that a lane reads at once
+constexpr uint32_t kTops = 256;         // largest scores of so many parts of the groups bound the k-th
 
 struct FinishArgs {
   ScoreTable g;
@@ -464,129 +627,172 @@ struct FinishArgs {
   uint32_t *alt_ids;
 };
 
-template <typename F>
-__device__ __forceinline__ double block_sum(double v, double *room, F wave_index) {
-  v = group_sum_f64<64>(v);
-  __syncthreads();
-  if (lane_id() == 0) room[wave_index] = v;
-  __syncthreads();
-  double s = 0.0;
-#pragma unroll
-  for (int w = 0; w < kFinishThreads / kWave; ++w) s += room[w];
-  return s;
-}
-__device__ __forceinline__ float block_max(float v, float *room) {
-  v = wave_max_f32(v);
-  __syncthreads();
-  if (lane_id() == 0) room[threadIdx.x / kWave] = v;
-  __syncthreads();
-  float s = room[0];
-#pragma unroll
-  for (int w = 1; w < kFinishThreads / kWave; ++w) s = fmaxf(s, room[w]);
-  return s;
-}
-
-// The part of lane `part` of LPR of a row's product with the query (in LDS), in fp64.
-template <typename T, int LPR>
-__device__ __forceinline__ double exact_dot(const T *x, const float *q, uint32_t d, uint32_t part) {
+// A row's product with the query (in LDS, zero from d on) in fp64, by a whole wavefront.
+template <typename T>
+__device__ __forceinline__ double exact_dot(const T *x, const float *q, uint32_t d) {
   double sum = 0.0;
-  for (uint32_t k = part * 8; k < d; k += LPR * 8) {
+  for (uint32_t k = lane_id() * 8; k < d; k += 512) {
     Unit<T> u;
     load_unit(u, x + k, (int64_t)d - k);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum = __builtin_fma((double)to_f32(u.v[e]), (double)q[k + e], sum);  // (q is zero from d on)
+    for (int e = 0; e < 8; ++e) sum = __builtin_fma((double)to_f32(u.v[e]), (double)q[k + e], sum);
   }
-  return sum;
+  return group_sum_f64<64>(sum);
 }
 
-// One workgroup per query: joins the splits' statistics, scores the given row, finds the alternatives.
-template <typename T, int GROUP>
-__global__ __launch_bounds__(kFinishThreads) void row_finish_kernel(FinishArgs a) {
+// Row `in` of a group.
+template <int GROUP>
+__device__ __forceinline__ uint64_t group_row(uint32_t group, uint32_t in) {
+  return GROUP == 64 ? (uint64_t)group * 64 + in : (uint64_t)(group / 2) * 32 + in / 4 * 8 + group % 2 * 4 + in % 4;
+}
+
+// Sum over LANES (16 or 64) lanes.
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v) {
+  v += __int_as_float(dpp_i32<kDppQuadXor1>(__float_as_int(v)));
+  v += __int_as_float(dpp_i32<kDppQuadXor2>(__float_as_int(v)));
+  v += __int_as_float(dpp_i32<kDppRowHalfMirror>(__float_as_int(v)));
+  v += __int_as_float(dpp_i32<kDppRowMirror>(__float_as_int(v)));
+  if constexpr (LANES == 64) {
+    LanePair p = lane_pair<true>(__float_as_uint(v));
+    v = __uint_as_float(p.low) + __uint_as_float(p.high);
+    p = lane_pair<false>(__float_as_uint(v));
+    v = __uint_as_float(p.low) + __uint_as_float(p.high);
+  }
+  return v;
+}
+
+// One workgroup per query: joins the splits' statistics, scores the given row, finds the alternatives.  Bound by the time
+// that one read after another takes, so as much as can be is read at once, and the workgroup waits for itself as seldom
+// as it can.  The rows of the groups in question are scored in fp32 first, 16 lanes to a row and several rows
+// of a lane in flight, and in fp64 where that leaves them among the best.
+template <typename T, int GROUP, int THREADS>
+__global__ __launch_bounds__(THREADS, THREADS == 256 ? 5 : 4) void row_finish_kernel(FinishArgs a) {
+  constexpr int kWaves = THREADS / kWave;
+  constexpr uint32_t kSharers = THREADS / kTops;  // lanes to one of the tops
   extern __shared__ __attribute__((aligned(16))) char dynamic[];
-  float *q = (float *)dynamic;  // [d rounded up to 8]
-  __shared__ double room[kFinishThreads / kWave];
-  __shared__ float room32[kFinishThreads / kWave];
+  float *q = (float *)dynamic;  // [d rounded up to 512: zeros]
+  __shared__ double room64[2][kWaves];
+  __shared__ float room32[4][kWaves];
+  __shared__ __attribute__((aligned(16))) float tops[kTops];
+  __shared__ uint32_t n_list, n_rough, n_best;
+  __shared__ float kth;
   const uint32_t i = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const ScoreTable &g = a.g;
-  const uint32_t d8 = (g.d + 7) / 8 * 8;
+  const T *rows = (const T *)g.rows;
+  const uint32_t n_groups = GROUP ? group_count(g.n, GROUP) : 0;
+  const float *gm = a.group_max + (uint64_t)i * n_groups;
+  const uint32_t target = a.targets ? a.targets[i] : ANN_PAD_ID;
+  if (tid == 0) kth = -INFINITY, n_list = 0, n_rough = 0, n_best = 0;
   float qsq = 0.0f;
-  for (uint32_t c = tid; c < d8; c += kFinishThreads) {
+  for (uint32_t c = tid; c < (g.d + 511) / 512 * 512; c += THREADS) {
     const float v = c < g.d ? to_f32(((const T *)g.q)[(uint64_t)i * g.q_stride + c]) : 0.0f;
     q[c] = v;
     qsq = __builtin_fmaf(v, v, qsq);
   }
-  // statistics (fp64: the splits' sums are joined once)
-  float m = -INFINITY;
-  for (uint32_t s = tid; s < a.splits; s += kFinishThreads) {
+  float m = -INFINITY, x_norm = 0.0f, top = -INFINITY;
+  float4 first = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  if (tid < a.splits) first = a.stats[(uint64_t)tid * g.nq + i];
+  if (first.y != 0.0f) m = first.x;
+  for (uint32_t s = tid + THREADS; s < a.splits; s += THREADS) {
     const float4 v = a.stats[(uint64_t)s * g.nq + i];
     if (v.y != 0.0f) m = fmaxf(m, v.x);
   }
-  m = block_max(m, room32);
+  if constexpr (GROUP != 0) {
+    for (uint32_t c = tid; c < n_groups; c += THREADS * kInFlight) {
+      float v[kInFlight];
+#pragma unroll
+      for (uint32_t u = 0; u < kInFlight; ++u) v[u] = c + u * THREADS < n_groups ? gm[c + u * THREADS] : -INFINITY;
+#pragma unroll
+      for (uint32_t u = 0; u < kInFlight; ++u) top = fmaxf(top, v[u]);
+    }
+    for (uint32_t c = tid; c < a.norm_runs; c += THREADS) x_norm = fmaxf(x_norm, a.norms[c]);
+#pragma unroll
+    for (uint32_t far = 1; far < kSharers; far *= 2) top = fmaxf(top, __int_as_float(xor_lane_i32(__float_as_int(top), (int)far)));
+    if (tid % kSharers == 0) tops[tid / kSharers] = top;
+  }
+  {
+    const float wm = wave_max_f32(m), wx = wave_max_f32(x_norm), wt = wave_max_f32(top), wq = lanes_sum<64>(qsq);
+    if (lane == 0) room32[0][wave] = wm, room32[1][wave] = wx, room32[2][wave] = wt, room32[3][wave] = wq;
+  }
+  __syncthreads();
+  m = room32[0][0], x_norm = room32[1][0], qsq = room32[3][0];
+  float largest = room32[2][0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) {
+    m = fmaxf(m, room32[0][w]), x_norm = fmaxf(x_norm, room32[1][w]), largest = fmaxf(largest, room32[2][w]);
+    qsq += room32[3][w];
+  }
+  // statistics (fp64: the splits' sums are joined once)
   double l = 0.0, t = 0.0;
-  for (uint32_t s = tid; s < a.splits; s += kFinishThreads) {
-    const float4 v = a.stats[(uint64_t)s * g.nq + i];
+  const auto join_split = [&](const float4 &v) {
     if (v.y != 0.0f) {
       const double by = (double)v.x - (double)m, f = exp(by);
       l += f * (double)v.y;
       t += f != 0.0 ? f * ((double)v.z + by * (double)v.y) : 0.0;
     }
+  };
+  join_split(first);
+  for (uint32_t s = tid + THREADS; s < a.splits; s += THREADS) join_split(a.stats[(uint64_t)s * g.nq + i]);
+  l = group_sum_f64<64>(l);
+  t = group_sum_f64<64>(t);
+  if (lane == 0) room64[0][wave] = l, room64[1][wave] = t;
+  double target_dot = 0.0;
+  if (target < g.n && wave == kWaves - 1) target_dot = exact_dot<T>(rows + (uint64_t)target * g.row_stride, q, g.d);
+  if constexpr (GROUP != 0) {
+    // The k-th largest of the tops: at least k groups reach it.
+    const float own = tops[tid / kSharers];
+    int above = 0;
+    for (uint32_t c = tid % kSharers * (kTops / kSharers); c < (tid % kSharers + 1) * (kTops / kSharers); c += 4) {
+      const float4 o = *(const float4 *)(tops + c);
+      const float v[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+      for (uint32_t e = 0; e < 4; ++e) above += v[e] > own || (v[e] == own && c + e < tid / kSharers);
+    }
+    above = group_sum_i32<(int)kSharers>(above);
+    if (tid % kSharers == 0 && above == (int)a.k - 1) kth = own;
   }
-  l = block_sum(l, room, wave);
-  t = block_sum(t, room, wave);
+  __syncthreads();
+  l = room64[0][0], t = room64[1][0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) l += room64[0][w], t += room64[1][w];
   const bool none = l == 0.0;  // no row left
   const double log_l = none ? 0.0 : log(l), lse = none ? -INFINITY : (double)m + log_l;
-  double target_dot = 0.0;
-  const uint32_t target = a.targets ? a.targets[i] : ANN_PAD_ID;
-  const bool given = target < g.n;  // (an id that is no row's: none)
-  if (given && wave == 0) target_dot = group_sum_f64<64>(exact_dot<T, 64>((const T *)g.rows + (uint64_t)target * g.row_stride, q, g.d, lane));
-  if (tid == 0) {
-    a.lse[i] = (float)lse;
-    if (a.entropy) {
-      const double h = none ? 0.0 : log_l - t / l;
-      a.entropy[i] = h < 0.0 ? 0.0f : (float)h;
-    }
+  if (wave == kWaves - 1 && lane == 0) {
     double lp = 0.0;
-    if (given) {
+    if (target < g.n) {  // (an id that is no row's: none)
       const float bias = g.bias ? g.bias[target] : 0.0f;
       lp = none || bias == -INFINITY ? -INFINITY : (double)g.scale * target_dot + (double)bias - lse;
     }
+    a.lse[i] = (float)lse;
     a.logprob[i] = lp > 0.0 ? 0.0f : (float)lp;
+    const double h = none ? 0.0 : log_l - t / l;
+    if (a.entropy) a.entropy[i] = h < 0.0 ? 0.0f : (float)h;
   }
   if constexpr (GROUP != 0) {
-    __shared__ float tops[kFinishThreads];
-    __shared__ uint32_t list[kGroupRange], n_list, n_best;
+    __shared__ uint32_t list[kListed], rough[kWaves * GROUP];
     __shared__ double best[2][kBest];
     __shared__ uint32_t best_id[2][kBest];
-    __shared__ float kth;
-    const uint32_t n_groups = group_count(g.n, GROUP);
-    const float *gm = a.group_max + (uint64_t)i * n_groups;
-    float x_norm = 0.0f, top = -INFINITY;
-    for (uint32_t c = tid; c < a.norm_runs; c += kFinishThreads) x_norm = fmaxf(x_norm, a.norms[c]);
     const float lost = (float)g.d * 0x1p-126f;  // squares below the smallest normal number may have gone
-    x_norm = sqrtf(block_max(x_norm, room32) + lost);
-    const float q_norm = sqrtf((float)block_sum((double)qsq, room, wave) + lost);
-    for (uint32_t c = tid; c < n_groups; c += kFinishThreads) top = fmaxf(top, gm[c]);
-    // The k-th largest of the lanes' maxima: at least k groups reach it.
-    tops[tid] = top;
-    if (tid == 0) kth = -INFINITY, n_best = 0;
-    __syncthreads();
-    uint32_t above = 0;
-    for (uint32_t c = 0; c < kFinishThreads; ++c) above += tops[c] > top || (tops[c] == top && c < tid);
-    if (above == a.k - 1) kth = top;
-    __syncthreads();
-    const float error = score_room(g.d, sizeof(T) == 4, q_norm, x_norm, g.scale, block_max(top, room32));
-    const float least = error < INFINITY ? kth - 2.0f * error : -INFINITY;  // (NaN compares false)
-    double bound = (double)(kth - error < INFINITY && error < INFINITY ? kth - error : -INFINITY);  // the k-th score is at least this
+    const float error = score_room(g.d, sizeof(T) == 4, sqrtf(qsq + lost), sqrtf(x_norm + lost), g.scale, largest);
+    const bool bounded = error < INFINITY && kth > -INFINITY;  // (false with NaN)
+    const float least = bounded ? kth - 2.0f * error : -INFINITY;
+    double bound = bounded ? (double)kth - (double)error : -INFINITY;  // the k-th score is at least this
     uint32_t side = 0;
+    // Place of candidate c among the candidates.
+    const auto place = [&](uint32_t c, uint32_t count) {
+      const double s = best[side][c];
+      const uint32_t id = best_id[side][c];
+      uint32_t rank = 0;
+      for (uint32_t o = 0; o < count; ++o) rank += best[side][o] > s || (best[side][o] == s && best_id[side][o] < id);
+      return rank;
+    };
     const auto keep_best = [&]() {  // the k best of the candidates, in order; all lanes
       __syncthreads();
       const uint32_t count = n_best;
-      for (uint32_t c = tid; c < count; c += kFinishThreads) {
-        const double s = best[side][c];
-        const uint32_t id = best_id[side][c];
-        uint32_t rank = 0;
-        for (uint32_t o = 0; o < count; ++o) rank += best[side][o] > s || (best[side][o] == s && best_id[side][o] < id);
-        if (rank < a.k) best[side ^ 1][rank] = s, best_id[side ^ 1][rank] = id;
+      for (uint32_t c = tid; c < count; c += THREADS) {
+        const uint32_t rank = place(c, count);
+        if (rank < a.k) best[side ^ 1][rank] = best[side][c], best_id[side ^ 1][rank] = best_id[side][c];
       }
       __syncthreads();
       side ^= 1;
@@ -594,43 +800,109 @@ __global__ __launch_bounds__(kFinishThreads) void row_finish_kernel(FinishArgs a
       if (count >= a.k && best[side][a.k - 1] > bound) bound = best[side][a.k - 1];
       __syncthreads();
     };
-    constexpr int kLanes = 64 / GROUP;  // to a row
-    for (uint32_t begin = 0; begin < n_groups; begin += kGroupRange) {
-      __syncthreads();
-      if (tid == 0) n_list = 0;
-      __syncthreads();
-      for (uint32_t c = begin + tid; c < n_groups && c < begin + kGroupRange; c += kFinishThreads)
-        if (gm[c] >= least) list[atomicAdd(&n_list, 1u)] = c;  // (the order plays no part)
+    constexpr uint32_t LANES = 16;  // to a row (64: a fifth slower with 768 columns, like with 128 of them)
+    constexpr int kRows = THREADS == 256 || GROUP == 16 ? 4 : 8;  // of a lane in flight
+    // All groups at once, or, where more are in question than the list holds, as many as it holds at a time.
+    uint32_t begin = 0, end = n_groups;
+    while (begin < n_groups) {
+      for (uint32_t c = begin + tid; c < end; c += THREADS * kInFlight) {
+        float v[kInFlight];
+#pragma unroll
+        for (uint32_t u = 0; u < kInFlight; ++u) v[u] = c + u * THREADS < end ? gm[c + u * THREADS] : NAN;
+#pragma unroll
+        for (uint32_t u = 0; u < kInFlight; ++u)
+          if (v[u] >= least) {
+            const uint32_t at = atomicAdd(&n_list, 1u);  // (the order plays no part)
+            if (at < kListed) list[at] = c + u * THREADS;
+          }
+      }
       __syncthreads();
       const uint32_t count = n_list;
-      for (uint32_t c0 = 0; c0 < count; c0 += kFinishThreads / kWave) {
-        const uint32_t held = n_best;
-        __syncthreads();  // all lanes have read it: they agree whether to make room
-        if (held + kFinishThreads / kLanes > kBest) keep_best();
+      __syncthreads();
+      if (tid == 0) n_list = 0;
+      if (count > kListed) {  // (of all groups)
+        end = kListed;
+        __syncthreads();
+        continue;
+      }
+      for (uint32_t c0 = 0; c0 < count; c0 += kWaves) {
         const uint32_t c = c0 + wave;
         if (c < count) {
-          const uint32_t group = list[c], in = lane / kLanes;
-          const uint64_t row = GROUP == 64 ? (uint64_t)group * 64 + in : (uint64_t)(group / 2) * 32 + in / 4 * 8 + group % 2 * 4 + in % 4;
-          const float bias = row < g.n ? (g.bias ? g.bias[row] : 0.0f) : -INFINITY;
-          if (bias != -INFINITY) {
-            double s = exact_dot<T, kLanes>((const T *)g.rows + row * g.row_stride, q, g.d, lane % kLanes);
-            s = group_sum_f64<kLanes>(s);
-            s = (double)g.scale * s + (double)bias;
-            if (lane % kLanes == 0 && s >= bound) {
-              const uint32_t at = atomicAdd(&n_best, 1u);
-              best[side][at] = s, best_id[side][at] = (uint32_t)row;
+          const uint32_t group = list[c];
+          for (uint32_t in0 = 0; in0 < GROUP; in0 += kWave / LANES * kRows) {
+            float dot[kRows];
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) dot[r] = 0.0f;
+            for (uint32_t k0 = 0; k0 < g.d; k0 += LANES * 8) {
+              const uint32_t k = k0 + lane % LANES * 8;
+              Unit<T> u[kRows];
+              const T *x[kRows];
+#pragma unroll
+              for (int r = 0; r < kRows; ++r) {  // (rows behind the last: the last once more)
+                const uint64_t row = group_row<GROUP>(group, in0 + r * (kWave / LANES) + lane / LANES);
+                x[r] = rows + (row < g.n ? row : g.n - 1) * g.row_stride + k;
+              }
+              if (k0 + LANES * 8 <= g.d) {
+#pragma unroll
+                for (int r = 0; r < kRows; ++r) load_unit(u[r], x[r]);
+              } else {
+#pragma unroll
+                for (int r = 0; r < kRows; ++r) load_unit(u[r], x[r], (int64_t)g.d - k);
+              }
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const float v = q[k + e];
+#pragma unroll
+                for (int r = 0; r < kRows; ++r) dot[r] = __builtin_fmaf(to_f32(u[r].v[e]), v, dot[r]);
+              }
+            }
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+              const uint64_t row = group_row<GROUP>(group, in0 + r * (kWave / LANES) + lane / LANES);
+              const float bias = row < g.n ? (g.bias ? g.bias[row] : 0.0f) : -INFINITY;
+              const float s = __builtin_fmaf(lanes_sum<LANES>(dot[r]), g.scale, bias);
+              // (not bounded: whatever is not left out; a score that is NaN in fp64 as well is dropped there)
+              if (lane % LANES == 0 && bias != -INFINITY && (!bounded || (double)s >= bound - (double)error)) rough[atomicAdd(&n_rough, 1u)] = (uint32_t)row;
             }
           }
         }
         __syncthreads();
+        const uint32_t found = n_rough;
+        for (uint32_t f0 = 0; f0 < found; f0 += kWaves) {
+          if ((begin | c0 | f0) != 0) {  // (at first there is room)
+            const uint32_t held = n_best;
+            __syncthreads();  // all lanes have read it: they agree whether to make more
+            if (held + kWaves > kBest) keep_best();
+          }
+          if (f0 + wave < found) {
+            const uint32_t row = rough[f0 + wave];
+            const double s = (double)g.scale * exact_dot<T>(rows + row * g.row_stride, q, g.d) + (double)(g.bias ? g.bias[row] : 0.0f);
+            if (lane == 0 && s >= bound) {
+              const uint32_t at = atomicAdd(&n_best, 1u);
+              best[side][at] = s, best_id[side][at] = row;
+            }
+          }
+          __syncthreads();
+        }
+        if (tid == 0) n_rough = 0;
+        __syncthreads();
+      }
+      __syncthreads();  // (the list has been read; n_list is zero)
+      begin = end;
+      end = end + kListed < n_groups ? end + kListed : n_groups;
+    }
+    const uint32_t count = n_best;
+    for (uint32_t c = tid; c < count; c += THREADS) {
+      const uint32_t rank = place(c, count);
+      if (rank < a.k) {
+        const double lp = best[side][c] - lse;
+        a.alt_ids[(uint64_t)i * a.k + rank] = best_id[side][c];
+        a.alt_logprobs[(uint64_t)i * a.k + rank] = lp > 0.0 ? 0.0f : (float)lp;
       }
     }
-    keep_best();
-    for (uint32_t c = tid; c < a.k; c += kFinishThreads) {
-      const bool is = c < n_best;
-      const double lp = is ? best[side][c] - lse : -INFINITY;
-      a.alt_ids[(uint64_t)i * a.k + c] = is ? best_id[side][c] : ANN_PAD_ID;
-      a.alt_logprobs[(uint64_t)i * a.k + c] = lp > 0.0 ? 0.0f : (float)lp;
+    for (uint32_t c = count + tid; c < a.k; c += THREADS) {
+      a.alt_ids[(uint64_t)i * a.k + c] = ANN_PAD_ID;
+      a.alt_logprobs[(uint64_t)i * a.k + c] = -INFINITY;
     }
   }
 }
@@ -640,6 +912,7 @@ struct ForwardPlan {
   uint32_t q_tiles = 0, splits = 0, norm_runs = 0;
   int group = 0;
   int blocks = 0;  // of 16 queries, if the rows are streamed
+  int slices = 0;  // of 16 columns, if the queries stay in registers
   uint64_t stats_at = 0, groups_at = 0, norms_at = 0;
   Parts parts;
 };
@@ -660,8 +933,11 @@ static ForwardPlan forward_plan(uint32_t nq, uint64_t n, uint32_t d, uint32_t ty
     const uint64_t most = (n + kStreamRows - 1) / kStreamRows;
     p.splits = most < kStreamGroups ? (uint32_t)most : kStreamGroups;
   } else {
-    p.q_tiles = (nq + kTile - 1) / kTile;
-    const uint32_t row_tiles = (uint32_t)((n + kTile - 1) / kTile);
+    const bool rows_short = type != ANN_F32 && d <= 128;
+    if (rows_short) p.slices = d <= 32 ? 2 : d <= 64 ? 4 : d <= 96 ? 6 : 8;
+    const uint32_t queries = rows_short ? kShortQueries : kTile, rows = rows_short ? kShortRows : kTile;
+    p.q_tiles = (nq + queries - 1) / queries;
+    const uint32_t row_tiles = (uint32_t)((n + rows - 1) / rows);
     uint32_t want = (kSplitTarget + p.q_tiles - 1) / p.q_tiles;
     want = (want + 7) / 8 * 8;
     p.splits = want < row_tiles ? want : row_tiles;
@@ -689,7 +965,22 @@ static ann_status forward(const ann_row_scores &s, uint32_t k, const ForwardPlan
       constexpr bool BIAS = decltype(with_bias)::value;
       constexpr int GROUP = decltype(group)::value;
       if (!p.blocks) {
-        row_scores_kernel<T, BIAS, GROUP><<<p.q_tiles * ((p.splits + 7) / 8 * 8), 256, 0, st>>>(g, p.q_tiles, p.splits, stats, groups);
+        // (rows too far apart for the offsets of the kernel for short ones: the other one, with as many splits)
+        const bool is_short = p.slices && g.row_stride <= kShortStride;
+        const uint32_t q_tiles = is_short ? p.q_tiles : (g.nq + kTile - 1) / kTile, grid = q_tiles * ((p.splits + 7) / 8 * 8);
+        const auto rows_short = [&](auto slices) {
+          if constexpr (sizeof(T) == 2) row_scores_short_kernel<T, decltype(slices)::value, BIAS, GROUP><<<grid, 256, 0, st>>>(g, q_tiles, p.splits, stats, groups);
+        };
+        if (!is_short)
+          row_scores_kernel<T, BIAS, GROUP><<<grid, 256, 0, st>>>(g, q_tiles, p.splits, stats, groups);
+        else if (p.slices == 2)
+          rows_short(std::integral_constant<int, 2>());
+        else if (p.slices == 4)
+          rows_short(std::integral_constant<int, 4>());
+        else if (p.slices == 6)
+          rows_short(std::integral_constant<int, 6>());
+        else
+          rows_short(std::integral_constant<int, 8>());
         if (GROUP) row_norms_kernel<T><<<p.norm_runs, 256, 0, st>>>(g, norms);
         return;
       }
@@ -722,13 +1013,21 @@ static ann_status forward(const ann_row_scores &s, uint32_t k, const ForwardPlan
     ANN_HIP(hipGetLastError());
     f.stats = stats, f.group_max = groups, f.norms = norms, f.splits = p.splits, f.norm_runs = p.norm_runs;
   }
-  const uint32_t lds = (g.d + 7) / 8 * 8 * sizeof(float);
+  const uint32_t lds = (g.d + 511) / 512 * 512 * sizeof(float);
+  const auto end = [&](auto group) {
+    constexpr int GROUP = decltype(group)::value;
+    // (few queries: what one of them takes counts, and 16 wavefronts read its groups at once)
+    if (s.nq < kFewQueries)
+      row_finish_kernel<T, GROUP, 1024><<<s.nq, 1024, lds, st>>>(f);
+    else
+      row_finish_kernel<T, GROUP, 256><<<s.nq, 256, lds, st>>>(f);
+  };
   if (k == 0)
-    row_finish_kernel<T, 0><<<s.nq, kFinishThreads, lds, st>>>(f);
+    end(std::integral_constant<int, 0>());
   else if (p.group == 16)
-    row_finish_kernel<T, 16><<<s.nq, kFinishThreads, lds, st>>>(f);
+    end(std::integral_constant<int, 16>());
   else
-    row_finish_kernel<T, 64><<<s.nq, kFinishThreads, lds, st>>>(f);
+    end(std::integral_constant<int, 64>());
   ANN_HIP(hipGetLastError());
   return ANN_OK;
 }

@@ -65,11 +65,15 @@ struct Unit {
   T v[8];
 };
 template <typename T>
+__device__ __forceinline__ void load_unit(Unit<T> &u, const T *p) {
+  typedef Piece<T, 16 / sizeof(T), sizeof(T)> P;
+  *(P *)u.v = *(const P *)p;
+  if constexpr (sizeof(T) == 4) *(P *)(u.v + 4) = *(const P *)(p + 4);
+}
+template <typename T>
 __device__ __forceinline__ void load_unit(Unit<T> &u, const T *p, int64_t there) {
   if (there >= 8) {
-    typedef Piece<T, 16 / sizeof(T), sizeof(T)> P;
-    *(P *)u.v = *(const P *)p;
-    if constexpr (sizeof(T) == 4) *(P *)(u.v + 4) = *(const P *)(p + 4);
+    load_unit(u, p);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) u.v[e] = e < there ? p[e] : (T)0.0f;
@@ -196,11 +200,12 @@ __device__ __forceinline__ void tile_product(f32x16 (&acc)[2][2], const Lines<T>
   }
 }
 
-__device__ __forceinline__ void clear(f32x16 (&acc)[2][2]) {
+template <int M, int N>
+__device__ __forceinline__ void clear(f32x16 (&acc)[M][N]) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < M; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < N; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
 }
