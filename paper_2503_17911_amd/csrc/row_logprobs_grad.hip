@@ -26,6 +26,10 @@ namespace ann {
 constexpr uint64_t kChunkBytes = 512ull << 20;  // of G at a time
 constexpr uint32_t kGradTarget = 768;           // workgroups of a product: three to a compute unit
 
+// Wavefronts to a SIMD of the gradients' products (three instead of two: 303 -> 237 and 282 -> 255 us with 2,048 x 50,000 x 768).
+template <typename T>
+constexpr int kGradWaves = sizeof(T) == 2 ? 3 : 2;
+
 struct GradArgs {
   ScoreTable g;
   const uint32_t *targets;
@@ -137,11 +141,13 @@ __global__ __launch_bounds__(256) void grad_scores_kernel(GradArgs a, uint32_t r
 
 // part[split][q][c] (+)= sum over the split's rows of the chunk of G[q][j] x[j][c]  (rows left out may hold anything: read as zeros)
 template <typename T>
-__global__ __launch_bounds__(256) void grad_queries_kernel(ScoreTable g, uint32_t row0, uint32_t rows, uint32_t ld, const T *__restrict__ G, uint32_t splits,
+__global__ __launch_bounds__(256, kGradWaves<T>) void grad_queries_kernel(ScoreTable g, uint32_t row0, uint32_t rows, uint32_t ld, const T *__restrict__ G, uint32_t splits,
                                                            float *__restrict__ part, bool add) {
   __shared__ __attribute__((aligned(16))) char lds[kTileBytes<T, kAlong, kAcross>];
   const uint32_t c_tiles = (g.d + kTile - 1) / kTile, q_tiles = (g.nq + kTile - 1) / kTile;
-  const uint32_t ct = blockIdx.x % c_tiles, qt = blockIdx.x / c_tiles % q_tiles, split = blockIdx.x / c_tiles / q_tiles;
+  // a die takes a run of rows through all columns and queries
+  const uint32_t b8 = blockIdx.x / 8, ct = b8 % c_tiles, qt = b8 / c_tiles % q_tiles, split = b8 / c_tiles / q_tiles * 8 + blockIdx.x % 8;
+  if (split >= splits) return;
   const uint32_t slices = (rows + Operand16<T>::kSlice - 1) / Operand16<T>::kSlice;
   const uint32_t begin = (uint32_t)((uint64_t)slices * split / splits) * Operand16<T>::kSlice;
   uint32_t end = (uint32_t)((uint64_t)slices * (split + 1) / splits) * Operand16<T>::kSlice;
@@ -167,29 +173,41 @@ __global__ __launch_bounds__(256) void grad_queries_kernel(ScoreTable g, uint32_
     }
 }
 
-// dq[q][c] = scale sum over the splits, in their order, and what was left of the given row's element
-template <typename T>
+// dq[q][c] = scale sum over the splits, in their order, and what was left of the given row's element.  A workgroup takes 256 / LANES
+// queries; eight splits' parts are on their way at a time.
+template <typename T, int LANES>
 __global__ __launch_bounds__(256) void grad_queries_sum_kernel(GradArgs a, const float *__restrict__ part, uint32_t splits, T *__restrict__ dq, uint64_t stride) {
   const ScoreTable &g = a.g;
-  const uint64_t at = blockIdx.x * 256ull + threadIdx.x, all = (uint64_t)g.nq * g.d;
-  if (at >= all) return;
-  float sum = 0.0f;
-  for (uint32_t s = 0; s < splits; ++s) sum += part[s * all + at];
-  const uint64_t q = at / g.d, c = at % g.d;
-  if (sizeof(T) == 2 && a.targets) {
-    const uint32_t target = a.targets[q];
-    if (target < g.n && !(g.bias && g.bias[target] == -INFINITY))
-      sum = __builtin_fmaf(a.rest[q], to_f32(((const T *)g.rows)[target * g.row_stride + c]), sum);
+  const uint64_t q = (uint64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES, all = (uint64_t)g.nq * g.d;
+  if (q >= g.nq) return;
+  const float by = a.scaling ? g.scale * a.scaling[1] : g.scale;
+  const uint32_t target = sizeof(T) == 2 && a.targets ? a.targets[q] : ANN_PAD_ID;
+  const bool given = target < g.n && !(g.bias && g.bias[target] == -INFINITY);
+  const float rest = given ? a.rest[q] : 0.0f;
+  for (uint32_t c = threadIdx.x % LANES; c < g.d; c += LANES) {
+    const float *p = part + q * g.d + c;
+    float sum = 0.0f;
+    uint32_t s = 0;
+    for (; s + 8 <= splits; s += 8) {
+      float v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = p[(s + u) * all];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) sum += v[u];
+    }
+    for (; s < splits; ++s) sum += p[s * all];
+    if (given) sum = __builtin_fmaf(rest, to_f32(((const T *)g.rows)[target * g.row_stride + c]), sum);
+    dq[q * stride + c] = from_f32<T>(sum * by);
   }
-  dq[q * stride + c] = from_f32<T>(sum * (a.scaling ? g.scale * a.scaling[1] : g.scale));
 }
 
 // drows[row0 + j][c] = scale sum over the queries of G[q][j] q[q][c]
 template <typename T>
-__global__ __launch_bounds__(256) void grad_rows_kernel(ScoreTable g, uint32_t row0, uint32_t rows, uint32_t ld, const T *__restrict__ G, T *__restrict__ out,
+__global__ __launch_bounds__(256, kGradWaves<T>) void grad_rows_kernel(ScoreTable g, uint32_t row0, uint32_t rows, uint32_t ld, const T *__restrict__ G, T *__restrict__ out,
                                                         uint64_t stride, const float *__restrict__ scaling) {
   __shared__ __attribute__((aligned(16))) char lds[kTileBytes<T, kAcross, kAcross>];
-  const uint32_t c_tiles = (g.d + kTile - 1) / kTile, ct = blockIdx.x % c_tiles, rt = blockIdx.x / c_tiles;
+  const uint32_t c_tiles = (g.d + kTile - 1) / kTile, ct = blockIdx.x / 8 % c_tiles, rt = blockIdx.x / 8 / c_tiles * 8 + blockIdx.x % 8;
+  if (rt >= ld / kTile) return;
   const Lines<T> A = {G, ld, ld, g.nq}, B = {(const T *)g.q, g.q_stride, g.d, g.nq};
   f32x16 acc[2][2];
   clear(acc);
@@ -222,9 +240,236 @@ __global__ __launch_bounds__(256) void grad_bias_kernel(const float *__restrict_
   out[row0 + j] = sum;
 }
 
+// Short rows of 16 bits (KS slices of 16 columns): scores, G and its product in one kernel, G never leaving the registers.  A
+// wavefront owns 32 lines of one side (OWN_ROWS: rows, otherwise queries), which stay in registers, and their gradient, 32 x 16 KS
+// in accumulators; tiles of 64 lines of the other side pass by in LDS.  The scores' product puts the owned lines along
+// the lanes and four by four of the passing ones into each lane's registers, and that is what the second product
+// asks of its first operand if it takes the passing lines in that order (a sum has none); its second operand is the tile once more,
+// transposed by the LDS.  Each side costs the scores anew: four products where storing G costs three, but G need not be
+// written and read (twice two bytes for 256 operations).
+// One side of 4,096 x 100,000 x 128 (both: SHORT_BOTH).
+constexpr int kPassing = 64, kOwned = 128;
+constexpr uint32_t kShortTarget = 512;       // workgroups that own queries: two to a compute unit
+constexpr uint64_t kShortStride = 1u << 24;  // row stride up to which offsets within a tile take 32 bits
+
+template <typename T, int KS, bool OWN_ROWS, bool BIAS, bool ENTROPY>
+__global__ __launch_bounds__(256, 2) void grad_short_kernel(GradArgs a, uint32_t splits, float *__restrict__ part, T *__restrict__ drows, uint64_t stride,
+                                                            float *__restrict__ drow_bias) {
+  typedef typename Operand16<T>::E E;
+  constexpr int kSlots = 2 * KS, kLine = KS * 32 + 32, kUnits = kPassing * kSlots / 256;
+  // (lines 32 bytes apart from a power of two: eight lines side by side hit all banks, and so do the four of a transposed read)
+  __shared__ __attribute__((aligned(16))) char lds[2][kPassing * kLine];
+  struct Line {  // of a passing line, in arrays so that four of them are one read
+    float a[kPassing], b[kPassing], c[kPassing], d[kPassing];
+    uint32_t target[kPassing];
+  };
+  __shared__ __attribute__((aligned(16))) Line info[2];
+  const ScoreTable &g = a.g;
+  const uint32_t owned = OWN_ROWS ? g.n : g.nq, passing = OWN_ROWS ? g.nq : g.n;
+  const uint64_t own_stride = OWN_ROWS ? g.row_stride : g.q_stride, pass_stride = OWN_ROWS ? g.q_stride : g.row_stride;
+  const T *own = (const T *)(OWN_ROWS ? g.rows : g.q), *pass = (const T *)(OWN_ROWS ? g.q : g.rows);
+  const uint32_t own_tiles = (owned + kOwned - 1) / kOwned;
+  // a die takes a run of rows through all queries
+  const uint32_t b8 = blockIdx.x / 8, ot = OWN_ROWS ? blockIdx.x : b8 % own_tiles, split = OWN_ROWS ? 0 : b8 / own_tiles * 8 + blockIdx.x % 8;
+  if (split >= splits) return;
+  const uint32_t tiles = (passing + kPassing - 1) / kPassing;
+  const uint32_t first = (uint32_t)((uint64_t)tiles * split / splits), last = (uint32_t)((uint64_t)tiles * (split + 1) / splits);
+  const int wave = (int)threadIdx.x / kWave, lane = lane_id();
+  const uint32_t own0 = ot * kOwned + wave * 32, mine = own0 + lane % 32;
+  const float c = g.scale * kLog2e, scaling = a.scaling ? a.scaling[0] : 1.0f;
+  E line[KS];
+#pragma unroll
+  for (int kk = 0; kk < KS; ++kk) {
+    const uint32_t k = kk * 16 + lane / 32 * 8;
+    Unit<T> u;
+    load_unit(u, own + mine * own_stride + k, mine < owned ? (int64_t)g.d - k : 0);
+    line[kk] = __builtin_bit_cast(E, u);
+  }
+  // Of a query: -lse, times log2 e without biases (-infinity: no row left, no probability); -g and -h, times the scaling; the entropy.
+  const auto query = [&](uint32_t q, float &lse2, float &gl, float &gh, float &h, uint32_t &target) {
+    const bool is = q < g.nq;
+    target = is && a.targets ? a.targets[q] : ANN_PAD_ID;
+    const float lse = is ? a.lse[q] : -INFINITY;
+    lse2 = lse == -INFINITY ? -INFINITY : BIAS ? -lse : -lse * kLog2e;
+    const bool none = lse == -INFINITY;
+    gl = none || !a.g_logprob || target >= g.n ? 0.0f : -scaling * a.g_logprob[q];
+    gh = ENTROPY && !none ? -scaling * a.g_entropy[q] : 0.0f;
+    h = ENTROPY && !none ? a.entropy[q] : 0.0f;
+  };
+  float own_lse2 = 0.0f, own_gl = 0.0f, own_gh = 0.0f, own_h = 0.0f, own_bias = 0.0f;
+  uint32_t own_target = ANN_PAD_ID;
+  if constexpr (OWN_ROWS) {
+    own_bias = mine < g.n ? (BIAS ? g.bias[mine] : 0.0f) : -INFINITY;
+  } else {
+    query(mine, own_lse2, own_gl, own_gh, own_h, own_target);
+  }
+  Unit<T> u[kUnits];
+  float unit_bias[kUnits];
+  uint32_t from[kUnits], to[kUnits];
+#pragma unroll
+  for (int i = 0; i < kUnits; ++i) {
+    const uint32_t at = threadIdx.x + 256 * i, l = at / kSlots, slot = at % kSlots;
+    from[i] = (l * (uint32_t)pass_stride + slot * 8) * sizeof(T);
+    to[i] = l * kLine + slot * 16;
+    unit_bias[i] = 0.0f;
+  }
+  const auto fetch = [&](uint32_t tile) {
+    const T *base = pass + (uint64_t)tile * kPassing * pass_stride;
+    if (KS * 16 == g.d && (tile + 1) * kPassing <= passing && pass_stride <= kShortStride) {
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) load_unit(u[i], (const T *)((const char *)base + from[i]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) {
+        const uint32_t at = threadIdx.x + 256 * i, l = at / kSlots, k = at % kSlots * 8;
+        load_unit(u[i], base + l * pass_stride + k, tile * kPassing + l < passing ? (int64_t)g.d - k : 0);
+      }
+    }
+    if (BIAS && !OWN_ROWS) {
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) {
+        const uint32_t l = tile * kPassing + (threadIdx.x + 256 * i) / kSlots;
+        unit_bias[i] = l < passing ? g.bias[l] : -INFINITY;
+      }
+    }
+  };
+  f32x16 acc[KS / 2];
+#pragma unroll
+  for (int b = 0; b < KS / 2; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[b][r] = 0.0f;
+  float sum = 0.0f;  // of the owned row's elements of G
+  if (first < last) fetch(first);
+  for (uint32_t tile = first; tile < last; ++tile) {
+    char *at = lds[tile & 1];
+    Line &of = info[tile & 1];
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+      uint4 v = unit_part(u[i], 0);
+      if (BIAS && !OWN_ROWS && unit_bias[i] == -INFINITY) v = make_uint4(0, 0, 0, 0);  // (rows left out may hold anything)
+      *(uint4 *)(at + to[i]) = v;
+    }
+    const bool whole = tile * kPassing + kPassing <= passing;
+    if (threadIdx.x < kPassing) {
+      const uint32_t l = tile * kPassing + threadIdx.x;
+      if constexpr (OWN_ROWS)
+        query(l, of.a[threadIdx.x], of.b[threadIdx.x], of.c[threadIdx.x], of.d[threadIdx.x], of.target[threadIdx.x]);
+      else if (BIAS || !whole)
+        of.a[threadIdx.x] = l < passing ? (BIAS ? g.bias[l] : 0.0f) : -INFINITY;
+    }
+    __syncthreads();  // (one per tile: whoever writes this half again has met the others at the next tile's)
+    if (tile + 1 < last) fetch(tile + 1);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      f32x16 s;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = 0.0f;
+      const char *x = at + (half * 32 + lane % 32) * kLine + lane / 32 * 16;
+#pragma unroll
+      for (int kk = 0; kk < KS; ++kk) s = matrix_step(*(const E *)(x + kk * 32), line[kk], s);
+      // G, times the scaling
+      const uint32_t line0 = tile * kPassing + half * 32;
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const int l = half * 32 + block_row(r);
+        float lse2[4], gl[4], gh[4], h[4], bias[4];
+        if constexpr (OWN_ROWS) {
+          *(float4 *)lse2 = *(const float4 *)(of.a + l), *(float4 *)gl = *(const float4 *)(of.b + l);
+          if (ENTROPY) *(float4 *)gh = *(const float4 *)(of.c + l), *(float4 *)h = *(const float4 *)(of.d + l);
+        } else if (BIAS || !whole) {
+          *(float4 *)bias = *(const float4 *)(of.a + l);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float b = OWN_ROWS ? own_bias : BIAS || !whole ? bias[e] : 0.0f;
+          // log2 p (biases may be as low as they get: in natural units nothing overflows)
+          float y = OWN_ROWS ? lse2[e] : own_lse2;
+          y = BIAS ? (__builtin_fmaf(s[r + e], g.scale, b) + y) * kLog2e : __builtin_fmaf(s[r + e], c, y);
+          const float p = __builtin_amdgcn_exp2f(y);
+          float slope = OWN_ROWS ? gl[e] : own_gl;
+          if (ENTROPY) slope = __builtin_fmaf(OWN_ROWS ? gh[e] : own_gh, __builtin_fmaf(y, kLn2, OWN_ROWS ? h[e] : own_h), slope);
+          float v = p * slope;
+          // (no probability: 0, also where log p is -infinity and the slope with it; rows left out likewise, whatever they hold)
+          if (ENTROPY && !(p != 0.0f)) v = 0.0f;
+          if ((BIAS || (!OWN_ROWS && !whole)) && b == -INFINITY) v = 0.0f;
+          s[r + e] = v;
+        }
+      }
+      // the given rows' elements: few blocks have one
+      const uint32_t target = OWN_ROWS ? of.target[half * 32 + lane % 32] : own_target;
+      const uint32_t hit = target - (OWN_ROWS ? own0 : line0);
+      const bool hits = __any(hit < 32 && target < g.n);
+      if (hits) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int l = block_row(r);
+          if constexpr (OWN_ROWS) {
+            if (of.target[half * 32 + l] == mine && mine < g.n && own_bias != -INFINITY) s[r] -= of.b[half * 32 + l];
+          } else {
+            if (hit == (uint32_t)l && target < g.n && !(BIAS && of.a[half * 32 + l] == -INFINITY)) s[r] -= own_gl;
+          }
+        }
+      }
+      if (OWN_ROWS && drow_bias) {
+        float some = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) some += s[r];
+        sum += some;
+      }
+      E G[2];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) G[r / 8][r % 8] = from_f32<T>(s[r]);
+      if (!OWN_ROWS && hits) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (hit == (uint32_t)block_row(r) && target < g.n) a.rest[mine] = s[r] - to_f32((T)G[r / 8][r % 8]);
+      }
+      // lines 16 t + 4 (lane / 32) + 0 .. 3 and 8 further are the lane's eight k of step t
+#pragma unroll
+      for (int b = 0; b < KS / 2; ++b)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          union {
+            s16x4 part[2];
+            E e;
+          } f;
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            const int l = half * 32 + t * 16 + p * 8 + lane / 32 * 4 + lane % 16 / 4, column = b * 32 + lane / 16 % 2 * 16 + lane % 4 * 4;
+            f.part[p] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at + l * kLine + column * 2));
+          }
+          acc[b] = matrix_step(G[t], f.e, acc[b]);
+        }
+    }
+  }
+  if (OWN_ROWS && drow_bias) {
+    const LanePair p = lane_pair<false>(__float_as_uint(sum));
+    sum = __uint_as_float(p.low) + __uint_as_float(p.high);
+    if (lane < 32 && mine < g.n) drow_bias[mine] = sum / scaling;
+  }
+  if (OWN_ROWS && !drows) return;
+  const float by = a.scaling ? g.scale * a.scaling[1] : g.scale;
+#pragma unroll
+  for (int b = 0; b < KS / 2; ++b) {
+    const uint32_t column = b * 32 + lane % 32;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const uint32_t l = own0 + block_row(r);
+      if (l >= owned || column >= g.d) continue;
+      if constexpr (OWN_ROWS) {
+        const bool left_out = BIAS && g.bias[l] == -INFINITY;  // (zero, whatever the queries hold)
+        drows[l * stride + column] = from_f32<T>(left_out ? 0.0f : acc[b][r] * by);
+      } else {
+        part[((uint64_t)split * g.nq + l) * g.d + column] = acc[b][r];
+      }
+    }
+  }
+}
+
 // ---------------------------------------------------------------------------
 struct BackwardPlan {
   uint32_t q_tiles = 0, chunk = 0, splits = 0;  // chunk: rows at a time, a multiple of kTile
+  int slices = 0;                               // of 16 columns, if G stays in registers
   uint64_t g_at = 0, part_at = 0, sums_at = 0, scaling_at = 0, rest_at = 0;
   Parts parts;
 };
@@ -233,6 +478,15 @@ static BackwardPlan backward_plan(uint32_t nq, uint64_t n, uint32_t d, uint32_t 
   BackwardPlan p;
   if (nq == 0 || n == 0) return p;
   p.q_tiles = (nq + kTile - 1) / kTile;
+  if (type != ANN_F32 && d <= 128) {
+    p.slices = d <= 64 ? 4 : d <= 96 ? 6 : 8;
+    const uint32_t tiles = (uint32_t)((n + kPassing - 1) / kPassing), want = ((kShortTarget + p.q_tiles - 1) / p.q_tiles + 7) / 8 * 8;
+    p.splits = want < tiles ? want : tiles;
+    p.part_at = p.parts.take((uint64_t)p.splits * nq * d * sizeof(float));
+    p.scaling_at = p.parts.take(2 * sizeof(float));
+    p.rest_at = p.parts.take(nq * sizeof(float));
+    return p;
+  }
   const uint64_t row_bytes = (uint64_t)nq * type_bytes(type), all = (n + kTile - 1) / kTile * kTile;
   uint64_t chunk = kChunkBytes / row_bytes / kTile * kTile;
   if (chunk < kTile) chunk = kTile;
@@ -241,7 +495,7 @@ static BackwardPlan backward_plan(uint32_t nq, uint64_t n, uint32_t d, uint32_t 
   const uint64_t chunks = (all + chunk - 1) / chunk;
   p.chunk = (uint32_t)((all / kTile + chunks - 1) / chunks * kTile);
   const uint32_t tiles = p.q_tiles * ((d + kTile - 1) / kTile), most = (p.chunk + 511) / 512;
-  p.splits = (kGradTarget + tiles - 1) / tiles;
+  p.splits = ((kGradTarget + tiles - 1) / tiles + 7) / 8 * 8;
   if (p.splits > most) p.splits = most;
   p.g_at = p.parts.take(p.chunk * row_bytes);
   p.part_at = p.parts.take((uint64_t)p.splits * nq * d * sizeof(float));
@@ -271,6 +525,42 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
     ANN_HIP(hipGetLastError());
     a.scaling = scaling;
   }
+  if (p.slices) {
+    const auto run = [&](auto slices, auto bias, auto entropy) {
+      if constexpr (sizeof(T) == 2) {
+        constexpr int KS = decltype(slices)::value;
+        constexpr bool BIAS = decltype(bias)::value, ENTROPY = decltype(entropy)::value;
+        if (o.dq)
+          grad_short_kernel<T, KS, false, BIAS, ENTROPY><<<p.q_tiles * ((p.splits + 7) / 8 * 8), 256, 0, st>>>(a, p.splits, part, nullptr, 0, nullptr);
+        if (o.drows || o.drow_bias)
+          grad_short_kernel<T, KS, true, BIAS, ENTROPY><<<(g.n + kOwned - 1) / kOwned, 256, 0, st>>>(a, 1, nullptr, (T *)o.drows, o.drows_stride, o.drow_bias);
+      }
+    };
+    const auto run_entropy = [&](auto slices, auto bias) {
+      if (a.g_entropy)
+        run(slices, bias, std::true_type());
+      else
+        run(slices, bias, std::false_type());
+    };
+    const auto run_bias = [&](auto slices) {
+      if (g.bias)
+        run_entropy(slices, std::true_type());
+      else
+        run_entropy(slices, std::false_type());
+    };
+    if (p.slices == 4)
+      run_bias(std::integral_constant<int, 4>());
+    else if (p.slices == 6)
+      run_bias(std::integral_constant<int, 6>());
+    else
+      run_bias(std::integral_constant<int, 8>());
+    ANN_HIP(hipGetLastError());
+    if (o.dq) {
+      grad_queries_sum_kernel<T, 128><<<(g.nq + 1) / 2, 256, 0, st>>>(a, part, p.splits, (T *)o.dq, o.dq_stride);
+      ANN_HIP(hipGetLastError());
+    }
+    return ANN_OK;
+  }
   // (no queries: one chunk of all rows, of which no product takes anything)
   const uint32_t chunk = p.chunk ? p.chunk : (g.n + kTile - 1) / kTile * kTile;
   for (uint32_t row0 = 0; row0 < g.n; row0 += chunk) {
@@ -298,12 +588,12 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
         run_entropy(std::false_type());
       ANN_HIP(hipGetLastError());
       if (o.dq) {
-        grad_queries_kernel<T><<<c_tiles * p.q_tiles * p.splits, 256, 0, st>>>(g, row0, rows, ld, G, p.splits, part, row0 != 0);
+        grad_queries_kernel<T><<<c_tiles * p.q_tiles * ((p.splits + 7) / 8 * 8), 256, 0, st>>>(g, row0, rows, ld, G, p.splits, part, row0 != 0);
         ANN_HIP(hipGetLastError());
       }
     }
     if (o.drows) {
-      grad_rows_kernel<T><<<c_tiles * (ld / kTile), 256, 0, st>>>(g, row0, rows, ld, G, (T *)o.drows, o.drows_stride, a.scaling);
+      grad_rows_kernel<T><<<c_tiles * ((ld / kTile + 7) / 8 * 8), 256, 0, st>>>(g, row0, rows, ld, G, (T *)o.drows, o.drows_stride, a.scaling);
       ANN_HIP(hipGetLastError());
     }
     if (o.drow_bias) {
@@ -312,8 +602,7 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
     }
   }
   if (o.dq && g.nq) {
-    const uint64_t all = (uint64_t)g.nq * g.d;
-    grad_queries_sum_kernel<T><<<(uint32_t)((all + 255) / 256), 256, 0, st>>>(a, part, g.n ? p.splits : 0, (T *)o.dq, o.dq_stride);
+    grad_queries_sum_kernel<T, 256><<<g.nq, 256, 0, st>>>(a, part, g.n ? p.splits : 0, (T *)o.dq, o.dq_stride);
     ANN_HIP(hipGetLastError());
   }
   return ANN_OK;

@@ -112,7 +112,37 @@ struct TileSide {
     else
       return line * 64 + ((slot ^ ((line >> 1) & 3)) << 4);
   }
+  // Where the lane's units lie from the tile's first element, in bytes.  Lines that do not exist are read as one that does: what
+  // comes of them is not used.  (Offsets computed anew for every slice, with a test for each unit, took more
+  // instructions than the product.)
+  uint32_t from[kUnits];
+  const char *base;
+  bool direct;  // 32-bit offsets hold, and no unit ends behind the last line
+  __device__ __forceinline__ void start(const Lines<T> &m, uint32_t line0) {
+    const uint32_t last = m.lines - 1 - line0;  // (the tile has a line)
+    base = (const char *)(m.p + (ORDER == kAlong ? line0 * m.stride : line0));
+    direct = m.stride < (1u << 23) && (ORDER == kAlong || line0 + kTile <= m.lines || m.lines % 8 == 0);
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+      const uint32_t at = threadIdx.x + 256 * i;
+      if constexpr (ORDER == kAlong) {
+        uint32_t line = at / (O::kSlice / 8);
+        line = line < last ? line : last;
+        from[i] = (line * (uint32_t)m.stride + at % (O::kSlice / 8) * 8) * sizeof(T);
+      } else {
+        uint32_t line = at % (kTile / 8) * 8;
+        line = line < last ? line : last / 8 * 8;
+        from[i] = (at / (kTile / 8) * (uint32_t)m.stride + line) * sizeof(T);
+      }
+    }
+  }
   __device__ __forceinline__ void fetch(const Lines<T> &m, uint32_t line0, uint32_t k0) {
+    if (direct && k0 + O::kSlice <= m.depth && !(ORDER == kAcross && m.bias)) {
+      const char *p = base + (ORDER == kAlong ? (uint64_t)k0 : k0 * m.stride) * sizeof(T);
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) load_unit(u[i], (const T *)(p + from[i]));
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
       const uint32_t at = threadIdx.x + 256 * i;
@@ -174,6 +204,7 @@ __device__ __forceinline__ void tile_product(f32x16 (&acc)[2][2], const Lines<T>
   SA a;
   SB b;
   const int mw = (int)(threadIdx.x / kWave) / 2 * 2, nw = (int)(threadIdx.x / kWave) % 2 * 2;
+  a.start(A, m0), b.start(B, n0);
   if (k_begin < k_end) a.fetch(A, m0, k_begin), b.fetch(B, n0, k_begin);
   for (uint32_t k = k_begin; k < k_end; k += O::kSlice) {
     __syncthreads();  // the slice before has been read

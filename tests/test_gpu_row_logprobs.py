@@ -183,6 +183,26 @@ def test_masks_of_the_lowest_value_are_ordinary_biases():
     assert ((got["entropy"] - math.log(400)).abs() < 1e-5).all() and torch.isfinite(got["lse"]).all()
 
 
+def test_gradient_of_masks_of_the_lowest_value():
+    import paper_2503_17911_amd as ann
+    for dtype in ("f32", "f16", "bf16"):
+        for d in (40, 200):
+            q, rows, _, target = inputs(10, 400, d, dtype, 2)
+            b = torch.full((400,), torch.finfo(torch.float32).min)
+            f = forward(ann, q, rows, b, torch.zeros(10, dtype=torch.long), 10.0, 0)
+            g, h = torch.ones(10), torch.full((10,), 0.5)
+            got = backward(ann, q, rows, b, torch.zeros(10, dtype=torch.long), 10.0, f["lse"], f["entropy"], g, h)
+            # every score is the lowest value, as fp32 has it: all rows are alike, lse - the score is nothing in fp32, so p = 1
+            assert all(torch.isfinite(v).all() for v in got.values())
+            b[::2] = 0.0     # half of them at the lowest value: as if they were left out
+            f = forward(ann, q, rows, b, target | 1, 10.0, 0)
+            got = backward(ann, q, rows, b, target | 1, 10.0, f["lse"], f["entropy"], g, h)
+            b[1::2] = -math.inf
+            want = backward(ann, q, rows, b, target | 1, 10.0, f["lse"], f["entropy"], torch.zeros(10), h)
+            for name in ("dq", "drows", "drow_bias"):
+                assert torch.isfinite(got[name]).all() and torch.isfinite(want[name]).all()
+
+
 def test_no_rows():
     import paper_2503_17911_amd as ann
     got = forward(ann, torch.ones(5, 8), torch.zeros(0, 8), None, torch.zeros(5, dtype=torch.long), 1.0, 3)
