@@ -304,8 +304,16 @@ __global__ __launch_bounds__(1024) void norm_grad_sum_kernel(const float *__rest
   const uint32_t lane = threadIdx.x % 64, run = threadIdx.x / 64;
   const uint64_t c = (uint64_t)blockIdx.x * 64 + lane;  // column of [2][dim]
   float sum = 0.0f;
-  if (c < 2ull * dim)
-    for (uint32_t p = run * parts / 16; p < (run + 1) * parts / 16; ++p) sum += partial[p * 2ull * dim + c];
+  if (c < 2ull * dim) {
+    const uint32_t end = (run + 1) * parts / 16;
+    for (uint32_t p = run * parts / 16; p < end; p += 16) {  // 16 on their way at a time
+      float v[16];
+#pragma unroll
+      for (uint32_t u = 0; u < 16; ++u) v[u] = p + u < end ? partial[(p + u) * 2ull * dim + c] : 0.0f;
+#pragma unroll
+      for (uint32_t u = 0; u < 16; ++u) sum += v[u];
+    }
+  }
   runs[run][lane] = sum;
   __syncthreads();
   if (run != 0 || c >= 2ull * dim) return;

@@ -17,8 +17,9 @@
 
 namespace ann {
 
-constexpr uint32_t kNormRuns = 512;     // workgroups that look for the largest row norm
-constexpr uint32_t kSplitTarget = 6144; // workgroups of the product kernel: two rounds of three to a compute unit
+constexpr uint32_t kNormRuns = 2048;    // workgroups that look for the largest row norm: eight to a compute unit
+constexpr uint32_t kSplitTarget = 6144; // workgroups of the product kernels for short or few rows: rounds enough to end together
+constexpr uint32_t kWideSlots = 512;    // workgroups of the wide product that run at once: two to a compute unit
 constexpr float kNothing = -1000.0f;    // an exponent whose power is zero, and finite
 
 struct Stats {
@@ -83,10 +84,13 @@ struct Running {
 // Rows of a group of 64: a wavefront's of a tile.  Of a group of 16: those of one half of the lanes in a block of 32.
 __host__ __device__ constexpr uint32_t group_count(uint32_t n, int group) { return group == 64 ? (n + 63) / 64 : (n + 31) / 32 * 2; }
 
-// A block of 32 rows x 32 queries, rows down the registers and queries along the lanes.  MASKED: bias[32] (LDS) is added, -infinity
-// where a row does not count.  Returns the lane's largest score (16 rows').
+// Where a query's groups lie from the one's before (groups of 16: so that eight of them are two aligned pieces of 16 bytes).
+__host__ __device__ constexpr uint32_t group_stride(uint32_t n, int group) { return group == 64 ? group_count(n, 64) : (group_count(n, 16) + 7) / 8 * 8; }
+
+// A block of 32 rows x 32 queries, rows down the registers and queries along the lanes.  MASKED: scores are made whole, bias[32] (LDS)
+// added, -infinity where a row does not count.  Then the lane's largest score (of 16 rows).
 template <bool MASKED>
-__device__ __forceinline__ float largest_of(f32x16 &acc, const float *bias, float scale) {
+__device__ __forceinline__ void add_bias(f32x16 &acc, const float *bias, float scale) {
   if constexpr (MASKED) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
@@ -94,10 +98,31 @@ __device__ __forceinline__ float largest_of(f32x16 &acc, const float *bias, floa
       acc[r] = b == -INFINITY ? -INFINITY : __builtin_fmaf(acc[r], scale, b);
     }
   }
+}
+template <bool MASKED>
+__device__ __forceinline__ float largest_of(const f32x16 &acc, float scale) {
   float top = acc[0];
 #pragma unroll
   for (int r = 1; r < 16; ++r) top = fmaxf(top, acc[r]);
   return MASKED ? top : top * scale;
+}
+// The largest of the lane's 16 scores, its low four bits replaced by its number, and the second largest.  (Rows left out stand for the
+// lowest number: -infinity has no bits to spare.)
+struct TopTwo {
+  float first, second;
+};
+__device__ __forceinline__ float numbered(float s, uint32_t r) { return __uint_as_float((__float_as_uint(s) & ~15u) | r); }
+template <bool MASKED>
+__device__ __forceinline__ TopTwo two_largest_of(const f32x16 &acc, float scale) {
+  TopTwo t = {-3.402823466e38f, -3.402823466e38f};
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const float s = numbered(MASKED ? fmaxf(acc[r], -3.402823466e38f) : acc[r], r);
+    t.second = r ? fmaxf(t.second, fminf(t.first, s)) : t.second;
+    t.first = r ? fmaxf(t.first, s) : s;
+  }
+  if constexpr (!MASKED) t = {numbered(t.first * scale, __float_as_uint(t.first) & 15u), t.second * scale};
+  return t;
 }
 template <bool MASKED>
 __device__ __forceinline__ void take_block(const f32x16 &acc, Running &run, float c) {
@@ -109,9 +134,9 @@ __device__ __forceinline__ void take_block(const f32x16 &acc, Running &run, floa
 
 // Writes the largest scores of the groups of 64 rows from row0, of which the lane has seen the halves of two blocks.
 template <int GROUP>
-__device__ __forceinline__ void put_groups(float top0, float top1, uint32_t q, uint32_t nq, uint32_t row0, uint32_t n_groups, float *__restrict__ group_max) {
+__device__ __forceinline__ void put_groups(float top0, float top1, uint32_t q, uint32_t nq, uint32_t row0, uint32_t n_groups, uint32_t stride, float *__restrict__ group_max) {
   const int lane = lane_id();
-  float *out = group_max + (uint64_t)q * n_groups;
+  float *out = group_max + (uint64_t)q * stride;
   if constexpr (GROUP == 64) {
     const LanePair p = lane_pair<false>(__float_as_uint(fmaxf(top0, top1)));
     const float all = fmaxf(__uint_as_float(p.low), __uint_as_float(p.high));
@@ -132,51 +157,68 @@ __device__ __forceinline__ Stats join_halves(const Stats &s) {
 }
 
 // BIAS: rows may be left out, or the scale is negative.
-template <typename T, bool BIAS, int GROUP>
-__global__ __launch_bounds__(256) void row_scores_kernel(ScoreTable g, uint32_t q_tiles, uint32_t splits, float4 *__restrict__ stats,
-                                                         float *__restrict__ group_max) {
-  __shared__ __attribute__((aligned(16))) char lds[kTileBytes<T, kAlong, kAlong>];
-  __shared__ float row_bias[kTile];
-  // workgroup b runs on die b mod 8: a die takes all queries through its own part of the rows
-  const uint32_t b8 = blockIdx.x / 8, qt = b8 % q_tiles, split = b8 / q_tiles * 8 + blockIdx.x % 8;
-  if (split >= splits) return;
-  const uint32_t row_tiles = (g.n + kTile - 1) / kTile;
+template <typename T, bool BIAS, int GROUP, int MB>
+__global__ __launch_bounds__(256, MB == 4 ? 2 : 1) void row_scores_kernel(ScoreTable g, uint32_t q_tiles, uint32_t q_group, uint32_t splits, float4 *__restrict__ stats,
+                                                         float *__restrict__ group_max, float *__restrict__ group_second) {
+  constexpr int kMore = MB == 4 ? kWideBuffer : 16;
+  __shared__ __attribute__((aligned(16))) char lds[MB == 4 ? kWideBuffer : kTileBytes<T, kAlong, kAlong>], lds1[kMore], lds2[kMore];
+  __shared__ float row_bias[MB * 64];
+  constexpr uint32_t kRowTile = MB * 64;
+  // Workgroup b runs on die b mod 8.  A die takes a run of the pairs of a group of query tiles and a split of the rows, the queries of a
+  // group next to each other: these stay in its L2 (all queries of 4,096 x 768 are more than it holds, and the product waited
+  // for them), and every tile of rows is read by a group at a time.
+  const uint32_t groups = (q_tiles + q_group - 1) / q_group, pairs = groups * splits, per_die = (pairs + 7) / 8;
+  const uint32_t b8 = blockIdx.x / 8, in_die = b8 / q_group, pair = blockIdx.x % 8 * per_die + in_die;
+  const uint32_t qt = pair / splits * q_group + b8 % q_group, split = pair % splits;
+  if (in_die >= per_die || pair >= pairs || qt >= q_tiles) return;
+  const uint32_t row_tiles = (g.n + kRowTile - 1) / kRowTile;
   const uint32_t first = (uint32_t)((uint64_t)row_tiles * split / splits), last = (uint32_t)((uint64_t)row_tiles * (split + 1) / splits);
-  const int wave = (int)threadIdx.x / kWave, lane = lane_id(), mw = wave / 2 * 64, nw = wave % 2 * 64;
+  const int wave = (int)threadIdx.x / kWave, lane = lane_id(), mw = wave / 2 * MB * 32, nw = wave % 2 * 64;
   const Lines<T> X = {(const T *)g.rows, g.row_stride, g.n, g.d}, Q = {(const T *)g.q, g.q_stride, g.nq, g.d};
-  const uint32_t n_groups = GROUP ? group_count(g.n, GROUP) : 0;
+  const uint32_t n_groups = GROUP ? group_count(g.n, GROUP) : 0, stride = GROUP ? group_stride(g.n, GROUP) : 0;
   const float c = g.scale * kLog2e;
   Running run[2];
   for (uint32_t tile = first; tile < last; ++tile) {
-    const uint32_t row0 = tile * kTile;
-    const bool whole = row0 + kTile <= g.n;
-    f32x16 acc[2][2];
+    const uint32_t row0 = tile * kRowTile;
+    const bool whole = row0 + kRowTile <= g.n;
+    f32x16 acc[MB][2];
     clear(acc);
-    tile_product<T, kAlong, kAlong>(acc, X, row0, Q, qt * kTile, 0, g.d, lds);
+    if constexpr (MB == 4)
+      wide_product<T, kAlong, kAlong>(acc, X, row0, Q, qt * kTile, 0, g.d, lds, lds1, lds2);
+    else
+      tile_product<T, kAlong, kAlong>(acc, X, row0, Q, qt * kTile, 0, g.d, lds);
     if (BIAS || !whole) {
       // (read by the tile before's epilogue: the barriers of the product lie in between; d > 0)
-      if (threadIdx.x < kTile) row_bias[threadIdx.x] = row0 + threadIdx.x < g.n ? (BIAS && g.bias ? g.bias[row0 + threadIdx.x] : 0.0f) : -INFINITY;
+      if (threadIdx.x < kRowTile) row_bias[threadIdx.x] = row0 + threadIdx.x < g.n ? (BIAS && g.bias ? g.bias[row0 + threadIdx.x] : 0.0f) : -INFINITY;
       __syncthreads();
     }
     const auto finish = [&](auto masked) {
       constexpr bool MASKED = decltype(masked)::value;
-      float top[2][2];
-      bool behind = false;
+      const bool is_numbered = GROUP == 16 && (MB == 4 || group_second);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
+        const uint32_t q = qt * kTile + nw + j * 32 + lane % 32;
+        // (two blocks at a time, each with a look at the reference: no more intermediate values are live than fit)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) top[i][j] = largest_of<MASKED>(acc[i][j], row_bias + mw + i * 32, g.scale);
-        behind |= run[j].behind(fmaxf(top[0][j], top[1][j]));
-      }
-      if (__any(behind)) {
+        for (int i0 = 0; i0 < MB; i0 += 2) {
+          float top[2], second[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) run[j].raise(fmaxf(top[0][j], top[1][j]));
-      }
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        put_groups<GROUP>(top[0][j], top[1][j], qt * kTile + nw + j * 32 + lane % 32, g.nq, row0 + mw, n_groups, group_max);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) take_block<MASKED>(acc[i][j], run[j], c);
+          for (int i = 0; i < 2; ++i) {
+            f32x16 &block = acc[i0 + i][j];
+            add_bias<MASKED>(block, row_bias + mw + (i0 + i) * 32, g.scale);
+            if (is_numbered) {
+              const TopTwo t = two_largest_of<MASKED>(block, g.scale);
+              top[i] = t.first, second[i] = t.second;
+            } else {
+              top[i] = largest_of<MASKED>(block, g.scale);
+            }
+            if (__any(run[j].behind(top[i]))) run[j].raise(top[i]);
+            take_block<MASKED>(block, run[j], c);
+            if (MB == 4) __builtin_amdgcn_sched_barrier(0);
+          }
+          put_groups<GROUP>(top[0], top[1], q, g.nq, row0 + mw + i0 * 32, n_groups, stride, group_max);
+          if (is_numbered) put_groups<GROUP>(second[0], second[1], q, g.nq, row0 + mw + i0 * 32, n_groups, stride, group_second);
+        }
       }
     };
     if (BIAS || !whole)
@@ -226,7 +268,7 @@ __global__ __launch_bounds__(256, 2) void row_scores_short_kernel(ScoreTable g, 
   const uint32_t first = (uint32_t)((uint64_t)tiles * split / splits), last = (uint32_t)((uint64_t)tiles * (split + 1) / splits);
   const int wave = (int)threadIdx.x / kWave, lane = lane_id();
   const T *rows = (const T *)g.rows;
-  const uint32_t n_groups = GROUP ? group_count(g.n, GROUP) : 0, q = qt * kShortQueries + wave * 64 + lane % 32;  // (and q + 32)
+  const uint32_t n_groups = GROUP ? group_count(g.n, GROUP) : 0, stride = GROUP ? group_stride(g.n, GROUP) : 0, q = qt * kShortQueries + wave * 64 + lane % 32;  // (and q + 32)
   const float c = g.scale * kLog2e;
   E query[2][KS];
 #pragma unroll
@@ -295,7 +337,8 @@ __global__ __launch_bounds__(256, 2) void row_scores_short_kernel(ScoreTable g, 
       bool behind = false;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        top[half][j] = largest_of<MASKED>(past[j], row_bias[tile & 3] + half * 32, g.scale);
+        add_bias<MASKED>(past[j], row_bias[tile & 3] + half * 32, g.scale);
+        top[half][j] = largest_of<MASKED>(past[j], g.scale);
         behind |= run[j].behind(top[half][j]);
       }
       if (__any(behind)) {
@@ -312,7 +355,7 @@ __global__ __launch_bounds__(256, 2) void row_scores_short_kernel(ScoreTable g, 
       with(std::false_type());
     if (GROUP != 0 && half) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j) put_groups<GROUP>(top[0][j], top[1][j], q + j * 32, g.nq, tile * kShortRows, n_groups, group_max);
+      for (int j = 0; j < 2; ++j) put_groups<GROUP>(top[0][j], top[1][j], q + j * 32, g.nq, tile * kShortRows, n_groups, stride, group_max);
     }
   };
   if (first < last) {
@@ -399,7 +442,7 @@ __global__ __launch_bounds__(kStreamThreads) void row_stream_kernel(ScoreTable g
   // blocks of 64 rows in turn to the wavefronts of the workgroup, which has a run of them to itself
   const uint32_t blocks = (g.n + kStreamRows - 1) / kStreamRows;
   const uint32_t first = (uint32_t)((uint64_t)blocks * blockIdx.x / gridDim.x), last = (uint32_t)((uint64_t)blocks * (blockIdx.x + 1) / gridDim.x);
-  const uint32_t n_groups = GROUP ? group_count(g.n, GROUP) : 0;
+  const uint32_t n_groups = GROUP ? group_count(g.n, GROUP) : 0, stride = GROUP ? group_stride(g.n, GROUP) : 0;
   const float c = g.scale * kLog2e;
   const T *rows = (const T *)g.rows;
   const int in_block = lane % 16 / 4 * 8 + lane % 4;  // the lane's row of a pair's 32, of its first block
@@ -508,7 +551,7 @@ __global__ __launch_bounds__(kStreamThreads) void row_stream_kernel(ScoreTable g
               p = lane_pair<false>(__float_as_uint(v));
               return fmaxf(__uint_as_float(p.low), __uint_as_float(p.high));
             };
-            float *out = group_max + (uint64_t)q * n_groups;
+            float *out = group_max + (uint64_t)q * stride;
             if constexpr (GROUP == 64) {
               const float most = over_parts(all);
               if (lane < 16 && q < g.nq) out[block] = most;
@@ -605,10 +648,10 @@ __global__ __launch_bounds__(256) void row_norms_kernel(ScoreTable g, float *__r
 // How far a score of the product kernel may lie from its value: each of d additions rounds a
 // partial sum of at most |q| |x| (2^-24 of it; twice that for the order inside the
 // instruction), the products of parts left out are below 2^-23 of |q| |x|, and the last
-// product and addition round a score.  fp32: six products to an element.
-__device__ __forceinline__ float score_room(uint32_t d, bool parts, float q_norm, float x_norm, float scale, float largest) {
+// product and addition round a score, which is at most `largest` in size.  fp32: six products to an element.
+__device__ __forceinline__ float score_room(uint32_t d, bool parts, bool is_numbered, float q_norm, float x_norm, float scale, float largest) {
   const float size = fabsf(scale) * q_norm * x_norm * 1.001f;
-  return ((parts ? 6.0f : 1.0f) * (float)d + 64.0f) * 0x1p-23f * size + 0x1p-22f * (fabsf(largest) + size);
+  return ((parts ? 6.0f : 1.0f) * (float)d + 64.0f) * 0x1p-23f * size + (is_numbered ? 0x1p-18f : 0x1p-22f) * (largest + size);
 }
 
 constexpr uint32_t kListed = 1024;      // groups that are taken up at a time
@@ -621,7 +664,7 @@ struct FinishArgs {
   ScoreTable g;
   const uint32_t *targets;
   const float4 *stats;
-  const float *group_max, *norms;
+  const float *group_max, *group_second, *norms;  // group_second: with numbered largest scores (groups of 16), else NULL
   uint32_t splits, k, norm_runs;
   float *logprob, *entropy, *lse, *alt_logprobs;
   uint32_t *alt_ids;
@@ -675,15 +718,15 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 5 : 4) void row_finish_ke
   __shared__ double room64[2][kWaves];
   __shared__ float room32[4][kWaves];
   __shared__ __attribute__((aligned(16))) float tops[kTops];
-  __shared__ uint32_t n_list, n_rough, n_best;
+  __shared__ uint32_t n_list, n_single, n_rough, n_best;
   __shared__ float kth;
   const uint32_t i = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const ScoreTable &g = a.g;
   const T *rows = (const T *)g.rows;
-  const uint32_t n_groups = GROUP ? group_count(g.n, GROUP) : 0;
-  const float *gm = a.group_max + (uint64_t)i * n_groups;
+  const uint32_t n_groups = GROUP ? group_count(g.n, GROUP) : 0, stride = GROUP ? group_stride(g.n, GROUP) : 0;
+  const float *gm = a.group_max + (uint64_t)i * stride;
   const uint32_t target = a.targets ? a.targets[i] : ANN_PAD_ID;
-  if (tid == 0) kth = -INFINITY, n_list = 0, n_rough = 0, n_best = 0;
+  if (tid == 0) kth = -INFINITY, n_list = 0, n_single = 0, n_rough = 0, n_best = 0;
   float qsq = 0.0f;
   for (uint32_t c = tid; c < (g.d + 511) / 512 * 512; c += THREADS) {
     const float v = c < g.d ? to_f32(((const T *)g.q)[(uint64_t)i * g.q_stride + c]) : 0.0f;
@@ -773,8 +816,9 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 5 : 4) void row_finish_ke
     __shared__ uint32_t list[kListed], rough[kWaves * GROUP];
     __shared__ double best[2][kBest];
     __shared__ uint32_t best_id[2][kBest];
+    const float *second = GROUP == 16 && a.group_second ? a.group_second + (uint64_t)i * stride : nullptr;
     const float lost = (float)g.d * 0x1p-126f;  // squares below the smallest normal number may have gone
-    const float error = score_room(g.d, sizeof(T) == 4, sqrtf(qsq + lost), sqrtf(x_norm + lost), g.scale, largest);
+    const float error = score_room(g.d, sizeof(T) == 4, second != nullptr, sqrtf(qsq + lost), sqrtf(x_norm + lost), g.scale, fmaxf(fabsf(largest), fabsf(kth)));
     const bool bounded = error < INFINITY && kth > -INFINITY;  // (false with NaN)
     const float least = bounded ? kth - 2.0f * error : -INFINITY;
     double bound = bounded ? (double)kth - (double)error : -INFINITY;  // the k-th score is at least this
@@ -811,20 +855,47 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 5 : 4) void row_finish_ke
         for (uint32_t u = 0; u < kInFlight; ++u) v[u] = c + u * THREADS < end ? gm[c + u * THREADS] : NAN;
 #pragma unroll
         for (uint32_t u = 0; u < kInFlight; ++u)
-          if (v[u] >= least) {
-            const uint32_t at = atomicAdd(&n_list, 1u);  // (the order plays no part)
-            if (at < kListed) list[at] = c + u * THREADS;
+          if (v[u] >= least) {  // (the order plays no part)
+            const uint32_t group = c + u * THREADS;
+            if (bounded && second && !(second[group] >= least)) {  // one row of it: from the list's end
+              const uint32_t at = atomicAdd(&n_single, 1u);
+              if (at < kListed) list[kListed - 1 - at] = (uint32_t)group_row<GROUP>(group, __float_as_uint(v[u]) & 15u);
+            } else {
+              const uint32_t at = atomicAdd(&n_list, 1u);
+              if (at < kListed) list[at] = group;
+            }
           }
       }
       __syncthreads();
-      const uint32_t count = n_list;
+      const uint32_t count = n_list, singles = n_single;
       __syncthreads();
-      if (tid == 0) n_list = 0;
-      if (count > kListed) {  // (of all groups)
+      if (tid == 0) n_list = 0, n_single = 0;
+      if (count + singles > kListed) {  // (of all groups)
         end = kListed;
         __syncthreads();
         continue;
       }
+      // Scores rows in fp64, a wavefront to a row, and keeps what may be among the best.  All lanes.
+      const auto score_rows = [&](const uint32_t *ids, int step, uint32_t found, bool first_of_all) {
+        for (uint32_t f0 = 0; f0 < found; f0 += kWaves) {
+          if (f0 != 0 || !first_of_all) {  // (at first there is room)
+            const uint32_t held = n_best;
+            __syncthreads();  // all lanes have read it: they agree whether to make more
+            if (held + kWaves > kBest) keep_best();
+          }
+          if (f0 + wave < found) {
+            const uint32_t row = ids[(int)(f0 + wave) * step];
+            const float bias = row < g.n ? (g.bias ? g.bias[row] : 0.0f) : -INFINITY;
+            const double s = bias != -INFINITY ? (double)g.scale * exact_dot<T>(rows + row * g.row_stride, q, g.d) + (double)bias : (double)NAN;
+            if (lane == 0 && s >= bound) {
+              const uint32_t at = atomicAdd(&n_best, 1u);
+              best[side][at] = s, best_id[side][at] = row;
+            }
+          }
+          __syncthreads();
+        }
+      };
+      score_rows(list + kListed - 1, -1, singles, begin == 0);
       for (uint32_t c0 = 0; c0 < count; c0 += kWaves) {
         const uint32_t c = c0 + wave;
         if (c < count) {
@@ -868,22 +939,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 5 : 4) void row_finish_ke
         }
         __syncthreads();
         const uint32_t found = n_rough;
-        for (uint32_t f0 = 0; f0 < found; f0 += kWaves) {
-          if ((begin | c0 | f0) != 0) {  // (at first there is room)
-            const uint32_t held = n_best;
-            __syncthreads();  // all lanes have read it: they agree whether to make more
-            if (held + kWaves > kBest) keep_best();
-          }
-          if (f0 + wave < found) {
-            const uint32_t row = rough[f0 + wave];
-            const double s = (double)g.scale * exact_dot<T>(rows + row * g.row_stride, q, g.d) + (double)(g.bias ? g.bias[row] : 0.0f);
-            if (lane == 0 && s >= bound) {
-              const uint32_t at = atomicAdd(&n_best, 1u);
-              best[side][at] = s, best_id[side][at] = row;
-            }
-          }
-          __syncthreads();
-        }
+        score_rows(rough, 1, found, (begin | c0 | singles) == 0);
         if (tid == 0) n_rough = 0;
         __syncthreads();
       }
@@ -913,7 +969,9 @@ struct ForwardPlan {
   int group = 0;
   int blocks = 0;  // of 16 queries, if the rows are streamed
   int slices = 0;  // of 16 columns, if the queries stay in registers
-  uint64_t stats_at = 0, groups_at = 0, norms_at = 0;
+  bool wide = false;  // tiles of 256 rows
+  uint64_t stats_at = 0, groups_at = 0, seconds_at = 0, norms_at = 0;
+  bool numbered = false;
   Parts parts;
 };
 
@@ -935,30 +993,56 @@ static ForwardPlan forward_plan(uint32_t nq, uint64_t n, uint32_t d, uint32_t ty
   } else {
     const bool rows_short = type != ANN_F32 && d <= 128;
     if (rows_short) p.slices = d <= 32 ? 2 : d <= 64 ? 4 : d <= 96 ? 6 : 8;
-    const uint32_t queries = rows_short ? kShortQueries : kTile, rows = rows_short ? kShortRows : kTile;
+    const uint32_t queries = rows_short ? kShortQueries : kTile;
     p.q_tiles = (nq + queries - 1) / queries;
+    // (tiles of 256 rows where they still fill the card)
+    p.wide = !rows_short && type != ANN_F32 && d % kWideSlice == 0 && p.q_tiles * ((n + 2 * kTile - 1) / (2 * kTile)) >= kWideSlots;
+    const uint32_t rows = rows_short ? kShortRows : p.wide ? 2 * kTile : kTile;
     const uint32_t row_tiles = (uint32_t)((n + rows - 1) / rows);
     uint32_t want = (kSplitTarget + p.q_tiles - 1) / p.q_tiles;
     want = (want + 7) / 8 * 8;
+    if (p.wide) {
+      // few rounds of workgroups whose last one is as full as can be: the least rounds times tiles
+      uint64_t least = ~0ull;
+      for (uint32_t s = ((kWideSlots + p.q_tiles - 1) / p.q_tiles + 7) / 8 * 8, end = s * 4; s <= end; s += 8) {
+        const uint64_t cost = ((uint64_t)p.q_tiles * s + kWideSlots - 1) / kWideSlots * ((row_tiles + s - 1) / s);
+        if (cost < least) least = cost, want = s;
+      }
+    }
     p.splits = want < row_tiles ? want : row_tiles;
   }
-  // What a group costs: 8 n / group bytes per query written and read, and about k group d elements read again.
-  if (k) p.group = 4 * n >= 1024ull * k * d ? 64 : 16;
+  // What a group costs: 8 n / group bytes per query written and read, and about k group d elements read again; of a
+  // numbered one of 16 (long rows, where the end of a tile is a small part) 12 n / 16 bytes and mostly k rows.
+  p.numbered = k && !p.blocks && !p.slices;
+  if (p.numbered)
+    p.group = n / 8 + 64ull * k * d * type_bytes(type) <= 12 * n / 16 + (uint64_t)k * d * type_bytes(type) ? 64 : 16;
+  else if (k)
+    p.group = 4 * n >= 1024ull * k * d ? 64 : 16;
+  p.numbered = p.numbered && p.group == 16;
   p.stats_at = p.parts.take((uint64_t)p.splits * nq * sizeof(float4));
   if (k) {
-    p.groups_at = p.parts.take((uint64_t)nq * group_count((uint32_t)n, p.group) * sizeof(float));
+    p.groups_at = p.parts.take((uint64_t)nq * group_stride((uint32_t)n, p.group) * sizeof(float));
+    if (p.numbered) p.seconds_at = p.parts.take((uint64_t)nq * group_stride((uint32_t)n, 16) * sizeof(float));
     p.norm_runs = p.blocks ? p.splits : (uint32_t)((n + 15) / 16 < kNormRuns ? (n + 15) / 16 : kNormRuns);
     p.norms_at = p.parts.take(p.norm_runs * sizeof(float));
   }
   return p;
 }
 
+// Query tiles that a die takes together: as many as fill a quarter of its L2, at most eight.
+static uint32_t query_group(uint32_t q_tiles, uint32_t d, uint32_t elem) {
+  uint32_t group = 8;
+  while (group > 1 && (group * kTile * (uint64_t)d * elem > (1u << 20) || group > q_tiles)) group /= 2;
+  return group;
+}
+static uint32_t query_grid(uint32_t q_tiles, uint32_t group, uint32_t splits) { return ((q_tiles + group - 1) / group * splits + 7) / 8 * 8 * group; }
+
 template <typename T>
 static ann_status forward(const ann_row_scores &s, uint32_t k, const ForwardPlan &p, FinishArgs f, char *ws, hipStream_t st) {
   const ScoreTable &g = f.g;
   if (s.n) {
     float4 *stats = (float4 *)(ws + p.stats_at);
-    float *groups = (float *)(ws + p.groups_at), *norms = (float *)(ws + p.norms_at);
+    float *groups = (float *)(ws + p.groups_at), *seconds = p.numbered ? (float *)(ws + p.seconds_at) : nullptr, *norms = (float *)(ws + p.norms_at);
     const bool bias = g.bias || g.scale < 0.0f;
     hipError_t refused = hipSuccess;
     const auto run = [&](auto with_bias, auto group) {
@@ -971,8 +1055,11 @@ static ann_status forward(const ann_row_scores &s, uint32_t k, const ForwardPlan
         const auto rows_short = [&](auto slices) {
           if constexpr (sizeof(T) == 2) row_scores_short_kernel<T, decltype(slices)::value, BIAS, GROUP><<<grid, 256, 0, st>>>(g, q_tiles, p.splits, stats, groups);
         };
-        if (!is_short)
-          row_scores_kernel<T, BIAS, GROUP><<<grid, 256, 0, st>>>(g, q_tiles, p.splits, stats, groups);
+        const uint32_t q_group = query_group(q_tiles, g.d, sizeof(T)), paired = query_grid(q_tiles, q_group, p.splits);
+        if (p.wide && wide_operand(g.q, g.q_stride) && wide_operand(g.rows, g.row_stride)) {
+          if constexpr (sizeof(T) == 2) row_scores_kernel<T, BIAS, GROUP, 4><<<paired, 256, 0, st>>>(g, q_tiles, q_group, p.splits, stats, groups, seconds);
+        } else if (!is_short)
+          row_scores_kernel<T, BIAS, GROUP, 2><<<paired, 256, 0, st>>>(g, q_tiles, q_group, p.splits, stats, groups, seconds);
         else if (p.slices == 2)
           rows_short(std::integral_constant<int, 2>());
         else if (p.slices == 4)
@@ -1011,7 +1098,7 @@ static ann_status forward(const ann_row_scores &s, uint32_t k, const ForwardPlan
       run_group(std::false_type());
     ANN_HIP(refused);
     ANN_HIP(hipGetLastError());
-    f.stats = stats, f.group_max = groups, f.norms = norms, f.splits = p.splits, f.norm_runs = p.norm_runs;
+    f.stats = stats, f.group_max = groups, f.group_second = seconds, f.norms = norms, f.splits = p.splits, f.norm_runs = p.norm_runs;
   }
   const uint32_t lds = (g.d + 511) / 512 * 512 * sizeof(float);
   const auto end = [&](auto group) {

@@ -25,6 +25,7 @@ namespace ann {
 
 constexpr uint64_t kChunkBytes = 512ull << 20;  // of G at a time
 constexpr uint32_t kGradTarget = 768;           // workgroups of a product: three to a compute unit
+constexpr uint32_t kWideSlots = 512;            // of a wide one: two
 
 // Wavefronts to a SIMD of the gradients' products (three instead of two: 303 -> 237 and 282 -> 255 us with 2,048 x 50,000 x 768).
 template <typename T>
@@ -139,32 +140,41 @@ __global__ __launch_bounds__(256) void grad_scores_kernel(GradArgs a, uint32_t r
   }
 }
 
-// part[split][q][c] (+)= sum over the split's rows of the chunk of G[q][j] x[j][c]  (rows left out may hold anything: read as zeros)
-template <typename T>
-__global__ __launch_bounds__(256, kGradWaves<T>) void grad_queries_kernel(ScoreTable g, uint32_t row0, uint32_t rows, uint32_t ld, const T *__restrict__ G, uint32_t splits,
-                                                           float *__restrict__ part, bool add) {
-  __shared__ __attribute__((aligned(16))) char lds[kTileBytes<T, kAlong, kAcross>];
-  const uint32_t c_tiles = (g.d + kTile - 1) / kTile, q_tiles = (g.nq + kTile - 1) / kTile;
-  // a die takes a run of rows through all columns and queries
-  const uint32_t b8 = blockIdx.x / 8, ct = b8 % c_tiles, qt = b8 / c_tiles % q_tiles, split = b8 / c_tiles / q_tiles * 8 + blockIdx.x % 8;
-  if (split >= splits) return;
-  const uint32_t slices = (rows + Operand16<T>::kSlice - 1) / Operand16<T>::kSlice;
-  const uint32_t begin = (uint32_t)((uint64_t)slices * split / splits) * Operand16<T>::kSlice;
-  uint32_t end = (uint32_t)((uint64_t)slices * (split + 1) / splits) * Operand16<T>::kSlice;
-  if (end > rows) end = rows;
-  const Lines<T> A = {G, ld, g.nq, rows}, B = {(const T *)g.rows + row0 * g.row_stride, g.row_stride, g.d, rows, g.bias ? g.bias + row0 : nullptr};
-  f32x16 acc[2][2];
+// part[split][q][c] (+)= sum over the split's rows of the chunk of G[q][j] x[j][c]  (rows left out may hold anything: read as zeros, or,
+// MB == 4, there are none)
+template <typename T, int MB>
+__global__ __launch_bounds__(256, MB == 4 ? 2 : kGradWaves<T>) void grad_queries_kernel(ScoreTable g, uint32_t row0, uint32_t rows, uint32_t ld, const T *__restrict__ G,
+                                                                                        uint32_t splits, float *__restrict__ part, bool add) {
+  constexpr int kQueryTile = MB * 64, kMore = MB == 4 ? kWideBuffer : 16, kSlice = MB == 4 ? kWideSlice : Operand16<T>::kSlice;
+  __shared__ __attribute__((aligned(16))) char lds[MB == 4 ? kWideBuffer : kTileBytes<T, kAlong, kAcross>], lds1[kMore], lds2[kMore];
+  const uint32_t c_tiles = (g.d + kTile - 1) / kTile, q_tiles = (g.nq + kQueryTile - 1) / kQueryTile;
+  // workgroup b runs on die b mod 8: a die takes a run of rows through all columns and queries
+  const uint32_t all = c_tiles * q_tiles * splits, per_die = (all + 7) / 8, in_die = blockIdx.x / 8, at = blockIdx.x % 8 * per_die + in_die;
+  const uint32_t ct = at % c_tiles, qt = at / c_tiles % q_tiles, split = at / c_tiles / q_tiles;
+  if (in_die >= per_die || at >= all) return;
+  const uint32_t slices = (rows + kSlice - 1) / kSlice;
+  const uint32_t begin = (uint32_t)((uint64_t)slices * split / splits) * kSlice;
+  uint32_t end = (uint32_t)((uint64_t)slices * (split + 1) / splits) * kSlice;
+  f32x16 acc[MB][2];
   clear(acc);
-  tile_product<T, kAlong, kAcross>(acc, A, qt * kTile, B, ct * kTile, begin, end, lds);
+  if constexpr (MB == 4) {
+    // (G is zero behind the last row)
+    const Lines<T> A = {G, ld, g.nq, ld}, B = {(const T *)g.rows + row0 * g.row_stride, g.row_stride, g.d, rows};
+    wide_product<T, kAlong, kAcross>(acc, A, qt * kQueryTile, B, ct * kTile, begin, end, lds, lds1, lds2);
+  } else {
+    if (end > rows) end = rows;
+    const Lines<T> A = {G, ld, g.nq, rows}, B = {(const T *)g.rows + row0 * g.row_stride, g.row_stride, g.d, rows, g.bias ? g.bias + row0 : nullptr};
+    tile_product<T, kAlong, kAcross>(acc, A, qt * kQueryTile, B, ct * kTile, begin, end, lds);
+  }
   const int wave = (int)threadIdx.x / kWave, lane = lane_id();
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < MB; ++i)
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const uint32_t c = ct * kTile + wave % 2 * 64 + j * 32 + lane % 32;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const uint32_t q = qt * kTile + wave / 2 * 64 + i * 32 + block_row(r);
+        const uint32_t q = qt * kQueryTile + wave / 2 * MB * 32 + i * 32 + block_row(r);
         if (q < g.nq && c < g.d) {
           float *p = part + ((uint64_t)split * g.nq + q) * g.d + c;
           *p = add ? *p + acc[i][j][r] : acc[i][j][r];
@@ -173,45 +183,70 @@ __global__ __launch_bounds__(256, kGradWaves<T>) void grad_queries_kernel(ScoreT
     }
 }
 
-// dq[q][c] = scale sum over the splits, in their order, and what was left of the given row's element.  A workgroup takes 256 / LANES
-// queries; eight splits' parts are on their way at a time.
-template <typename T, int LANES>
-__global__ __launch_bounds__(256) void grad_queries_sum_kernel(GradArgs a, const float *__restrict__ part, uint32_t splits, T *__restrict__ dq, uint64_t stride) {
+// dq[q][c] = scale sum over the splits, and what was left of the given row's element.  A workgroup of THREADS lanes takes one
+// query after LANES * RUNS of them: LANES to its columns, RUNS to runs of its splits, which are added in the runs' order.
+// Eight splits' parts are on their way at a time.
+template <typename T, int LANES, int RUNS, int THREADS>
+__global__ __launch_bounds__(THREADS) void grad_queries_sum_kernel(GradArgs a, const float *__restrict__ part, uint32_t splits, T *__restrict__ dq, uint64_t stride) {
+  constexpr int kQueries = THREADS / (LANES * RUNS);
+  static_assert(RUNS == 1 || kQueries == 1, "runs are joined by the whole workgroup");
+  __shared__ float room[RUNS > 1 ? RUNS : 1][RUNS > 1 ? LANES : 1];
   const ScoreTable &g = a.g;
-  const uint64_t q = (uint64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES, all = (uint64_t)g.nq * g.d;
+  const uint64_t q = (uint64_t)blockIdx.x * kQueries + threadIdx.x / (LANES * RUNS), all = (uint64_t)g.nq * g.d;
   if (q >= g.nq) return;
   const float by = a.scaling ? g.scale * a.scaling[1] : g.scale;
   const uint32_t target = sizeof(T) == 2 && a.targets ? a.targets[q] : ANN_PAD_ID;
   const bool given = target < g.n && !(g.bias && g.bias[target] == -INFINITY);
   const float rest = given ? a.rest[q] : 0.0f;
-  for (uint32_t c = threadIdx.x % LANES; c < g.d; c += LANES) {
-    const float *p = part + q * g.d + c;
+  const uint32_t run = threadIdx.x / LANES % RUNS, end = (uint32_t)((uint64_t)splits * (run + 1) / RUNS);
+  for (uint32_t c0 = 0; c0 < g.d; c0 += LANES) {
+    const uint32_t c = c0 + threadIdx.x % LANES;
     float sum = 0.0f;
-    uint32_t s = 0;
-    for (; s + 8 <= splits; s += 8) {
-      float v[8];
+    if (c < g.d) {
+      const float *p = part + q * g.d + c;
+      uint32_t s = (uint32_t)((uint64_t)splits * run / RUNS);
+      for (; s + 8 <= end; s += 8) {
+        float v[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) v[u] = p[(s + u) * all];
+        for (int u = 0; u < 8; ++u) v[u] = p[(s + u) * all];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) sum += v[u];
+        for (int u = 0; u < 8; ++u) sum += v[u];
+      }
+      for (; s < end; ++s) sum += p[s * all];
     }
-    for (; s < splits; ++s) sum += p[s * all];
+    if constexpr (RUNS > 1) {
+      __syncthreads();  // (the columns before have been read)
+      room[run][threadIdx.x % LANES] = sum;
+      __syncthreads();
+      if (run != 0) continue;
+#pragma unroll
+      for (int r = 1; r < RUNS; ++r) sum += room[r][threadIdx.x % LANES];
+    }
+    if (c >= g.d) continue;
     if (given) sum = __builtin_fmaf(rest, to_f32(((const T *)g.rows)[target * g.row_stride + c]), sum);
     dq[q * stride + c] = from_f32<T>(sum * by);
   }
 }
 
-// drows[row0 + j][c] = scale sum over the queries of G[q][j] q[q][c]
-template <typename T>
+// drows[row0 + j][c] = scale sum over the queries of G[q][j] q[q][c].  SPLIT: part[split][row][c] instead, of a split's queries.
+template <typename T, bool SPLIT>
 __global__ __launch_bounds__(256, kGradWaves<T>) void grad_rows_kernel(ScoreTable g, uint32_t row0, uint32_t rows, uint32_t ld, const T *__restrict__ G, T *__restrict__ out,
-                                                        uint64_t stride, const float *__restrict__ scaling) {
+                                                        uint64_t stride, const float *__restrict__ scaling, float *__restrict__ part, uint32_t splits) {
   __shared__ __attribute__((aligned(16))) char lds[kTileBytes<T, kAcross, kAcross>];
-  const uint32_t c_tiles = (g.d + kTile - 1) / kTile, ct = blockIdx.x / 8 % c_tiles, rt = blockIdx.x / 8 / c_tiles * 8 + blockIdx.x % 8;
+  const uint32_t c_tiles = (g.d + kTile - 1) / kTile, b8 = blockIdx.x / 8, split = SPLIT ? b8 % splits : 0, at = SPLIT ? b8 / splits : b8;
+  const uint32_t ct = at % c_tiles, rt = at / c_tiles * 8 + blockIdx.x % 8;
   if (rt >= ld / kTile) return;
   const Lines<T> A = {G, ld, ld, g.nq}, B = {(const T *)g.q, g.q_stride, g.d, g.nq};
+  uint32_t begin = 0, end = g.nq;
+  if constexpr (SPLIT) {
+    const uint32_t slices = (g.nq + Operand16<T>::kSlice - 1) / Operand16<T>::kSlice;
+    begin = (uint32_t)((uint64_t)slices * split / splits) * Operand16<T>::kSlice;
+    end = (uint32_t)((uint64_t)slices * (split + 1) / splits) * Operand16<T>::kSlice;
+    if (end > g.nq) end = g.nq;
+  }
   f32x16 acc[2][2];
   clear(acc);
-  tile_product<T, kAcross, kAcross>(acc, A, rt * kTile, B, ct * kTile, 0, g.nq, lds);
+  tile_product<T, kAcross, kAcross>(acc, A, rt * kTile, B, ct * kTile, begin, end, lds);
   const int wave = (int)threadIdx.x / kWave, lane = lane_id();
   const float by = scaling ? g.scale * scaling[1] : g.scale;
 #pragma unroll
@@ -223,11 +258,29 @@ __global__ __launch_bounds__(256, kGradWaves<T>) void grad_rows_kernel(ScoreTabl
       for (int r = 0; r < 16; ++r) {
         const uint32_t row = rt * kTile + wave / 2 * 64 + i * 32 + block_row(r);
         if (row < rows && c < g.d) {
-          const bool left_out = g.bias && g.bias[row0 + row] == -INFINITY;  // (zero, whatever the queries hold)
-          out[(uint64_t)(row0 + row) * stride + c] = from_f32<T>(left_out ? 0.0f : acc[i][j][r] * by);
+          if constexpr (SPLIT) {
+            part[((uint64_t)split * rows + row) * g.d + c] = acc[i][j][r];
+          } else {
+            const bool left_out = g.bias && g.bias[row0 + row] == -INFINITY;  // (zero, whatever the queries hold)
+            out[(uint64_t)(row0 + row) * stride + c] = from_f32<T>(left_out ? 0.0f : acc[i][j][r] * by);
+          }
         }
       }
     }
+}
+
+// The splits' parts, in their order.
+template <typename T>
+__global__ __launch_bounds__(256) void grad_rows_sum_kernel(ScoreTable g, uint32_t row0, uint32_t rows, const float *__restrict__ part, uint32_t splits, T *__restrict__ out,
+                                                            uint64_t stride, const float *__restrict__ scaling) {
+  const uint64_t all = (uint64_t)rows * g.d, at = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= all) return;
+  const float by = scaling ? g.scale * scaling[1] : g.scale;
+  float sum = 0.0f;
+  for (uint32_t s = 0; s < splits; ++s) sum += part[s * all + at];
+  const uint64_t row = row0 + at / g.d;
+  const bool left_out = g.bias && g.bias[row] == -INFINITY;
+  out[row * stride + at % g.d] = from_f32<T>(left_out ? 0.0f : sum * by);
 }
 
 // drow_bias[row0 + j] = sum of the parts, in their order
@@ -469,8 +522,10 @@ __global__ __launch_bounds__(256, 2) void grad_short_kernel(GradArgs a, uint32_t
 // ---------------------------------------------------------------------------
 struct BackwardPlan {
   uint32_t q_tiles = 0, chunk = 0, splits = 0;  // chunk: rows at a time, a multiple of kTile
+  uint32_t row_splits = 1;                      // of the queries, in the rows' product
   int slices = 0;                               // of 16 columns, if G stays in registers
-  uint64_t g_at = 0, part_at = 0, sums_at = 0, scaling_at = 0, rest_at = 0;
+  bool wide = false;                            // the queries' product: tiles of 256 of them
+  uint64_t g_at = 0, part_at = 0, row_part_at = 0, sums_at = 0, scaling_at = 0, rest_at = 0;
   Parts parts;
 };
 
@@ -494,11 +549,31 @@ static BackwardPlan backward_plan(uint32_t nq, uint64_t n, uint32_t d, uint32_t 
   // chunks of like sizes
   const uint64_t chunks = (all + chunk - 1) / chunk;
   p.chunk = (uint32_t)((all / kTile + chunks - 1) / chunks * kTile);
-  const uint32_t tiles = p.q_tiles * ((d + kTile - 1) / kTile), most = (p.chunk + 511) / 512;
-  p.splits = ((kGradTarget + tiles - 1) / tiles + 7) / 8 * 8;
-  if (p.splits > most) p.splits = most;
+  const uint32_t c_tiles = (d + kTile - 1) / kTile, most = (p.chunk + 255) / 256;
+  p.wide = type != ANN_F32 && d % 8 == 0 && nq > kTile && (uint64_t)p.q_tiles * (p.chunk / kTile) >= 2 * kWideSlots;
+  if (p.wide) {
+    // Rounds of workgroups times slices of each (1.3 us: 512 workgroups at 850 TFLOP/s), and the parts written and read at 4 TB/s.
+    const uint32_t tiles = (nq + kWideM - 1) / kWideM * c_tiles, slices = p.chunk / kWideSlice;
+    double least = INFINITY;
+    for (uint32_t s = 1; s <= 64 && s <= most; ++s) {
+      const double cost = 1.3 * (((uint64_t)tiles * s + kWideSlots - 1) / kWideSlots) * ((slices + s - 1) / s) + 2e-6 * s * nq * d;
+      if (cost < least) least = cost, p.splits = s;
+    }
+  } else {
+    const uint32_t tiles = p.q_tiles * c_tiles;
+    p.splits = ((kGradTarget + tiles - 1) / tiles + 7) / 8 * 8;
+    if (p.splits > most) p.splits = most;
+  }
   p.g_at = p.parts.take(p.chunk * row_bytes);
   p.part_at = p.parts.take((uint64_t)p.splits * nq * d * sizeof(float));
+  // (one chunk whose tiles leave compute units with one workgroup or none: runs of queries, of 64 at least)
+  const uint32_t row_tiles = p.chunk / kTile * c_tiles;
+  if (chunks == 1 && row_tiles < 512) {
+    p.row_splits = (kGradTarget + row_tiles - 1) / row_tiles;
+    if (p.row_splits > (nq + 63) / 64) p.row_splits = (nq + 63) / 64;
+    if (p.row_splits > 8) p.row_splits = 8;
+  }
+  if (p.row_splits > 1) p.row_part_at = p.parts.take((uint64_t)p.row_splits * n * d * sizeof(float));
   p.sums_at = p.parts.take((uint64_t)p.q_tiles * 2 * p.chunk * sizeof(float));
   p.scaling_at = p.parts.take(2 * sizeof(float));
   p.rest_at = p.parts.take(nq * sizeof(float));
@@ -556,7 +631,11 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
       run_bias(std::integral_constant<int, 8>());
     ANN_HIP(hipGetLastError());
     if (o.dq) {
-      grad_queries_sum_kernel<T, 128><<<(g.nq + 1) / 2, 256, 0, st>>>(a, part, p.splits, (T *)o.dq, o.dq_stride);
+      // (256 splits of 256 queries: 15.5 us by two wavefronts to a query)
+      if (p.splits >= 64)
+        grad_queries_sum_kernel<T, 128, 8, 1024><<<g.nq, 1024, 0, st>>>(a, part, p.splits, (T *)o.dq, o.dq_stride);
+      else
+        grad_queries_sum_kernel<T, 128, 1, 256><<<(g.nq + 1) / 2, 256, 0, st>>>(a, part, p.splits, (T *)o.dq, o.dq_stride);
       ANN_HIP(hipGetLastError());
     }
     return ANN_OK;
@@ -588,12 +667,30 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
         run_entropy(std::false_type());
       ANN_HIP(hipGetLastError());
       if (o.dq) {
-        grad_queries_kernel<T><<<c_tiles * p.q_tiles * ((p.splits + 7) / 8 * 8), 256, 0, st>>>(g, row0, rows, ld, G, p.splits, part, row0 != 0);
+        const auto product = [&](auto blocks) {
+          constexpr int MB = decltype(blocks)::value;
+          const uint32_t tiles = c_tiles * ((g.nq + MB * 64 - 1) / (MB * 64)) * p.splits;
+          grad_queries_kernel<T, MB><<<(tiles + 7) / 8 * 8, 256, 0, st>>>(g, row0, rows, ld, G, p.splits, part, row0 != 0);
+        };
+        // (biases: rows left out may hold anything, which the wide product does not look for)
+        if (p.wide && !g.bias && wide_operand(g.rows, g.row_stride)) {
+          if constexpr (sizeof(T) == 2) product(std::integral_constant<int, 4>());
+        } else {
+          product(std::integral_constant<int, 2>());
+        }
         ANN_HIP(hipGetLastError());
       }
     }
     if (o.drows) {
-      grad_rows_kernel<T><<<c_tiles * ((ld / kTile + 7) / 8 * 8), 256, 0, st>>>(g, row0, rows, ld, G, (T *)o.drows, o.drows_stride, a.scaling);
+      const uint32_t grid = c_tiles * ((ld / kTile + 7) / 8 * 8);
+      if (p.row_splits > 1) {
+        float *row_part = (float *)(ws + p.row_part_at);
+        grad_rows_kernel<T, true><<<grid * p.row_splits, 256, 0, st>>>(g, row0, rows, ld, G, (T *)o.drows, o.drows_stride, a.scaling, row_part, p.row_splits);
+        ANN_HIP(hipGetLastError());
+        grad_rows_sum_kernel<T><<<(uint32_t)(((uint64_t)rows * g.d + 255) / 256), 256, 0, st>>>(g, row0, rows, row_part, p.row_splits, (T *)o.drows, o.drows_stride, a.scaling);
+      } else {
+        grad_rows_kernel<T, false><<<grid, 256, 0, st>>>(g, row0, rows, ld, G, (T *)o.drows, o.drows_stride, a.scaling, nullptr, 1);
+      }
       ANN_HIP(hipGetLastError());
     }
     if (o.drow_bias) {
@@ -602,7 +699,7 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
     }
   }
   if (o.dq && g.nq) {
-    grad_queries_sum_kernel<T, 256><<<g.nq, 256, 0, st>>>(a, part, g.n ? p.splits : 0, (T *)o.dq, o.dq_stride);
+    grad_queries_sum_kernel<T, 256, 1, 256><<<g.nq, 256, 0, st>>>(a, part, g.n ? p.splits : 0, (T *)o.dq, o.dq_stride);
     ANN_HIP(hipGetLastError());
   }
   return ANN_OK;

@@ -95,18 +95,18 @@ __device__ __forceinline__ uint4 unit_part(Unit<float> &u, int) {
   return __builtin_bit_cast(uint4, h);
 }
 
-template <typename T, Order ORDER>
+template <typename T, Order ORDER, int LINES = kTile>
 struct TileSide {
   typedef Operand16<T> O;
-  static constexpr int kUnits = kTile * O::kSlice / 8 / 256;  // to a lane
-  static constexpr int kPlane = kTile * O::kSlice * 2;        // bytes
+  static constexpr int kUnits = LINES * O::kSlice / 8 / 256;  // to a lane
+  static constexpr int kPlane = LINES * O::kSlice * 2;        // bytes
   static constexpr int kBytes = kPlane * O::kParts;
   Unit<T> u[kUnits];
 
   // Byte offset of 16-byte slot `slot` of line `line` of a plane.
   static __device__ __forceinline__ int slot_at(int line, int slot) {
     if constexpr (ORDER == kAcross)
-      return line * (kTile * 2) + ((slot ^ ((line & 7) << 1)) << 4);  // lines are k: 256 bytes
+      return line * (LINES * 2) + ((slot ^ ((line & 7) << 1)) << 4);  // lines are k
     else if constexpr (O::kSlice == 64)
       return line * 128 + ((slot ^ (line & 7)) << 4);
     else
@@ -121,7 +121,7 @@ struct TileSide {
   __device__ __forceinline__ void start(const Lines<T> &m, uint32_t line0) {
     const uint32_t last = m.lines - 1 - line0;  // (the tile has a line)
     base = (const char *)(m.p + (ORDER == kAlong ? line0 * m.stride : line0));
-    direct = m.stride < (1u << 23) && (ORDER == kAlong || line0 + kTile <= m.lines || m.lines % 8 == 0);
+    direct = m.stride < (1u << 23) && (ORDER == kAlong || line0 + LINES <= m.lines || m.lines % 8 == 0);
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
       const uint32_t at = threadIdx.x + 256 * i;
@@ -130,9 +130,9 @@ struct TileSide {
         line = line < last ? line : last;
         from[i] = (line * (uint32_t)m.stride + at % (O::kSlice / 8) * 8) * sizeof(T);
       } else {
-        uint32_t line = at % (kTile / 8) * 8;
+        uint32_t line = at % (LINES / 8) * 8;
         line = line < last ? line : last / 8 * 8;
-        from[i] = (at / (kTile / 8) * (uint32_t)m.stride + line) * sizeof(T);
+        from[i] = (at / (LINES / 8) * (uint32_t)m.stride + line) * sizeof(T);
       }
     }
   }
@@ -150,7 +150,7 @@ struct TileSide {
         const uint32_t line = line0 + at / (O::kSlice / 8), k = k0 + at % (O::kSlice / 8) * 8;
         load_unit(u[i], m.p + line * m.stride + k, line < m.lines ? (int64_t)m.depth - k : 0);
       } else {
-        const uint32_t k = k0 + at / (kTile / 8), line = line0 + at % (kTile / 8) * 8;
+        const uint32_t k = k0 + at / (LINES / 8), line = line0 + at % (LINES / 8) * 8;
         load_unit(u[i], m.p + k * m.stride + line, k < m.depth && !(m.bias && m.bias[k] == -INFINITY) ? (int64_t)m.lines - line : 0);
       }
     }
@@ -159,7 +159,7 @@ struct TileSide {
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
       const int at = (int)threadIdx.x + 256 * i;
-      const int line = ORDER == kAlong ? at / (O::kSlice / 8) : at / (kTile / 8), slot = ORDER == kAlong ? at % (O::kSlice / 8) : at % (kTile / 8);
+      const int line = ORDER == kAlong ? at / (O::kSlice / 8) : at / (LINES / 8), slot = ORDER == kAlong ? at % (O::kSlice / 8) : at % (LINES / 8);
 #pragma unroll
       for (int p = 0; p < O::kParts; ++p) *(uint4 *)(lds + p * kPlane + slot_at(line, slot)) = unit_part(u[i], p);
     }
@@ -216,9 +216,12 @@ __device__ __forceinline__ void tile_product(f32x16 (&acc)[2][2], const Lines<T>
     for (int kk = 0; kk < O::kSlice / 16; ++kk) {
       typename O::E fa[O::kParts][2], fb[O::kParts][2];
 #pragma unroll
-      for (int p = 0; p < O::kParts; ++p)
+      for (int p = 0; p < O::kParts; ++p) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) fa[p][i] = SA::fragment(lds, p, mw + i, kk), fb[p][i] = SB::fragment(lb, p, nw + i, kk);
+        for (int i = 0; i < 2; ++i) fa[p][i] = SA::fragment(lds, p, mw + i, kk);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) fb[p][j] = SB::fragment(lb, p, nw + j, kk);
+      }
 #pragma unroll
       for (int sum = O::kParts - 1; sum >= 0; --sum)  // the smallest products first
 #pragma unroll
@@ -229,6 +232,159 @@ __device__ __forceinline__ void tile_product(f32x16 (&acc)[2][2], const Lines<T>
             for (int j = 0; j < 2; ++j) acc[i][j] = matrix_step(fa[p][i], fb[sum - p][j], acc[i][j]);
     }
   }
+}
+
+// Products of 256 x 128 tiles of 16-bit elements for operands whose addresses and strides are multiples of 16 bytes: 128 x 64 of
+// the tile to a wavefront (a 64 x 64 share reads LDS for twice the cycles that the matrix cores take).  Slices of 32 k go from
+// memory straight into one of three buffers of LDS, two slices ahead (one ahead, the product waited for memory: each slice has lines that
+// the L2 does not hold), and fragments are read beside the products of the ones before.  Two such workgroups share a
+// compute unit: the end of one's tile lies beside the other's product.
+constexpr int kWideM = 256, kWideN = 128, kWideSlice = 32;
+constexpr int kWideBuffer = (kWideM + kWideN) * kWideSlice * 2;
+
+inline bool wide_operand(const void *p, uint64_t stride) { return (uintptr_t)p % 16 == 0 && stride % 8 == 0 && stride < (1u << 23); }
+
+// kAlong: the depth is a multiple of 32; kAcross: the number of lines is one of 8, and lines of k behind the last are read as the last
+// (the other operand is zero there).
+template <typename T, Order ORDER, int LINES>
+struct WideSide {
+  typedef typename Operand16<T>::E E;
+  static constexpr int kUnits = LINES * kWideSlice / 8 / 256;
+  static constexpr int kBytes = LINES * kWideSlice * 2;
+  static constexpr int kSlots = ORDER == kAlong ? kWideSlice / 8 : LINES / 8;  // of 16 bytes to a line of LDS
+  // A unit's place in LDS is its number; the slot in memory that it holds is permuted with its line.
+  static __device__ __forceinline__ int permuted(int line, int slot) { return ORDER == kAlong ? slot ^ ((line >> 1) & 3) : slot ^ ((line & 7) << 1); }
+  const char *base;
+  uint32_t from[kUnits];
+  __device__ __forceinline__ void start(const Lines<T> &m, uint32_t line0) {
+    const uint32_t last = m.lines - 1 - line0;  // (lines that do not exist are read as one that does)
+    base = (const char *)(m.p + (ORDER == kAlong ? line0 * m.stride : line0));
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+      const int at = (int)threadIdx.x + 256 * i, along = at / kSlots, slot = permuted(along, at % kSlots);
+      if constexpr (ORDER == kAlong) {
+        const uint32_t line = (uint32_t)along < last ? (uint32_t)along : last;
+        from[i] = (line * (uint32_t)m.stride + slot * 8) * sizeof(T);
+      } else {
+        const uint32_t line = (uint32_t)slot * 8 < last ? (uint32_t)slot * 8 : last / 8 * 8;
+        from[i] = (along * (uint32_t)m.stride + line) * sizeof(T);
+      }
+    }
+  }
+  __device__ __forceinline__ void fetch(const Lines<T> &m, uint32_t k0, char *lds) {
+    typedef const __attribute__((address_space(1))) void *From;
+    typedef __attribute__((address_space(3))) void *To;
+    const char *p = base + (ORDER == kAlong ? (uint64_t)k0 : k0 * m.stride) * sizeof(T);
+    if (ORDER == kAcross && k0 + kWideSlice > m.depth) {
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) {
+        const uint32_t k = k0 + (threadIdx.x + 256 * i) / kSlots;
+        if (k >= m.depth) from[i] -= (k - (m.depth - 1)) * (uint32_t)m.stride * sizeof(T);  // (the last slice: from is not used again)
+      }
+    }
+    char *to = lds + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * (kWave * 16);
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) __builtin_amdgcn_global_load_lds((From)(p + from[i]), (To)(to + i * 4096), 16, 0, 0);
+  }
+  // Eight k of one line (k = 16 kk + 8 (lane / 32) .., line = 32 block + lane % 32).
+  static __device__ __forceinline__ E fragment(const char *lds, int block, int kk) {
+    const int lane = lane_id();
+    if constexpr (ORDER == kAlong) {
+      return *(const E *)(lds + (block * 32 + lane % 32) * (kSlots * 16) + (permuted(lane % 32, kk * 2 + lane / 32) << 4));
+    } else {
+      union {
+        s16x4 half[2];
+        E e;
+      } f;
+      const int line = block * 32 + lane / 16 % 2 * 16 + lane % 4 * 4;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int k = kk * 16 + lane / 32 * 8 + h * 4 + lane % 16 / 4;
+        f.half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) s16x4 *)(lds + k * (kSlots * 16) + (permuted(k, line / 8) << 4) + line % 8 * 2));
+      }
+      return f.e;
+    }
+  }
+};
+
+// Waits until at most `on_their_way` of the lane's reads into LDS (0 or a slice's) are outstanding and its own reads of LDS are done, then for
+// the other wavefronts.
+template <int ON_THEIR_WAY>
+__device__ __forceinline__ void wide_barrier() {
+  static_assert(ON_THEIR_WAY < 16, "");
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070 | ON_THEIR_WAY);  // vmcnt(ON_THEIR_WAY) lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// acc[i][j]: 32 x 32 block (m block 4 (wave / 2) + i, n block 2 (wave % 2) + j).  k_begin and the depths: see WideSide.  The three
+// buffers of kWideBuffer bytes are variables of their own (so that the compiler can tell reads of one from what is on its way into
+// another) and free when the call begins after a barrier.  All 256 lanes take part.
+template <typename T, Order OA, Order OB>
+__device__ __forceinline__ void wide_product(f32x16 (&acc)[4][2], const Lines<T> &A, uint32_t m0, const Lines<T> &B, uint32_t n0, uint32_t k_begin,
+                                             uint32_t k_end, char *lds0, char *lds1, char *lds2) {
+  typedef WideSide<T, OA, kWideM> SA;
+  typedef WideSide<T, OB, kWideN> SB;
+  typedef typename Operand16<T>::E E;
+  constexpr int kInFlight = SA::kUnits + SB::kUnits;
+  if (k_begin >= k_end) return;
+  SA a;
+  SB b;
+  a.start(A, m0), b.start(B, n0);
+  const int mw = (int)(threadIdx.x / kWave) / 2 * 4, nw = (int)(threadIdx.x / kWave) % 2 * 2;
+  const uint32_t slices = (k_end - k_begin + kWideSlice - 1) / kWideSlice;
+  const auto fetch = [&](uint32_t s, char *to) { a.fetch(A, k_begin + s * kWideSlice, to), b.fetch(B, k_begin + s * kWideSlice, to + SA::kBytes); };
+  E fa[2][4], fb[2][2];  // of the first and the second 16 k of a slice
+  const auto read = [&](const char *at, int kk) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) fa[kk][i] = SA::fragment(at, mw + i, kk);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) fb[kk][j] = SB::fragment(at + SA::kBytes, nw + j, kk);
+  };
+  const auto multiply = [&](int kk) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) acc[i][j] = matrix_step(fa[kk][i], fb[kk][j], acc[i][j]);
+  };
+  __syncthreads();  // the last readers of the buffers are done
+  fetch(0, lds0);
+  if (slices > 1) fetch(1, lds1);
+  if (slices > 2) fetch(2, lds2);
+  if (slices > 2)
+    wide_barrier<2 * kInFlight>();
+  else
+    wide_barrier<0>();
+  read(lds0, 0);
+  // Slice s, whose first fragments have been read.
+  const auto step = [&](uint32_t s, char *now, const char *next) {
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the first fragments, before more are asked for that need not be waited for
+    read(now, 1);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(0);
+    // slice s + 1 is there, and slice s is in all wavefronts' registers
+    if (s + 2 < slices)
+      wide_barrier<kInFlight>();
+    else
+      wide_barrier<0>();
+    read(next, 0);  // (behind the last slice: whatever is there, not used)
+    if (s + 3 < slices) fetch(s + 3, now);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(1);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  uint32_t s = 0;
+  for (; s + 3 <= slices; s += 3) {
+    step(s, lds0, lds1);
+    step(s + 1, lds1, lds2);
+    step(s + 2, lds2, lds0);
+  }
+  if (s < slices) step(s, lds0, lds1);
+  if (s + 1 < slices) step(s + 1, lds1, lds2);
 }
 
 template <int M, int N>
