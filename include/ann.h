@@ -541,7 +541,7 @@ uint64_t ann_layer_norm_backward_workspace(uint64_t n, uint32_t dim);
  * The scores of nq queries against n rows, s[i][j] = scale * <q_i, x_j> + bias_j.
  * They are never stored: the calls below take them as they are computed.
  *   q, rows    [nq], [n] rows of d elements of `type` with their strides;
- *              d <= ANN_MAX_SCORE_DIM, n and nq < 2^31.
+ *              d <= ANN_MAX_SCORE_DIM, n <= 2^31 - 256, nq < 2^24.
  *   scale      an inverse temperature; finite.
  *   row_bias   [n] fp32, NULL allowed: zeros.  A row whose bias is -infinity is left
  *              out of every query's softmax, whatever its elements hold.  (Squared
@@ -598,7 +598,10 @@ uint64_t ann_row_logprobs_workspace(uint32_t nq, uint64_t n, uint32_t d, uint32_
  * only); dq, drows (of `type`, with their strides) and drow_bias ([n] fp32) each may be NULL where not wanted.
  * G is rounded to 16 bits before its products with 16-bit rows and queries (bf16: to
  * bf16; f16: to f16 after a power of two that brings the largest weight to
- * 2^13 .. 2^14), and taken as three bf16 parts with fp32 ones; drow_bias sums it in fp32.
+ * 2^13 .. 2^14), and taken as three bf16 parts with fp32 ones; drow_bias sums it in fp32.  What that
+ * rounding leaves of the given rows' elements, and in drows of all elements where queries are few, is added.
+ * A score and lse of the size of a mask (1e6 and more) leave nothing of their difference's
+ * small part in fp32: probabilities among such scores alone (no other row left) are not those of the forward pass.
  * Queries without a given row take no part with their g_logprob; rows left out get
  * zero.  A query whose lse is -infinity (no row left) gets zero.
  * Errors as ann_row_logprobs.

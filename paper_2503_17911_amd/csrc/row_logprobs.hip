@@ -1124,7 +1124,7 @@ ann_status check_scores(const char *what, const ann_row_scores *s) {
   if (s->type > ANN_BF16) return fail(ANN_EINVAL, "%s: unknown type %u", what, s->type);
   if (s->d == 0) return fail(ANN_EINVAL, "%s: d == 0", what);
   if (s->d > ANN_MAX_SCORE_DIM) return fail(ANN_ECAPACITY, "%s: d = %u exceeds ANN_MAX_SCORE_DIM = %u", what, s->d, ANN_MAX_SCORE_DIM);
-  if (s->n >= (1ull << 31) || s->nq >= (1u << 31)) return fail(ANN_ECAPACITY, "%s: n and nq must be below 2^31", what);
+  if (s->n > kMaxRows || s->nq >= kMaxQueries) return fail(ANN_ECAPACITY, "%s: n must be at most 2^31 - 256 and nq below 2^24", what);
   if (!(fabsf(s->scale) < INFINITY)) return fail(ANN_EINVAL, "%s: scale must be finite", what);
   if (s->nq && (!s->q || s->q_stride < s->d)) return fail(ANN_EINVAL, "%s: q is NULL or its stride shorter than a row", what);
   if (s->n && (!s->rows || s->row_stride < s->d)) return fail(ANN_EINVAL, "%s: rows is NULL or its stride shorter than a row", what);
@@ -1144,7 +1144,7 @@ ann_status check_workspace(const char *what, const void *workspace, uint64_t byt
 using namespace ann;
 
 extern "C" uint64_t ann_row_logprobs_workspace(uint32_t nq, uint64_t n, uint32_t d, uint32_t type, uint32_t k) {
-  if (n >= (1ull << 31) || nq >= (1u << 31) || k > ANN_MAX_ALTERNATIVES) return 0;
+  if (n > kMaxRows || nq >= kMaxQueries || k > ANN_MAX_ALTERNATIVES) return 0;
   return forward_plan(nq, n, d, type, k).parts.bytes;
 }
 

@@ -6,6 +6,10 @@ namespace ann {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 
+// A launch has fewer than 2^32 lanes: 256 to a query, two to a row.
+constexpr uint64_t kMaxRows = (1ull << 31) - 256;
+constexpr uint32_t kMaxQueries = 1u << 24;
+
 // s[i][j] = scale <q_i, rows_j> + bias_j
 struct ScoreTable {
   const void *q, *rows;

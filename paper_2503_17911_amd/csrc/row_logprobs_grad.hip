@@ -17,6 +17,9 @@
 // is formed as g (1 - p) in fp32 before it is rounded: apart, g x_t and g p x_t would cancel.
 // What its rounding leaves goes to dq in fp32: that element outweighs all others
 // and rows of a cluster are alike, so that dq, their difference, erred by 0.6 % (bf16) with it, 0.17 % is the rounding of dq.
+// The rows' gradient has few terms that count, often the given row's one alone: G's rounding would add to the result's (0.24 % instead of
+// 0.17 % in bf16).  So what it leaves is taken along: where queries are few (kFewQueries) of every element, in 16 bits more, otherwise of the
+// given rows' elements.
 #include "row_logprobs.hpp"
 
 #include <math.h>
@@ -30,6 +33,8 @@ constexpr uint32_t kWideSlots = 512;            // of a wide one: two
 // Wavefronts to a SIMD of the gradients' products (three instead of two: 303 -> 237 and 282 -> 255 us with 2,048 x 50,000 x 768).
 template <typename T>
 constexpr int kGradWaves = sizeof(T) == 2 ? 3 : 2;
+
+constexpr uint32_t kFewQueries = 256;  // up to so many, the rows' gradient takes all of G's remainders
 
 struct GradArgs {
   ScoreTable g;
@@ -64,7 +69,7 @@ __global__ __launch_bounds__(1024) void grad_scaling_kernel(GradArgs a, float *_
 // four rows of one query.  BIAS: biases and rows left out.  SUMS: row_sums[2 q_tile + half][ld] gets sums over 64 queries.
 template <typename T, bool BIAS, bool ENTROPY, bool SUMS>
 __global__ __launch_bounds__(256) void grad_scores_kernel(GradArgs a, uint32_t row0, uint32_t q_tiles, uint32_t ld, T *__restrict__ G,
-                                                          float *__restrict__ row_sums) {
+                                                          T *__restrict__ rests, float *__restrict__ row_sums) {
   __shared__ __attribute__((aligned(16))) char lds[kTileBytes<T, kAlong, kAlong>];
   __shared__ float row_bias[kTile];
   const ScoreTable &g = a.g;
@@ -109,13 +114,15 @@ __global__ __launch_bounds__(256) void grad_scores_kernel(GradArgs a, uint32_t r
         T *out = G + (uint64_t)q * ld + rt * kTile + mw + i * 32 + lane / 32 * 4;
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
-          Piece<T, 4> o;
+          Piece<T, 4> o, left;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             o.v[e] = from_f32<T>(acc[i][j][r + e] * scaling);
+            if (sizeof(T) == 2 && rests) left.v[e] = from_f32<T>(__builtin_fmaf(acc[i][j][r + e], scaling, -to_f32(o.v[e])));
             if (sizeof(T) == 2 && (uint32_t)(i * 32 + block_row(r + e)) == hit) a.rest[q] = __builtin_fmaf(acc[i][j][r + e], scaling, -to_f32(o.v[e]));
           }
           *(Piece<T, 4> *)(out + r * 2) = o;
+          if (sizeof(T) == 2 && rests) *(Piece<T, 4> *)(rests + (out - G) + r * 2) = left;
         }
       }
     }
@@ -229,9 +236,11 @@ __global__ __launch_bounds__(THREADS) void grad_queries_sum_kernel(GradArgs a, c
 }
 
 // drows[row0 + j][c] = scale sum over the queries of G[q][j] q[q][c].  SPLIT: part[split][row][c] instead, of a split's queries.
-template <typename T, bool SPLIT>
-__global__ __launch_bounds__(256, kGradWaves<T>) void grad_rows_kernel(ScoreTable g, uint32_t row0, uint32_t rows, uint32_t ld, const T *__restrict__ G, T *__restrict__ out,
-                                                        uint64_t stride, const float *__restrict__ scaling, float *__restrict__ part, uint32_t splits) {
+// RESTS: also of what G's rounding left; else what that of the given rows' elements did.
+template <typename T, bool SPLIT, bool RESTS>
+__global__ __launch_bounds__(256, RESTS ? 2 : kGradWaves<T>) void grad_rows_kernel(GradArgs a, uint32_t row0, uint32_t rows, uint32_t ld, const T *__restrict__ G, const T *__restrict__ rests,
+                                                        T *__restrict__ out, uint64_t stride, float *__restrict__ part, uint32_t splits) {
+  const ScoreTable &g = a.g;
   __shared__ __attribute__((aligned(16))) char lds[kTileBytes<T, kAcross, kAcross>];
   const uint32_t c_tiles = (g.d + kTile - 1) / kTile, b8 = blockIdx.x / 8, split = SPLIT ? b8 % splits : 0, at = SPLIT ? b8 / splits : b8;
   const uint32_t ct = at % c_tiles, rt = at / c_tiles * 8 + blockIdx.x % 8;
@@ -247,8 +256,49 @@ __global__ __launch_bounds__(256, kGradWaves<T>) void grad_rows_kernel(ScoreTabl
   f32x16 acc[2][2];
   clear(acc);
   tile_product<T, kAcross, kAcross>(acc, A, rt * kTile, B, ct * kTile, begin, end, lds);
+  if constexpr (RESTS) {
+    const Lines<T> R = {rests, ld, ld, g.nq};
+    tile_product<T, kAcross, kAcross>(acc, R, rt * kTile, B, ct * kTile, begin, end, lds);
+  }
   const int wave = (int)threadIdx.x / kWave, lane = lane_id();
-  const float by = scaling ? g.scale * scaling[1] : g.scale;
+  if constexpr (sizeof(T) == 2) {
+    if (!RESTS && a.targets) {
+      // the queries whose given row is one of the tile's, in their order, 256 at a time
+      uint32_t *list = (uint32_t *)lds;  // [256] queries, [256] rows of the tile, [4] counts
+      const uint32_t tile0 = row0 + rt * kTile;
+      for (uint32_t q0 = begin; q0 < end; q0 += 256) {
+        const uint32_t q = q0 + threadIdx.x, at = (q < end ? a.targets[q] : ANN_PAD_ID) - tile0;
+        const bool mine = at < kTile && tile0 + at < g.n && !(g.bias && g.bias[tile0 + at] == -INFINITY);
+        const uint64_t of_wave = __ballot(mine);
+        __syncthreads();  // the list has been read
+        if (lane == 0) list[512 + wave] = __popcll(of_wave);
+        __syncthreads();
+        uint32_t place = __popcll(of_wave & ((1ull << lane) - 1)), count = 0;
+        for (int w = 0; w < 4; ++w) {
+          if (w < wave) place += list[512 + w];
+          count += list[512 + w];
+        }
+        if (mine) list[place] = q, list[256 + place] = at;
+        __syncthreads();
+        for (uint32_t k = 0; k < count; ++k) {
+          const uint32_t of = list[k], row = list[256 + k];
+          if (row / 64 != (uint32_t)wave / 2) continue;
+          const float rest = a.rest[of];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t c = ct * kTile + wave % 2 * 64 + j * 32 + lane % 32;
+            const float v = c < g.d ? to_f32(((const T *)g.q)[of * g.q_stride + c]) : 0.0f;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int r = 0; r < 16; ++r)
+                if (row % 64 == (uint32_t)(i * 32 + block_row(r))) acc[i][j][r] = __builtin_fmaf(rest, v, acc[i][j][r]);
+          }
+        }
+      }
+    }
+  }
+  const float by = a.scaling ? g.scale * a.scaling[1] : g.scale;
 #pragma unroll
   for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -478,21 +528,29 @@ __global__ __launch_bounds__(256, 2) void grad_short_kernel(GradArgs a, uint32_t
           if (hit == (uint32_t)block_row(r) && target < g.n) a.rest[mine] = s[r] - to_f32((T)G[r / 8][r % 8]);
       }
       // lines 16 t + 4 (lane / 32) + 0 .. 3 and 8 further are the lane's eight k of step t
+      const auto multiply = [&](const E(&by)[2]) {
 #pragma unroll
-      for (int b = 0; b < KS / 2; ++b)
+        for (int b = 0; b < KS / 2; ++b)
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          union {
-            s16x4 part[2];
-            E e;
-          } f;
+          for (int t = 0; t < 2; ++t) {
+            union {
+              s16x4 part[2];
+              E e;
+            } f;
 #pragma unroll
-          for (int p = 0; p < 2; ++p) {
-            const int l = half * 32 + t * 16 + p * 8 + lane / 32 * 4 + lane % 16 / 4, column = b * 32 + lane / 16 % 2 * 16 + lane % 4 * 4;
-            f.part[p] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at + l * kLine + column * 2));
+            for (int p = 0; p < 2; ++p) {
+              const int l = half * 32 + t * 16 + p * 8 + lane / 32 * 4 + lane % 16 / 4, column = b * 32 + lane / 16 % 2 * 16 + lane % 4 * 4;
+              f.part[p] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at + l * kLine + column * 2));
+            }
+            acc[b] = matrix_step(by[t], f.e, acc[b]);
           }
-          acc[b] = matrix_step(G[t], f.e, acc[b]);
-        }
+      };
+      multiply(G);
+      if (OWN_ROWS && (hits || g.nq <= kFewQueries)) {  // what the rounding left, in 16 bits more
+#pragma unroll
+        for (int r = 0; r < 16; ++r) G[r / 8][r % 8] = from_f32<T>(s[r] - to_f32((T)G[r / 8][r % 8]));
+        multiply(G);
+      }
     }
   }
   if (OWN_ROWS && drow_bias) {
@@ -525,7 +583,7 @@ struct BackwardPlan {
   uint32_t row_splits = 1;                      // of the queries, in the rows' product
   int slices = 0;                               // of 16 columns, if G stays in registers
   bool wide = false;                            // the queries' product: tiles of 256 of them
-  uint64_t g_at = 0, part_at = 0, row_part_at = 0, sums_at = 0, scaling_at = 0, rest_at = 0;
+  uint64_t g_at = 0, rests_at = 0, part_at = 0, row_part_at = 0, sums_at = 0, scaling_at = 0, rest_at = 0;
   Parts parts;
 };
 
@@ -565,6 +623,7 @@ static BackwardPlan backward_plan(uint32_t nq, uint64_t n, uint32_t d, uint32_t 
     if (p.splits > most) p.splits = most;
   }
   p.g_at = p.parts.take(p.chunk * row_bytes);
+  if (type != ANN_F32 && nq <= kFewQueries) p.rests_at = p.parts.take(p.chunk * row_bytes);
   p.part_at = p.parts.take((uint64_t)p.splits * nq * d * sizeof(float));
   // (one chunk whose tiles leave compute units with one workgroup or none: runs of queries, of 64 at least)
   const uint32_t row_tiles = p.chunk / kTile * c_tiles;
@@ -591,7 +650,7 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
   GradArgs a = args;
   const ScoreTable &g = a.g;
   const uint32_t c_tiles = (g.d + kTile - 1) / kTile;
-  T *G = (T *)(ws + p.g_at);
+  T *G = (T *)(ws + p.g_at), *rests = sizeof(T) == 2 && g.nq && g.nq <= kFewQueries && o.drows ? (T *)(ws + p.rests_at) : nullptr;
   float *part = (float *)(ws + p.part_at), *sums = (float *)(ws + p.sums_at);
   a.rest = (float *)(ws + p.rest_at);
   if (sizeof(T) == 2 && std::is_same<T, f16_t>::value && g.nq && g.n) {
@@ -647,7 +706,7 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
     if (g.nq) {
       const uint32_t grid = p.q_tiles * ((ld / kTile + 7) / 8 * 8);
       const auto run = [&](auto bias, auto entropy, auto row_sums) {
-        grad_scores_kernel<T, decltype(bias)::value, decltype(entropy)::value, decltype(row_sums)::value><<<grid, 256, 0, st>>>(a, row0, p.q_tiles, ld, G, sums);
+        grad_scores_kernel<T, decltype(bias)::value, decltype(entropy)::value, decltype(row_sums)::value><<<grid, 256, 0, st>>>(a, row0, p.q_tiles, ld, G, rests, sums);
       };
       const auto run_sums = [&](auto bias, auto entropy) {
         if (o.drow_bias)
@@ -682,14 +741,24 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
       }
     }
     if (o.drows) {
-      const uint32_t grid = c_tiles * ((ld / kTile + 7) / 8 * 8);
+      const uint32_t grid = c_tiles * ((ld / kTile + 7) / 8 * 8) * p.row_splits;
+      float *row_part = (float *)(ws + p.row_part_at);
+      const auto product = [&](auto split, auto with_rests) {
+        grad_rows_kernel<T, decltype(split)::value, decltype(with_rests)::value>
+            <<<grid, 256, 0, st>>>(a, row0, rows, ld, G, rests, (T *)o.drows, o.drows_stride, row_part, p.row_splits);
+      };
+      const auto with_split = [&](auto split) {
+        if (sizeof(T) == 2 && rests)
+          product(split, std::integral_constant<bool, sizeof(T) == 2>());
+        else
+          product(split, std::false_type());
+      };
       if (p.row_splits > 1) {
-        float *row_part = (float *)(ws + p.row_part_at);
-        grad_rows_kernel<T, true><<<grid * p.row_splits, 256, 0, st>>>(g, row0, rows, ld, G, (T *)o.drows, o.drows_stride, a.scaling, row_part, p.row_splits);
+        with_split(std::true_type());
         ANN_HIP(hipGetLastError());
         grad_rows_sum_kernel<T><<<(uint32_t)(((uint64_t)rows * g.d + 255) / 256), 256, 0, st>>>(g, row0, rows, row_part, p.row_splits, (T *)o.drows, o.drows_stride, a.scaling);
       } else {
-        grad_rows_kernel<T, false><<<grid, 256, 0, st>>>(g, row0, rows, ld, G, (T *)o.drows, o.drows_stride, a.scaling, nullptr, 1);
+        with_split(std::false_type());
       }
       ANN_HIP(hipGetLastError());
     }
@@ -710,7 +779,7 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
 using namespace ann;
 
 extern "C" uint64_t ann_row_logprobs_backward_workspace(uint32_t nq, uint64_t n, uint32_t d, uint32_t type) {
-  if (n >= (1ull << 31) || nq >= (1u << 31) || d == 0 || type > ANN_BF16) return 0;
+  if (n > kMaxRows || nq >= kMaxQueries || d == 0 || type > ANN_BF16) return 0;
   return backward_plan(nq, n, d, type).parts.bytes;
 }
 
