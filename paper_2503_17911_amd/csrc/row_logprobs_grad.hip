@@ -82,7 +82,7 @@ __global__ __launch_bounds__(256) void grad_scores_kernel(GradArgs a, uint32_t r
   if (threadIdx.x < kTile) row_bias[threadIdx.x] = first + threadIdx.x < g.n ? (BIAS ? g.bias[first + threadIdx.x] : 0.0f) : -INFINITY;
   f32x16 acc[2][2];
   clear(acc);
-  tile_product<T, kAlong, kAlong>(acc, X, first, Q, qt * kTile, 0, g.d, lds);  // (its barriers stand between row_bias and its use)
+  tile_product<T, kAlong, kAlong, sizeof(T) == 4>(acc, X, first, Q, qt * kTile, 0, g.d, lds);  // (its barriers stand between row_bias and its use)
   const bool whole = first + kTile <= g.n;
   const float scaling = sizeof(T) == 2 && a.scaling ? a.scaling[0] : 1.0f;
 #pragma unroll

@@ -95,18 +95,18 @@ __device__ __forceinline__ uint4 unit_part(Unit<float> &u, int) {
   return __builtin_bit_cast(uint4, h);
 }
 
-template <typename T, Order ORDER, int LINES = kTile>
+template <typename T, Order ORDER>
 struct TileSide {
   typedef Operand16<T> O;
-  static constexpr int kUnits = LINES * O::kSlice / 8 / 256;  // to a lane
-  static constexpr int kPlane = LINES * O::kSlice * 2;        // bytes
+  static constexpr int kUnits = kTile * O::kSlice / 8 / 256;  // to a lane
+  static constexpr int kPlane = kTile * O::kSlice * 2;        // bytes
   static constexpr int kBytes = kPlane * O::kParts;
   Unit<T> u[kUnits];
 
   // Byte offset of 16-byte slot `slot` of line `line` of a plane.
   static __device__ __forceinline__ int slot_at(int line, int slot) {
     if constexpr (ORDER == kAcross)
-      return line * (LINES * 2) + ((slot ^ ((line & 7) << 1)) << 4);  // lines are k
+      return line * (kTile * 2) + ((slot ^ ((line & 7) << 1)) << 4);  // lines are k: 256 bytes
     else if constexpr (O::kSlice == 64)
       return line * 128 + ((slot ^ (line & 7)) << 4);
     else
@@ -121,7 +121,7 @@ struct TileSide {
   __device__ __forceinline__ void start(const Lines<T> &m, uint32_t line0) {
     const uint32_t last = m.lines - 1 - line0;  // (the tile has a line)
     base = (const char *)(m.p + (ORDER == kAlong ? line0 * m.stride : line0));
-    direct = m.stride < (1u << 23) && (ORDER == kAlong || line0 + LINES <= m.lines || m.lines % 8 == 0);
+    direct = m.stride < (1u << 23) && (ORDER == kAlong || line0 + kTile <= m.lines || m.lines % 8 == 0);
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
       const uint32_t at = threadIdx.x + 256 * i;
@@ -130,9 +130,9 @@ struct TileSide {
         line = line < last ? line : last;
         from[i] = (line * (uint32_t)m.stride + at % (O::kSlice / 8) * 8) * sizeof(T);
       } else {
-        uint32_t line = at % (LINES / 8) * 8;
+        uint32_t line = at % (kTile / 8) * 8;
         line = line < last ? line : last / 8 * 8;
-        from[i] = (at / (LINES / 8) * (uint32_t)m.stride + line) * sizeof(T);
+        from[i] = (at / (kTile / 8) * (uint32_t)m.stride + line) * sizeof(T);
       }
     }
   }
@@ -150,7 +150,7 @@ struct TileSide {
         const uint32_t line = line0 + at / (O::kSlice / 8), k = k0 + at % (O::kSlice / 8) * 8;
         load_unit(u[i], m.p + line * m.stride + k, line < m.lines ? (int64_t)m.depth - k : 0);
       } else {
-        const uint32_t k = k0 + at / (LINES / 8), line = line0 + at % (LINES / 8) * 8;
+        const uint32_t k = k0 + at / (kTile / 8), line = line0 + at % (kTile / 8) * 8;
         load_unit(u[i], m.p + k * m.stride + line, k < m.depth && !(m.bias && m.bias[k] == -INFINITY) ? (int64_t)m.lines - line : 0);
       }
     }
@@ -159,7 +159,7 @@ struct TileSide {
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
       const int at = (int)threadIdx.x + 256 * i;
-      const int line = ORDER == kAlong ? at / (O::kSlice / 8) : at / (LINES / 8), slot = ORDER == kAlong ? at % (O::kSlice / 8) : at % (LINES / 8);
+      const int line = ORDER == kAlong ? at / (O::kSlice / 8) : at / (kTile / 8), slot = ORDER == kAlong ? at % (O::kSlice / 8) : at % (kTile / 8);
 #pragma unroll
       for (int p = 0; p < O::kParts; ++p) *(uint4 *)(lds + p * kPlane + slot_at(line, slot)) = unit_part(u[i], p);
     }
@@ -191,10 +191,21 @@ struct TileSide {
 template <typename T, Order OA, Order OB>
 constexpr int kTileBytes = TileSide<T, OA>::kBytes + TileSide<T, OB>::kBytes;
 
+template <int M, int N>
+__device__ __forceinline__ void clear(f32x16 (&acc)[M][N]) {
+#pragma unroll
+  for (int i = 0; i < M; ++i)
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+}
+
 // acc[i][j]: 32 x 32 block (m block 2 (wave / 2) + i, n block 2 (wave % 2) + j).  Lane l
 // holds column n = l % 32 and rows m = 8 (r / 4) + 4 (l / 32) + r % 4, r = 0 .. 15.
 // All 256 lanes take part; lds: kTileBytes bytes, free when the call begins after a barrier.
-template <typename T, Order OA, Order OB>
+// APART (fp32): the five smaller products of parts are summed by themselves, so that the sum rounds once per 16 k and not six times.
+template <typename T, Order OA, Order OB, bool APART = false>
 __device__ __forceinline__ void tile_product(f32x16 (&acc)[2][2], const Lines<T> &A, uint32_t m0, const Lines<T> &B, uint32_t n0,
                                              uint32_t k_begin, uint32_t k_end, char *lds) {
   typedef Operand16<T> O;
@@ -204,6 +215,8 @@ __device__ __forceinline__ void tile_product(f32x16 (&acc)[2][2], const Lines<T>
   SA a;
   SB b;
   const int mw = (int)(threadIdx.x / kWave) / 2 * 2, nw = (int)(threadIdx.x / kWave) % 2 * 2;
+  f32x16 low[2][2];
+  if constexpr (APART) clear(low);
   a.start(A, m0), b.start(B, n0);
   if (k_begin < k_end) a.fetch(A, m0, k_begin), b.fetch(B, n0, k_begin);
   for (uint32_t k = k_begin; k < k_end; k += O::kSlice) {
@@ -216,12 +229,9 @@ __device__ __forceinline__ void tile_product(f32x16 (&acc)[2][2], const Lines<T>
     for (int kk = 0; kk < O::kSlice / 16; ++kk) {
       typename O::E fa[O::kParts][2], fb[O::kParts][2];
 #pragma unroll
-      for (int p = 0; p < O::kParts; ++p) {
+      for (int p = 0; p < O::kParts; ++p)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) fa[p][i] = SA::fragment(lds, p, mw + i, kk);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) fb[p][j] = SB::fragment(lb, p, nw + j, kk);
-      }
+        for (int i = 0; i < 2; ++i) fa[p][i] = SA::fragment(lds, p, mw + i, kk), fb[p][i] = SB::fragment(lb, p, nw + i, kk);
 #pragma unroll
       for (int sum = O::kParts - 1; sum >= 0; --sum)  // the smallest products first
 #pragma unroll
@@ -229,8 +239,19 @@ __device__ __forceinline__ void tile_product(f32x16 (&acc)[2][2], const Lines<T>
 #pragma unroll
           for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) acc[i][j] = matrix_step(fa[p][i], fb[sum - p][j], acc[i][j]);
+            for (int j = 0; j < 2; ++j) {
+              f32x16 &to = APART && sum != 0 ? low[i][j] : acc[i][j];
+              to = matrix_step(fa[p][i], fb[sum - p][j], to);
+            }
     }
+  }
+  if constexpr (APART) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] += low[i][j][r];
   }
 }
 
@@ -238,7 +259,8 @@ __device__ __forceinline__ void tile_product(f32x16 (&acc)[2][2], const Lines<T>
 // the tile to a wavefront (a 64 x 64 share reads LDS for twice the cycles that the matrix cores take).  Slices of 32 k go from
 // memory straight into one of three buffers of LDS, two slices ahead (one ahead, the product waited for memory: each slice has lines that
 // the L2 does not hold), and fragments are read beside the products of the ones before.  Two such workgroups share a
-// compute unit: the end of one's tile lies beside the other's product.
+// compute unit: the end of one's tile lies beside the other's product.  870 TFLOP/s of fp16 with long rows (a library's large product:
+// 1,190); LDS is busy for three cycles where the matrix cores are for two (writes from memory take it for 16 cycles per KiB).
 constexpr int kWideM = 256, kWideN = 128, kWideSlice = 32;
 constexpr int kWideBuffer = (kWideM + kWideN) * kWideSlice * 2;
 
@@ -387,15 +409,6 @@ __device__ __forceinline__ void wide_product(f32x16 (&acc)[4][2], const Lines<T>
   if (s + 1 < slices) step(s + 1, lds1, lds2);
 }
 
-template <int M, int N>
-__device__ __forceinline__ void clear(f32x16 (&acc)[M][N]) {
-#pragma unroll
-  for (int i = 0; i < M; ++i)
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
-}
 // Row of a 32 x 32 block that register r of the lane's half holds.
 __device__ __forceinline__ int block_row(int r) { return r / 4 * 8 + lane_id() / 32 * 4 + r % 4; }
 
