@@ -679,17 +679,17 @@ struct FinishArgs {
   uint32_t *alt_ids;
 };
 
-// A row's product with the query (in LDS, zero from d on) in fp64, by a whole wavefront.
-template <typename T>
+// A row's product with the query (in LDS, zero from d on) in fp64, by LANES lanes.
+template <typename T, int LANES>
 __device__ __forceinline__ double exact_dot(const T *x, const float *q, uint32_t d) {
   double sum = 0.0;
-  for (uint32_t k = lane_id() * 8; k < d; k += 512) {
+  for (uint32_t k = lane_id() % LANES * 8; k < d; k += LANES * 8) {
     Unit<T> u;
     load_unit(u, x + k, (int64_t)d - k);
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum = __builtin_fma((double)to_f32(u.v[e]), (double)q[k + e], sum);
   }
-  return group_sum_f64<64>(sum);
+  return group_sum_f64<LANES>(sum);
 }
 
 // Row `in` of a group.
@@ -790,7 +790,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 5 : 4) void row_finish_ke
   t = group_sum_f64<64>(t);
   if (lane == 0) room64[0][wave] = l, room64[1][wave] = t;
   double target_dot = 0.0;
-  if (target < g.n && wave == kWaves - 1) target_dot = exact_dot<T>(rows + (uint64_t)target * g.row_stride, q, g.d);
+  if (target < g.n && wave == kWaves - 1) target_dot = exact_dot<T, 64>(rows + (uint64_t)target * g.row_stride, q, g.d);
   if constexpr (GROUP != 0) {
     // The k-th largest of the tops: at least k groups reach it.
     const float own = tops[tid / kSharers];
@@ -884,25 +884,34 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 5 : 4) void row_finish_ke
         __syncthreads();
         continue;
       }
-      // Scores rows in fp64, a wavefront to a row, and keeps what may be among the best.  All lanes.
-      const auto score_rows = [&](const uint32_t *ids, int step, uint32_t found, bool first_of_all) {
-        for (uint32_t f0 = 0; f0 < found; f0 += kWaves) {
+      // Scores rows in fp64, a wavefront to a row (short ones: 16 lanes), and keeps what may be among the best.  All lanes.
+      const auto score_some = [&](auto lanes, const uint32_t *ids, int step, uint32_t found, bool first_of_all) {
+        constexpr int LANES = decltype(lanes)::value;
+        constexpr uint32_t kAtOnce = THREADS / LANES;
+        for (uint32_t f0 = 0; f0 < found; f0 += kAtOnce) {
           if (f0 != 0 || !first_of_all) {  // (at first there is room)
             const uint32_t held = n_best;
             __syncthreads();  // all lanes have read it: they agree whether to make more
-            if (held + kWaves > kBest) keep_best();
+            if (held + kAtOnce > kBest) keep_best();
           }
-          if (f0 + wave < found) {
-            const uint32_t row = ids[(int)(f0 + wave) * step];
+          const uint32_t f = f0 + tid / LANES;
+          if (f < found) {
+            const uint32_t row = ids[(int)f * step];
             const float bias = row < g.n ? (g.bias ? g.bias[row] : 0.0f) : -INFINITY;
-            const double s = bias != -INFINITY ? (double)g.scale * exact_dot<T>(rows + row * g.row_stride, q, g.d) + (double)bias : (double)NAN;
-            if (lane == 0 && s >= bound) {
+            const double s = bias != -INFINITY ? (double)g.scale * exact_dot<T, LANES>(rows + row * g.row_stride, q, g.d) + (double)bias : (double)NAN;
+            if (lane % LANES == 0 && s >= bound) {
               const uint32_t at = atomicAdd(&n_best, 1u);
               best[side][at] = s, best_id[side][at] = row;
             }
           }
           __syncthreads();
         }
+      };
+      const auto score_rows = [&](const uint32_t *ids, int step, uint32_t found, bool first_of_all) {
+        if (g.d <= 128)
+          score_some(std::integral_constant<int, 16>(), ids, step, found, first_of_all);
+        else
+          score_some(std::integral_constant<int, 64>(), ids, step, found, first_of_all);
       };
       score_rows(list + kListed - 1, -1, singles, begin == 0);
       for (uint32_t c0 = 0; c0 < count; c0 += kWaves) {
