@@ -30,7 +30,7 @@ constexpr uint64_t kChunkBytes = 512ull << 20;  // of G at a time
 constexpr uint32_t kGradTarget = 768;           // workgroups of a product: three to a compute unit
 constexpr uint32_t kWideSlots = 512;            // of a wide one: two
 
-// Wavefronts to a SIMD of the gradients' products (three instead of two: 303 -> 237 and 282 -> 255 us with 2,048 x 50,000 x 768).
+// Wavefronts to a SIMD of the gradients' products by tiles of 128 (three instead of two: 303 -> 237 and 282 -> 255 us with 2,048 x 50,000 x 768).
 template <typename T>
 constexpr int kGradWaves = sizeof(T) == 2 ? 3 : 2;
 
@@ -149,6 +149,7 @@ __global__ __launch_bounds__(256) void grad_scores_kernel(GradArgs a, uint32_t r
 
 // part[split][q][c] (+)= sum over the split's rows of the chunk of G[q][j] x[j][c]  (rows left out may hold anything: read as zeros, or,
 // MB == 4, there are none)
+// MB == 4: tiles of 256 queries by the wide product (2,048 x 50,000 x 768 fp16: 183 us, 860 TFLOP/s; by tiles of 128: 240).
 template <typename T, int MB>
 __global__ __launch_bounds__(256, MB == 4 ? 2 : kGradWaves<T>) void grad_queries_kernel(ScoreTable g, uint32_t row0, uint32_t rows, uint32_t ld, const T *__restrict__ G,
                                                                                         uint32_t splits, float *__restrict__ part, bool add) {
@@ -350,7 +351,8 @@ __global__ __launch_bounds__(256) void grad_bias_kernel(const float *__restrict_
 // asks of its first operand if it takes the passing lines in that order (a sum has none); its second operand is the tile once more,
 // transposed by the LDS.  Each side costs the scores anew: four products where storing G costs three, but G need not be
 // written and read (twice two bytes for 256 operations).
-// One side of 4,096 x 100,000 x 128 (both: SHORT_BOTH).
+// 4,096 x 100,000 x 128 bf16: 290 us for the queries' side, 327 for the rows' (730 and 640 TFLOP/s; 1,097 us with G stored); bound by the
+// exponentials' instructions beside the products.
 constexpr int kPassing = 64, kOwned = 128;
 constexpr uint32_t kShortTarget = 512;       // workgroups that own queries: two to a compute unit
 constexpr uint64_t kShortStride = 1u << 24;  // row stride up to which offsets within a tile take 32 bits
