@@ -106,6 +106,8 @@ __global__ __launch_bounds__(256) void grad_scores_kernel(GradArgs a, uint32_t r
         const float p = __builtin_amdgcn_exp2f(s * kLog2e);
         const float slope = ENTROPY ? __builtin_fmaf(gh, s + h, gl) : gl;
         float v = -(p * slope);
+        // (no probability: 0, also where the score is so low that its slope overflows)
+        if (ENTROPY && !(p != 0.0f)) v = 0.0f;
         if ((uint32_t)(i * 32 + block_row(r)) == hit) v += gl;
         if ((BIAS || !whole) && bias == -INFINITY) v = 0.0f;
         acc[i][j][r] = none ? 0.0f : v;
