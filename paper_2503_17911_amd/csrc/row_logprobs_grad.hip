@@ -12,8 +12,9 @@
 // G in 16 bits: bf16 has the range for any probability.  f16 does not (a million
 // like rows have p = 2^-20, its smallest normal number is 2^-14), so G is stored
 // times the power of two that brings |g| + |h| (H + 1/e), which no element of G exceeds, to
-// 2^13 .. 2^14; what lies 2^-28 below the largest then starts to lose bits, 2^-38 is
-// lost, which a sum over 2^31 rows cannot show in f16.  The element of the given row
+// 2^13 .. 2^14 for the query with the largest; what lies 2^-28 below that starts to lose bits, 2^-38 is
+// lost: n such elements are less than half a step of the largest in f16 (2^-11 of it) up to n = 2^27, and queries
+// with much smaller weights than the largest keep the bits that this leaves them.  The element of the given row
 // is formed as g (1 - p) in fp32 before it is rounded: apart, g x_t and g p x_t would cancel.
 // What its rounding leaves goes to dq in fp32: that element outweighs all others
 // and rows of a cluster are alike, so that dq, their difference, erred by 0.6 % (bf16) with it, 0.17 % is the rounding of dq.
@@ -44,14 +45,17 @@ struct GradArgs {
   float *rest;           // [nq]: what the rounding of the given row's element left (16 bits)
 };
 
-// scaling[0]: the power of two for G, scaling[1]: its inverse.
+// scaling[0]: the power of two for G, scaling[1]: its inverse.  A query counts as it does in G: with g_logprob where a row is given, not at
+// all without a row left (or with statistics that are NaN).  Weights that are not finite spoil their own query, not the scale of the others.
 __global__ __launch_bounds__(1024) void grad_scaling_kernel(GradArgs a, float *__restrict__ scaling) {
   __shared__ float room[16];
   float most = 0.0f;
   for (uint32_t i = threadIdx.x; i < a.g.nq; i += 1024) {
-    float v = a.g_logprob ? fabsf(a.g_logprob[i]) : 0.0f;
-    if (a.g_entropy) v += fabsf(a.g_entropy[i]) * (fabsf(a.entropy[i]) + 0.375f);
-    most = fmaxf(most, v);
+    if (!(a.lse[i] > -INFINITY)) continue;
+    const bool given = a.targets && a.targets[i] < a.g.n;
+    const float g = a.g_logprob && given ? fabsf(a.g_logprob[i]) : 0.0f;
+    const float h = a.g_entropy ? fabsf(a.g_entropy[i]) * (fabsf(a.entropy[i]) + 0.375f) : 0.0f;
+    if (g < INFINITY && h < INFINITY) most = fmaxf(most, fminf(g + h, 3.402823466e38f));
   }
   most = wave_max_f32(most);
   if (threadIdx.x % kWave == 0) room[threadIdx.x / kWave] = most;
@@ -59,8 +63,8 @@ __global__ __launch_bounds__(1024) void grad_scaling_kernel(GradArgs a, float *_
   if (threadIdx.x != 0) return;
   for (int w = 0; w < 16; ++w) most = fmaxf(most, room[w]);
   int e = 0;
-  if (most > 0.0f && most < INFINITY) frexpf(most, &e);  // most < 2^e
-  e = e < -100 ? -100 : e > 100 ? 100 : e;
+  if (most > 0.0f) frexpf(most, &e);  // most < 2^e, e <= 128
+  e = e < -100 ? -100 : e;
   scaling[0] = ldexpf(1.0f, 14 - e);
   scaling[1] = ldexpf(1.0f, e - 14);
 }
