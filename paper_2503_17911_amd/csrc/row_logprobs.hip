@@ -658,9 +658,12 @@ __global__ __launch_bounds__(256) void row_norms_kernel(ScoreTable g, float *__r
 // partial sum of at most |q| |x| (2^-24 of it; twice that for the order inside the
 // instruction), the products of parts left out are below 2^-23 of |q| |x|, and the last
 // product and addition round a score, which is at most `largest` in size.  fp32: six products to an element.
+// Below fp32's normal numbers roundings are steps of their own size (a number in the low four bits is up to 16 of
+// the smallest), and products and parts may be taken for zero: at most 2^-126 to an addition, before and after the scale.
 __device__ __forceinline__ float score_room(uint32_t d, bool parts, bool is_numbered, float q_norm, float x_norm, float scale, float largest) {
   const float size = fabsf(scale) * q_norm * x_norm * 1.001f;
-  return ((parts ? 6.0f : 1.0f) * (float)d + 64.0f) * 0x1p-23f * size + (is_numbered ? 0x1p-18f : 0x1p-22f) * (largest + size);
+  const float additions = (parts ? 6.0f : 1.0f) * (float)d + 64.0f;
+  return additions * 0x1p-23f * size + (is_numbered ? 0x1p-18f : 0x1p-22f) * (largest + size) + additions * 0x1p-126f * (1.0f + fabsf(scale));
 }
 
 constexpr uint32_t kListed = 1024;      // groups that are taken up at a time
