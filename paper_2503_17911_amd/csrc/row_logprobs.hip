@@ -114,8 +114,9 @@ __device__ __forceinline__ float largest_of(const f32x16 &acc, float scale) {
   for (int r = 1; r < 16; ++r) top = fmaxf(top, acc[r]);
   return MASKED ? top : top * scale;
 }
-// The largest of the lane's 16 scores, its low four bits replaced by its number, and the second largest.  (Rows left out stand for the
-// lowest number: -infinity has no bits to spare.)
+// The largest of the lane's 16 scores, its low four bits replaced by its number, and the second largest.  (Infinite scores stand for the
+// lowest and the largest number: they have no bits to spare.  Without biases they come with rows whose norm is infinite, and then the
+// maxima are not used.)
 struct TopTwo {
   float first, second;
 };
@@ -125,7 +126,7 @@ __device__ __forceinline__ TopTwo two_largest_of(const f32x16 &acc, float scale)
   TopTwo t = {-3.402823466e38f, -3.402823466e38f};
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
-    const float s = numbered(MASKED ? fmaxf(acc[r], -3.402823466e38f) : acc[r], r);
+    const float s = numbered(MASKED ? __builtin_amdgcn_fmed3f(acc[r], -3.402823466e38f, 3.402823466e38f) : acc[r], r);
     t.second = r ? fmaxf(t.second, fminf(t.first, s)) : t.second;
     t.first = r ? fmaxf(t.first, s) : s;
   }
@@ -867,7 +868,8 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 5 : 4) void row_finish_ke
         for (uint32_t u = 0; u < kInFlight; ++u) v[u] = c + u * THREADS < end ? gm[c + u * THREADS] : NAN;
 #pragma unroll
         for (uint32_t u = 0; u < kInFlight; ++u)
-          if (v[u] >= least) {  // (the order plays no part)
+          // (the order plays no part; not bounded: every group, a NaN may have hidden its other rows)
+          if (v[u] >= least || (!bounded && c + u * THREADS < end)) {
             const uint32_t group = c + u * THREADS;
             if (bounded && second && !(second[group] >= least)) {  // one row of it: from the list's end
               const uint32_t at = atomicAdd(&n_single, 1u);
