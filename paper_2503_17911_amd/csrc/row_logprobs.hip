@@ -1,9 +1,14 @@
 // Log probabilities of given rows under the softmax of all rows' scores
 // s[i][j] = scale <q_i, x_j> + bias_j, with the softmax' entropy and its largest
 // alternatives.  The scores stay in the accumulators of the product: each lane
-// keeps, for its queries, a running maximum m, l = sum exp(s - m) and
+// keeps, for its queries, a reference m near the largest score, l = sum exp(s - m) and
 // t = sum exp(s - m) (s - m) (all fp32) over the rows that pass by; at the end
 // lse = m + log l, entropy = log l - t / l.
+//
+// Without biases (and with a scale that is not negative) m and the exponents are kept times log2 e, so that an exponent is one
+// fused multiply-add of the product's result that rounds once: with m in natural units, m log2 e was rounded apart from m, which moved
+// all of a lane's exponentials alike (lse, and the log probabilities with it, by up to half a step of 1.44 m).  What the rounding of
+// scale log2 e does to lse is made up for at the end, to first order: lse changes by its relative error times the mean score.
 //
 // Alternatives: the product kernel also writes the largest score of every group of
 // rows (one number for kGroup scores).  The k best rows lie in groups whose
@@ -30,13 +35,16 @@ constexpr uint32_t kSplitTarget = 6144; // workgroups of the product kernels for
 constexpr uint32_t kWideSlots = 512;    // workgroups of the wide product that run at once: two to a compute unit
 constexpr float kNothing = -1000.0f;    // an exponent whose power is zero, and finite
 
+// BIAS: natural units; otherwise m and t are times log2 e.
 struct Stats {
   float m, l, t;
 };
+template <bool BIAS>
 __device__ __forceinline__ void join(Stats &a, const Stats &b) {
+  constexpr float kUnit = BIAS ? kLog2e : 1.0f;
   const float m = fmaxf(a.m, b.m);
   const float da = fmaxf(a.m - m, kNothing), db = fmaxf(b.m - m, kNothing);
-  const float fa = __builtin_amdgcn_exp2f(da * kLog2e), fb = __builtin_amdgcn_exp2f(db * kLog2e);
+  const float fa = __builtin_amdgcn_exp2f(da * kUnit), fb = __builtin_amdgcn_exp2f(db * kUnit);
   a.t = fa * __builtin_fmaf(da, a.l, a.t) + fb * __builtin_fmaf(db, b.l, b.t);
   a.l = __builtin_fmaf(fa, a.l, fb * b.l);
   a.m = m;
@@ -46,13 +54,15 @@ __device__ __forceinline__ void join(Stats &a, const Stats &b) {
 // largest score: it is raised when one lies kSlack above it, which is seldom, and nothing is scaled in between.  The scores of a tile are
 // summed by themselves and the tiles' sums with what the last addition lost: over a million rows plain sums erred by
 // 4.6e-6, ten times the rounding of the scores.
-constexpr float kSlack = 20.0f;  // exp(20) times 2^31 rows is far from fp32's end
+template <bool BIAS>
 struct Running {
+  static constexpr float kUnit = BIAS ? kLog2e : 1.0f;
+  static constexpr float kSlack = BIAS ? 20.0f : 28.0f;  // exp(20) times 2^31 rows is far from fp32's end
   float m = -3.402823466e38f, l = 0.0f, t = 0.0f, l_lost = 0.0f, t_lost = 0.0f;
 
-  __device__ __forceinline__ bool behind(float top) const { return top > m + kSlack; }
+  __device__ __forceinline__ bool behind(float top) const { return BIAS ? top > m + kSlack : __builtin_fmaf(top, kLog2e, -m) > kSlack; }
   __device__ __forceinline__ void raise(float top) {
-    const float next = behind(top) ? top : m, step = fmaxf(m - next, kNothing), f = __builtin_amdgcn_exp2f(step * kLog2e);
+    const float next = behind(top) ? BIAS ? top : top * kLog2e : m, step = fmaxf(m - next, kNothing), f = __builtin_amdgcn_exp2f(step * kUnit);
     t = f * __builtin_fmaf(step, l, t), t_lost *= f;
     l *= f, l_lost *= f;
     m = next;
@@ -63,28 +73,21 @@ struct Running {
     lost = (next - sum) - v;
     sum = next;
   }
-  // N scores, none of which lies far above m.  MASKED: they are whole, and -infinity means a row left out; otherwise a score
-  // is s * scale, with c = scale log2 e.
+  // N scores, none of which lies far above m: whole ones with BIAS, else they are s * scale, with c = scale log2 e.  MASKED: -infinity
+  // means a row left out.
   template <bool MASKED, int N>
   __device__ __forceinline__ void take(const float (&s)[N], float c) {
     float sum = 0.0f, weighed = 0.0f;
-    const float m2 = m * kLog2e;
 #pragma unroll
     for (int r = 0; r < N; ++r) {
-      if constexpr (MASKED) {
-        const float y = s[r] == -INFINITY ? kNothing : s[r] - m;
-        const float p = __builtin_amdgcn_exp2f(y * kLog2e);
-        sum += p;
-        weighed = __builtin_fmaf(p, y, weighed);
-      } else {
-        const float y = __builtin_fmaf(s[r], c, -m2);
-        const float p = __builtin_amdgcn_exp2f(y);
-        sum += p;
-        weighed = __builtin_fmaf(p, y, weighed);
-      }
+      float y = BIAS ? s[r] - m : __builtin_fmaf(s[r], c, -m);
+      if (MASKED) y = s[r] == -INFINITY ? kNothing : y;
+      const float p = __builtin_amdgcn_exp2f(y * kUnit);
+      sum += p;
+      weighed = __builtin_fmaf(p, y, weighed);
     }
     add(l, l_lost, sum);
-    add(t, t_lost, MASKED ? weighed : weighed * kLn2);
+    add(t, t_lost, weighed);
   }
   __device__ __forceinline__ Stats stats() const { return {m, l, t}; }
 };
@@ -95,24 +98,30 @@ __host__ __device__ constexpr uint32_t group_count(uint32_t n, int group) { retu
 // Where a query's groups lie from the one's before (groups of 16: so that eight of them are two aligned pieces of 16 bytes).
 __host__ __device__ constexpr uint32_t group_stride(uint32_t n, int group) { return group == 64 ? group_count(n, 64) : (group_count(n, 16) + 7) / 8 * 8; }
 
-// A block of 32 rows x 32 queries, rows down the registers and queries along the lanes.  MASKED: scores are made whole, bias[32] (LDS)
-// added, -infinity where a row does not count.  Then the lane's largest score (of 16 rows).
-template <bool MASKED>
+// A block of 32 rows x 32 queries, rows down the registers and queries along the lanes.  BIAS: scores are made whole, bias[32] (LDS)
+// added.  MASKED: -infinity where a row does not count.  Then the lane's largest score (of 16 rows).
+template <bool MASKED, bool BIAS>
 __device__ __forceinline__ void add_bias(f32x16 &acc, const float *bias, float scale) {
+  static_assert(MASKED || !BIAS, "biases may leave rows out");
   if constexpr (MASKED) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const float b = bias[block_row(r)];
-      acc[r] = b == -INFINITY ? -INFINITY : __builtin_fmaf(acc[r], scale, b);
+      acc[r] = b == -INFINITY ? -INFINITY : BIAS ? __builtin_fmaf(acc[r], scale, b) : acc[r];
     }
   }
 }
-template <bool MASKED>
+// The score of a largest element (a scale of zero leaves -infinity, no row at all, as it is).
+template <bool MASKED, bool BIAS>
+__device__ __forceinline__ float scaled(float top, float scale) {
+  return BIAS || (MASKED && top == -INFINITY) ? top : top * scale;
+}
+template <bool MASKED, bool BIAS>
 __device__ __forceinline__ float largest_of(const f32x16 &acc, float scale) {
   float top = acc[0];
 #pragma unroll
   for (int r = 1; r < 16; ++r) top = fmaxf(top, acc[r]);
-  return MASKED ? top : top * scale;
+  return scaled<MASKED, BIAS>(top, scale);
 }
 // The largest of the lane's 16 scores, its low four bits replaced by its number, and the second largest.  (Infinite scores stand for the
 // lowest and the largest number: they have no bits to spare.  Without biases they come with rows whose norm is infinite, and then the
@@ -121,20 +130,24 @@ struct TopTwo {
   float first, second;
 };
 __device__ __forceinline__ float numbered(float s, uint32_t r) { return __uint_as_float((__float_as_uint(s) & ~15u) | r); }
-template <bool MASKED>
+__device__ __forceinline__ float finite(float s) { return __builtin_amdgcn_fmed3f(s, -3.402823466e38f, 3.402823466e38f); }
+template <bool MASKED, bool BIAS>
 __device__ __forceinline__ TopTwo two_largest_of(const f32x16 &acc, float scale) {
   TopTwo t = {-3.402823466e38f, -3.402823466e38f};
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
-    const float s = numbered(MASKED ? __builtin_amdgcn_fmed3f(acc[r], -3.402823466e38f, 3.402823466e38f) : acc[r], r);
+    const float s = numbered(MASKED ? finite(acc[r]) : acc[r], r);
     t.second = r ? fmaxf(t.second, fminf(t.first, s)) : t.second;
     t.first = r ? fmaxf(t.first, s) : s;
   }
-  if constexpr (!MASKED) t = {numbered(t.first * scale, __float_as_uint(t.first) & 15u), t.second * scale};
+  if constexpr (!BIAS) {
+    const float first = t.first * scale;
+    t = {numbered(MASKED ? finite(first) : first, __float_as_uint(t.first) & 15u), t.second * scale};
+  }
   return t;
 }
-template <bool MASKED>
-__device__ __forceinline__ void take_block(const f32x16 &acc, Running &run, float c) {
+template <bool MASKED, bool BIAS>
+__device__ __forceinline__ void take_block(const f32x16 &acc, Running<BIAS> &run, float c) {
   float s[16];
 #pragma unroll
   for (int r = 0; r < 16; ++r) s[r] = acc[r];
@@ -158,10 +171,11 @@ __device__ __forceinline__ void put_groups(float top0, float top1, uint32_t q, u
 }
 
 // The statistics of the two lanes, 32 apart, that share a query.
+template <bool BIAS>
 __device__ __forceinline__ Stats join_halves(const Stats &s) {
   const LanePair m = lane_pair<false>(__float_as_uint(s.m)), l = lane_pair<false>(__float_as_uint(s.l)), t = lane_pair<false>(__float_as_uint(s.t));
   Stats a = {__uint_as_float(m.low), __uint_as_float(l.low), __uint_as_float(t.low)};
-  join(a, {__uint_as_float(m.high), __uint_as_float(l.high), __uint_as_float(t.high)});
+  join<BIAS>(a, {__uint_as_float(m.high), __uint_as_float(l.high), __uint_as_float(t.high)});
   return a;
 }
 
@@ -187,7 +201,7 @@ __global__ __launch_bounds__(256, MB == 4 ? 2 : 1) void row_scores_kernel(ScoreT
   const Lines<T> X = {(const T *)g.rows, g.row_stride, g.n, g.d}, Q = {(const T *)g.q, g.q_stride, g.nq, g.d};
   const uint32_t n_groups = GROUP ? group_count(g.n, GROUP) : 0, stride = GROUP ? group_stride(g.n, GROUP) : 0;
   const float c = g.scale * kLog2e;
-  Running run[2];
+  Running<BIAS> run[2];
   for (uint32_t tile = first; tile < last; ++tile) {
     const uint32_t row0 = tile * kRowTile;
     const bool whole = row0 + kRowTile <= g.n;
@@ -215,15 +229,15 @@ __global__ __launch_bounds__(256, MB == 4 ? 2 : 1) void row_scores_kernel(ScoreT
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             f32x16 &block = acc[i0 + i][j];
-            add_bias<MASKED>(block, row_bias + mw + (i0 + i) * 32, g.scale);
+            add_bias<MASKED, BIAS>(block, row_bias + mw + (i0 + i) * 32, g.scale);
             if (is_numbered) {
-              const TopTwo t = two_largest_of<MASKED>(block, g.scale);
+              const TopTwo t = two_largest_of<MASKED, BIAS>(block, g.scale);
               top[i] = t.first, second[i] = t.second;
             } else {
-              top[i] = largest_of<MASKED>(block, g.scale);
+              top[i] = largest_of<MASKED, BIAS>(block, g.scale);
             }
             if (__any(run[j].behind(top[i]))) run[j].raise(top[i]);
-            take_block<MASKED>(block, run[j], c);
+            take_block<MASKED, BIAS>(block, run[j], c);
             if (MB == 4) __builtin_amdgcn_sched_barrier(0);
           }
           put_groups<GROUP>(top[0], top[1], q, g.nq, row0 + mw + i0 * 32, n_groups, stride, group_max);
@@ -234,21 +248,21 @@ __global__ __launch_bounds__(256, MB == 4 ? 2 : 1) void row_scores_kernel(ScoreT
     if (BIAS || !whole)
       finish(std::true_type());
     else
-      finish(std::false_type());
+      finish(std::integral_constant<bool, BIAS>());
   }
   // the two halves of a wavefront, then the two wavefronts that share queries
   __shared__ Stats other[2][64];
   Stats st[2];
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    st[j] = join_halves(run[j].stats());
+    st[j] = join_halves<BIAS>(run[j].stats());
     if (wave >= 2 && lane < 32) other[wave % 2][j * 32 + lane] = st[j];
   }
   __syncthreads();
   if (wave < 2 && lane < 32) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      join(st[j], other[wave][j * 32 + lane]);
+      join<BIAS>(st[j], other[wave][j * 32 + lane]);
       const uint32_t q = qt * kTile + nw + j * 32 + lane;
       if (q < g.nq) stats[(uint64_t)split * g.nq + q] = make_float4(st[j].m, st[j].l, st[j].t, 0.0f);
     }
@@ -338,7 +352,7 @@ __global__ __launch_bounds__(256, 2) void row_scores_short_kernel(ScoreTable g, 
       for (int j = 0; j < 2; ++j) acc[j] = matrix_step(x, query[j][kk], acc[j]);
     }
   };
-  Running run[2];
+  Running<BIAS> run[2];
   float top[2][2];  // of either half of a tile
   // The scores of a half of a tile are taken on while `also` (the next half's product) is formed.
   const auto end = [&](f32x16(&past)[2], uint32_t tile, int half, auto also) {
@@ -347,8 +361,8 @@ __global__ __launch_bounds__(256, 2) void row_scores_short_kernel(ScoreTable g, 
       bool behind = false;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        add_bias<MASKED>(past[j], row_bias[tile & 3] + half * 32, g.scale);
-        top[half][j] = largest_of<MASKED>(past[j], g.scale);
+        add_bias<MASKED, BIAS>(past[j], row_bias[tile & 3] + half * 32, g.scale);
+        top[half][j] = largest_of<MASKED, BIAS>(past[j], g.scale);
         behind |= run[j].behind(top[half][j]);
       }
       if (__any(behind)) {
@@ -357,12 +371,12 @@ __global__ __launch_bounds__(256, 2) void row_scores_short_kernel(ScoreTable g, 
       }
       also();
 #pragma unroll
-      for (int j = 0; j < 2; ++j) take_block<MASKED>(past[j], run[j], c);
+      for (int j = 0; j < 2; ++j) take_block<MASKED, BIAS>(past[j], run[j], c);
     };
     if (BIAS || tile * kShortRows + kShortRows > g.n)
       with(std::true_type());
     else
-      with(std::false_type());
+      with(std::integral_constant<bool, BIAS>());
     if (GROUP != 0 && half) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) put_groups<GROUP>(top[0][j], top[1][j], q + j * 32, g.nq, tile * kShortRows, n_groups, stride, group_max);
@@ -385,7 +399,7 @@ __global__ __launch_bounds__(256, 2) void row_scores_short_kernel(ScoreTable g, 
   }
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    const Stats s = join_halves(run[j].stats());
+    const Stats s = join_halves<BIAS>(run[j].stats());
     if (lane < 32 && q + j * 32 < g.nq) stats[(uint64_t)split * g.nq + q + j * 32] = make_float4(s.m, s.l, s.t, 0.0f);
   }
 }
@@ -474,7 +488,7 @@ __global__ __launch_bounds__(kStreamThreads) void row_stream_kernel(ScoreTable g
       }
     }
   };
-  Running run[NB];
+  Running<BIAS> run[NB];
   f32x4 acc[NB][4];
   float squares[4] = {0.0f, 0.0f, 0.0f, 0.0f}, largest = 0.0f;
   uint32_t block = first + wave, round = 0;
@@ -547,10 +561,10 @@ __global__ __launch_bounds__(kStreamThreads) void row_stream_kernel(ScoreTable g
             for (int r = 0; r < 4; ++r) {
               const int i = b * 4 + r;
               s[i] = acc[j][b][r];
-              if constexpr (MASKED) s[i] = bias[i] == -INFINITY ? -INFINITY : __builtin_fmaf(s[i], g.scale, bias[i]);
+              if constexpr (MASKED) s[i] = bias[i] == -INFINITY ? -INFINITY : BIAS ? __builtin_fmaf(s[i], g.scale, bias[i]) : s[i];
               top[b] = r ? fmaxf(top[b], s[i]) : s[i];
             }
-            if constexpr (!MASKED) top[b] *= g.scale;
+            top[b] = scaled<MASKED, BIAS>(top[b], g.scale);
           }
           const float all = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
           if constexpr (GROUP != 0) {
@@ -580,7 +594,7 @@ __global__ __launch_bounds__(kStreamThreads) void row_stream_kernel(ScoreTable g
       if (BIAS || !whole)
         finish(std::true_type());
       else
-        finish(std::false_type());
+        finish(std::integral_constant<bool, BIAS>());
     }
     block = next_block, round = next_round;
   }
@@ -594,7 +608,7 @@ __global__ __launch_bounds__(kStreamThreads) void row_stream_kernel(ScoreTable g
     for (int far = 16; far < 64; far *= 2) {
       const Stats b = {__int_as_float(xor_lane_i32(__float_as_int(a.m), far)), __int_as_float(xor_lane_i32(__float_as_int(a.l), far)),
                        __int_as_float(xor_lane_i32(__float_as_int(a.t), far))};
-      join(a, b);
+      join<BIAS>(a, b);
     }
     if (lane < 16) room[wave * NB * 16 + j * 16 + lane] = a;
   }
@@ -616,7 +630,7 @@ __global__ __launch_bounds__(kStreamThreads) void row_stream_kernel(ScoreTable g
   if (threadIdx.x < NB * 16 && threadIdx.x < g.nq) {
     Stats a = room[threadIdx.x];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) join(a, room[w * NB * 16 + threadIdx.x]);
+    for (int w = 1; w < kWaves; ++w) join<BIAS>(a, room[w * NB * 16 + threadIdx.x]);
     stats[(uint64_t)blockIdx.x * g.nq + threadIdx.x] = make_float4(a.m, a.l, a.t, 0.0f);
   }
   if (GROUP != 0 && threadIdx.x == 0) {
@@ -679,6 +693,7 @@ struct FinishArgs {
   const float4 *stats;
   const float *group_max, *group_second, *norms;  // group_second: with numbered largest scores (groups of 16), else NULL
   uint32_t splits, k, norm_runs;
+  double unit, scale_error;  // natural units to one of the statistics'; how much scale log2 e lacks where the kernels take it rounded, relative
   float *logprob, *entropy, *lse, *alt_logprobs;
   uint32_t *alt_ids;
 };
@@ -783,9 +798,9 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 5 : 4) void row_finish_ke
   double l = 0.0, t = 0.0;
   const auto join_split = [&](const float4 &v) {
     if (v.y != 0.0f) {
-      const double by = (double)v.x - (double)m, f = exp(by);
+      const double by = ((double)v.x - (double)m) * a.unit, f = exp(by);
       l += f * (double)v.y;
-      t += f != 0.0 ? f * ((double)v.z + by * (double)v.y) : 0.0;
+      t += f != 0.0 ? f * ((double)v.z * a.unit + by * (double)v.y) : 0.0;
     }
   };
   join_split(first);
@@ -813,7 +828,8 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 5 : 4) void row_finish_ke
 #pragma unroll
   for (int w = 1; w < kWaves; ++w) l += room64[0][w], t += room64[1][w];
   const bool none = l == 0.0;  // no row left
-  const double log_l = none ? 0.0 : log(l), lse = none ? -INFINITY : (double)m + log_l;
+  const double log_l = none ? 0.0 : log(l), shift = a.scale_error * ((double)m * a.unit + t / l);
+  const double lse = none ? -INFINITY : (double)m * a.unit + log_l + (fabs(shift) < INFINITY ? shift : 0.0);
   if (wave == kWaves - 1 && lane == 0) {
     double lp = 0.0;
     if (target < g.n) {  // (an id that is no row's: none)
@@ -1122,6 +1138,9 @@ static ann_status forward(const ann_row_scores &s, uint32_t k, const ForwardPlan
     ANN_HIP(refused);
     ANN_HIP(hipGetLastError());
     f.stats = stats, f.group_max = groups, f.group_second = seconds, f.norms = norms, f.splits = p.splits, f.norm_runs = p.norm_runs;
+    const float c = g.scale * kLog2e;
+    f.unit = bias ? 1.0 : M_LN2;
+    f.scale_error = bias || c == 0.0f ? 0.0 : (double)g.scale * M_LOG2E / (double)c - 1.0;
   }
   const uint32_t lds = (g.d + 511) / 512 * 512 * sizeof(float);
   const auto end = [&](auto group) {
