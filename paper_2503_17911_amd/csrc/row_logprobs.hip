@@ -212,6 +212,8 @@ __global__ __launch_bounds__(256, MB == 4 ? 2 : 1) void row_scores_kernel(ScoreT
     if constexpr (MB == 4)
       wide_product<T, kAlong, kAlong>(acc, X, row0, Q, qt * kTile, 0, g.d, lds, lds1, lds2);
     else
+      // (fp32: the smaller products apart take so many registers that one workgroup fits where two did: 155 -> 213 us for 513 x 50,000 x 100;
+      // with one sum the log probabilities err by 6e-8 there, by 2.8e-7 with 768 columns, about as far as a plain fp32 product's)
       tile_product<T, kAlong, kAlong>(acc, X, row0, Q, qt * kTile, 0, g.d, lds);
     if (BIAS || !whole) {
       // (read by the tile before's epilogue: the barriers of the product lie in between; d > 0)
@@ -491,7 +493,8 @@ __global__ __launch_bounds__(kStreamThreads) void row_stream_kernel(ScoreTable g
     }
   };
   Running<BIAS> run[NB];
-  f32x4 acc[NB][4];
+  constexpr bool kApart = O::kParts > 1;
+  f32x4 acc[NB][4], low[kApart ? NB : 1][4];  // low: the smaller products of fp32 parts, so that the sum rounds once per 32 columns and not six times
   float squares[4] = {0.0f, 0.0f, 0.0f, 0.0f}, largest = 0.0f;
   uint32_t block = first + wave, round = 0;
   if (block < last) fetch(next, block, 0);
@@ -507,7 +510,10 @@ __global__ __launch_bounds__(kStreamThreads) void row_stream_kernel(ScoreTable g
 #pragma unroll
       for (int j = 0; j < NB; ++j)
 #pragma unroll
-        for (int b = 0; b < 4; ++b) acc[j][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int b = 0; b < 4; ++b) {
+          acc[j][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+          if constexpr (kApart) low[j][b] = acc[j][b];
+        }
     }
 #pragma unroll
     for (int s = 0; s < S; ++s) {
@@ -529,7 +535,10 @@ __global__ __launch_bounds__(kStreamThreads) void row_stream_kernel(ScoreTable g
 #pragma unroll
           for (int p = 0; p <= sum; ++p)
 #pragma unroll
-            for (int j = 0; j < NB; ++j) acc[j][b] = small_step(x[p], q[sum - p][j], acc[j][b]);
+            for (int j = 0; j < NB; ++j) {
+              f32x4 &to = kApart && sum != 0 ? low[kApart ? j : 0][b] : acc[j][b];
+              to = small_step(x[p], q[sum - p][j], to);
+            }
       }
     }
     if (ends) {
@@ -562,7 +571,7 @@ __global__ __launch_bounds__(kStreamThreads) void row_stream_kernel(ScoreTable g
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
               const int i = b * 4 + r;
-              s[i] = acc[j][b][r];
+              s[i] = kApart ? acc[j][b][r] + low[kApart ? j : 0][b][r] : acc[j][b][r];
               if constexpr (MASKED) s[i] = bias[i] == -INFINITY ? -INFINITY : BIAS ? __builtin_fmaf(s[i], g.scale, bias[i]) : s[i];
               top[b] = r ? fmaxf(top[b], s[i]) : s[i];
             }
