@@ -43,3 +43,17 @@ def test_rows_of_infinity_beside_rows_that_are_not_numbers(nq, n, d, dtype):
     rows[group[0]] = math.nan
     got = L.forward(ann, q, rows, None, target, 20.0, 20)
     assert torch.equal(got["alt_ids"].long(), wanted(q, rows, None, 20))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("bias", ["none", "plain", "holes"])
+@pytest.mark.parametrize("nq, n, d", SHAPES)
+def test_rows_that_are_not_numbers(nq, n, d, bias, dtype):
+    """They are no alternatives, and hide none: among them the likeliest rows, the last row and a whole group."""
+    import paper_2503_17911_amd as ann
+    q, rows, b, target = L.inputs(nq, n, d, dtype, 6, bias)
+    rows[target[3:].clamp(0, n - 1)[:4]] = math.nan
+    rows[128:160], rows[n - 1] = math.nan, math.nan
+    got = L.forward(ann, q, rows, b, target, 20.0, 10)
+    assert torch.equal(got["alt_ids"].long(), wanted(q, rows, b, 10))
+    assert got["lse"].isnan().all()

@@ -34,3 +34,13 @@ def test_scores_below_the_normal_numbers(nq, n, d, k, dtype, scale):
     got = L.forward(ann, q, rows, None, target, scale, k)
     ids, _ = R.alternatives(R.scores(q, rows, scale, None), k)
     assert torch.equal(got["alt_ids"].long(), ids)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("scale", [0.0, 2.0 ** -130, 2.0 ** -30])
+@pytest.mark.parametrize("nq, n, d", [(5, 3000, 40), (5, 31, 16), (70, 3000, 40), (70, 3001, 200), (70, 20, 200), (1100, 15_001, 192)])
+def test_statistics_of_small_scales(nq, n, d, scale, dtype):
+    import paper_2503_17911_amd as ann
+    for bias in ("none", "holes"):
+        q, rows, b, target = L.inputs(nq, n, d, dtype, 4, bias)
+        L.check_forward(ann, q, rows, b, target, scale, 0)
