@@ -551,7 +551,7 @@ uint64_t ann_layer_norm_backward_workspace(uint64_t n, uint32_t dim);
  *              that is not below n): none.  NULL: none for any query.
  * Products of 16-bit elements are exact and summed in fp32; fp32 elements are
  * taken as three bf16 parts (six of the nine products; what is left out is below
- * 2^-23 of the product).
+ * 2^-23 of the product; elements below 2^-110 in size keep fewer bits).
  */
 typedef struct {
   const void *q, *rows;
@@ -577,9 +577,13 @@ typedef struct {
  * logprob and lse are required; entropy may be NULL; alt_ids and alt_logprobs
  * both or neither (k = 0: both NULL).  k <= ANN_MAX_ALTERNATIVES.  A query with no row left (all biases
  * -infinity, or n = 0): lse -infinity, entropy 0, logprob -infinity (0 where no
- * row is given), no alternatives.  A score of a row that is not
- * left out that is not finite (or, times log2 e, not) leaves that query's statistics NaN or infinite, and only
- * its; a row whose score is NaN is no alternative.  nq = 0 does nothing.
+ * row is given), no alternatives.  Scores beyond fp32's range, of rows that are not
+ * left out: NaN or +infinity leaves that query's statistics NaN or infinite, and
+ * only its (the alternatives are right: rows with +infinity first, rows with NaN never).
+ * -infinity is a probability of zero; without row_bias and with a scale that is
+ * not negative the entropy is NaN then.  That range is fp32's for scores with row_bias
+ * (masks of the lowest finite value are ordinary biases); without it the scores
+ * times log2 e have to be in it.  nq = 0 does nothing.
  * Errors: ANN_EINVAL (NULL arguments, unknown type, d == 0, strides, scale,
  * alternatives without k or the reverse, workspace), ANN_ECAPACITY (d, k, n, nq).
  */
@@ -599,7 +603,10 @@ uint64_t ann_row_logprobs_workspace(uint32_t nq, uint64_t n, uint32_t d, uint32_
  * G is rounded to 16 bits before its products with 16-bit rows and queries (bf16: to
  * bf16; f16: to f16 after a power of two that brings the largest weight to
  * 2^13 .. 2^14), and taken as three bf16 parts with fp32 ones; drow_bias sums it in fp32.  What that
- * rounding leaves of the given rows' elements, and in drows of all elements where queries are few, is added.
+ * rounding leaves of the given rows' elements, and in drows of all elements where queries are few, is added;
+ * elsewhere it remains: it is as large as the results' own rounding where no given row outweighs the others (the entropy's
+ * gradient alone).  The power of two goes by the queries that take part, and by finite weights only.
+ * A row whose probability is zero gets and adds nothing, however low its score, unless it is a query's given row.
  * A score and lse of the size of a mask (1e6 and more) leave nothing of their difference's
  * small part in fp32: probabilities among such scores alone (no other row left) are not those of the forward pass.
  * Queries without a given row take no part with their g_logprob; rows left out get

@@ -17,13 +17,14 @@
 // and their rows are scored again in fp64 and put in order.  That is exact whatever the
 // distribution, ties included; how many rows are scored again is all that depends on it.
 // Long rows (more than 128 columns, no stream): a group's second largest score is written as well, and the largest carries
-// its row's number in its low four bits; mostly that row alone is scored again (4,096 x 100,003 x 768, k = 20: 400 -> 190 us
+// its row's number in its low four bits; mostly that row alone is scored again (4,000 x 100,003 x 768, k = 20: 400 -> 190 us
 // for the end; the product kernel pays 130 of them back).
 //
 // Three product kernels, chosen by forward_plan(): row_stream_kernel for few queries, bound by reading the rows (1 x 1M x 128 bf16:
 // 43 us, 6.0 TB/s; 8 x 200,000 x 960 fp32: 171 us, 4.5 TB/s); row_scores_short_kernel for 16-bit rows of at most 128 columns, bound by the
-// instructions of the exponentials (10,000 x 1M x 128: 3.5 ms, 730 TFLOP/s); row_scores_kernel for the rest, bound by the matrix cores'
-// supply (4,096 x 100,003 x 768 without alternatives: 0.75 ms, 834 TFLOP/s).
+// instructions of the exponentials (10,000 x 1M x 128: 3.5 ms, 720 TFLOP/s; vector instructions issue in 80 % of the cycles, the matrix cores work in
+// 41 %); row_scores_kernel for the rest, bound by the matrix cores' supply (4,000 x 100,003 x 768 without alternatives: 0.84 ms for the call,
+// 730 TFLOP/s; the kernel with k = 20: 0.96 ms).
 #include "row_logprobs.hpp"
 
 #include <math.h>
@@ -182,7 +183,8 @@ __device__ __forceinline__ Stats join_halves(const Stats &s) {
 }
 
 // BIAS: rows may be left out, or the scale is negative.  MB: blocks of 32 rows to a wavefront; four: the wide product, for 16-bit
-// rows of whole slices where tiles of 256 rows still fill the card (4,096 x 100,003 x 768 with k = 20: 907 us by tiles of 128).
+// rows of whole slices where tiles of 256 rows still fill the card (4,000 x 100,003 x 768 fp16, the call: 1,074 us against 1,118 by tiles of 128 with
+// k = 20, 840 against 922 without alternatives, though 29 registers a lane are kept in scratch memory).
 template <typename T, bool BIAS, int GROUP, int MB>
 __global__ __launch_bounds__(256, MB == 4 ? 2 : 1) void row_scores_kernel(ScoreTable g, uint32_t q_tiles, uint32_t q_group, uint32_t splits, float4 *__restrict__ stats,
                                                          float *__restrict__ group_max, float *__restrict__ group_second) {
