@@ -494,8 +494,8 @@ ann_status ann_bruteforce_topk(const float *x, uint64_t n, uint32_t d, const flo
                                uint32_t metric, uint32_t *out_ids, float *out_dist, void *stream);
 
 /*
- * The head of a model over a table of rows: what an encoder does last (layer
- * norm) and what it is trained with and weighed by (probabilities of rows under
+ * The model over a table of rows: what an encoder does first (embeddings of tokens),
+ * between its layers (root-mean-square norm) and last (layer norm), and what it is trained with and weighed by (probabilities of rows under
  * the softmax of all rows' scores), each with its gradient.  These calls only
  * enqueue work on the caller's stream: they allocate nothing, wait for nothing
  * and keep nothing between calls, and may be captured into a graph.  Where a call
@@ -536,6 +536,84 @@ ann_status ann_layer_norm_backward(const void *dy, uint64_t dy_stride, const voi
                                    const float *mean, const float *rstd, void *dx, uint64_t dx_stride, void *dweight,
                                    void *dbias, void *workspace, uint64_t workspace_bytes, void *stream);
 uint64_t ann_layer_norm_backward_workspace(uint64_t n, uint32_t dim);
+
+/*
+ * Rows of a table of embeddings by their ids, times a scale:
+ *   y[i] = scale * table[ids[i]]; zeros where ids[i] is not below `rows` (ANN_PAD_ID: padding).
+ *   table        [rows] rows of `dim` elements of table_type: `type` or ANN_F32.
+ *   y            [n] rows of `type`.
+ * Rounded once.  n = 0 does nothing.  n < 2^31, rows <= 2^31, dim <= ANN_MAX_NORM_DIM.
+ * Errors: ANN_EINVAL (NULL arguments, types, dim == 0, strides), ANN_ECAPACITY.
+ */
+ann_status ann_embedding(const void *table, uint64_t rows, uint32_t dim, uint64_t table_stride, uint32_t table_type,
+                         const uint32_t *ids, uint64_t n, float scale, void *y, uint64_t y_stride, uint32_t type,
+                         void *stream);
+
+/*
+ * Gradient of the table:  dtable[r] = scale * sum of dy[i] over the i with ids[i] = r.
+ *   dy           [n] rows of `type`; rows of padding are not read.
+ *   dtable       [rows] rows of table_type.  accumulate == 0: every row is written, zeros
+ *                where no id names it.  Otherwise the sums are added to what is
+ *                there (in fp32, rounded once) and rows that no id names are left alone:
+ *                a table that is also scored against, or several batches.
+ * Sums are fp32 in a fixed order, of equal ids by their positions.  n = 0: as above (zeros, or nothing).
+ * Limits and errors as ann_embedding, and the workspace (ANN_EINVAL).
+ */
+ann_status ann_embedding_backward(const void *dy, uint64_t dy_stride, uint32_t type, const uint32_t *ids, uint64_t n,
+                                  float scale, uint64_t rows, uint32_t dim, void *dtable, uint64_t dtable_stride,
+                                  uint32_t table_type, uint32_t accumulate, void *workspace, uint64_t workspace_bytes,
+                                  void *stream);
+uint64_t ann_embedding_backward_workspace(uint64_t n, uint64_t rows, uint32_t dim);
+
+/*
+ * Root-mean-square norm of n rows of `dim` elements, after the residual's addition:
+ *   h = x + residual, rounded to `type` (residual NULL: h = x)
+ *   y = h * rstd * weight,  rstd = 1 / sqrt(mean(h^2) + eps).
+ *   type         of x, residual, sum and y; weight_type: of weight, `type` or ANN_F32.
+ *   weight       [dim], NULL allowed (ones).
+ *   sum          h, the residual of the next layer and what the backward pass reads;
+ *                NULL where not wanted, and without a residual.
+ *   rstd         [n] fp32, for the backward pass; NULL allowed.
+ * sum may be x or residual, y may be x or residual (same strides); sum and y are not
+ * the same rows.  n = 0 does nothing.  dim <= ANN_MAX_NORM_DIM.
+ * Errors: ANN_EINVAL (NULL x or y, dim == 0, types, strides, sum without residual or over y, eps negative
+ * or NaN), ANN_ECAPACITY.
+ */
+ann_status ann_rms_norm(const void *x, uint64_t n, uint32_t dim, uint64_t x_stride, uint32_t type, const void *residual,
+                        uint64_t residual_stride, const void *weight, uint32_t weight_type, float eps, void *sum,
+                        uint64_t sum_stride, void *y, uint64_t y_stride, float *rstd, void *stream);
+
+/*
+ * The same with y in 8 bits, for products of 8-bit elements: codes e4m3 (4 bits of
+ * exponent, 3 of mantissa, largest value 448, no infinities) with a scale to
+ * every `group` columns of a row:
+ *   scale = max(largest |v| of the group, 2^-100) / 448,  code = v / scale rounded once,  v = h * rstd * weight in fp32.
+ *   group        32, 64 or 128 columns (the last group of a row may be shorter), or 0: one scale to a row.
+ *   scales       [n] rows of ceil(dim / group) (group 0: one) fp32.
+ * y is not x or residual.  Values that are not numbers get the code for that and do not
+ * count for their group's scale.  Otherwise as ann_rms_norm; ANN_EINVAL also for
+ * another group, scales NULL or scale_stride shorter than a row's scales.
+ */
+ann_status ann_rms_norm_e4m3(const void *x, uint64_t n, uint32_t dim, uint64_t x_stride, uint32_t type,
+                             const void *residual, uint64_t residual_stride, const void *weight, uint32_t weight_type,
+                             float eps, void *sum, uint64_t sum_stride, uint8_t *y, uint64_t y_stride, uint32_t group,
+                             float *scales, uint64_t scale_stride, float *rstd, void *stream);
+
+/*
+ * Gradients of ann_rms_norm from dy, h (its sum, or x without a residual) and rstd:
+ *   dx = rstd * (a - xh * mean(a * xh)) + dsum,  a = dy * weight,  xh = h * rstd
+ *   dsum         [n] rows of `type`: the gradient that arrives at h itself, over the residual; NULL: none.
+ *   dx           [n] rows of `type`: the gradient of x, and of the residual; may be dy or dsum (same stride).
+ *   dweight      [dim] of weight_type, the sum over the rows of dy * xh in fp32 in a fixed
+ *                order; NULL where not wanted (no workspace needed).
+ * n = 0 writes zeros to dweight.  Errors as ann_rms_norm, and the workspace (ANN_EINVAL).
+ */
+ann_status ann_rms_norm_backward(const void *dy, uint64_t dy_stride, const void *h, uint64_t h_stride, uint64_t n,
+                                 uint32_t dim, uint32_t type, const void *dsum, uint64_t dsum_stride,
+                                 const void *weight, uint32_t weight_type, const float *rstd, void *dx,
+                                 uint64_t dx_stride, void *dweight, void *workspace, uint64_t workspace_bytes,
+                                 void *stream);
+uint64_t ann_rms_norm_backward_workspace(uint64_t n, uint32_t dim);
 
 /*
  * The scores of nq queries against n rows, s[i][j] = scale * <q_i, x_j> + bias_j.

@@ -34,7 +34,8 @@ EXPORTED_SYMBOLS = ["ann_sq_train", "ann_sq_train_truncated", "ann_sq_encode", "
                     "ann_search_batch", "ann_rescore", "ann_rerank", "ann_rerank_adaptive", "ann_bruteforce_topk", "ann_build_entry_table",
                     "ann_entry_scan", "ann_build_prs", "ann_build_prs_ratio", "ann_build_row_norms", "ann_schedule_queries", "ann_reserve_workspace",
                     "ann_search_batch_static", "ann_layer_norm", "ann_layer_norm_backward", "ann_row_logprobs", "ann_row_logprobs_backward",
-                    "ann_layer_norm_backward_workspace", "ann_row_logprobs_workspace", "ann_row_logprobs_backward_workspace",
+                    "ann_embedding", "ann_embedding_backward", "ann_rms_norm", "ann_rms_norm_e4m3", "ann_rms_norm_backward",
+                    "ann_embedding_backward_workspace", "ann_rms_norm_backward_workspace", "ann_layer_norm_backward_workspace", "ann_row_logprobs_workspace", "ann_row_logprobs_backward_workspace",
                     "ann_default_expansions_per_step", "ann_last_error", "ann_version"]
 
 
@@ -103,13 +104,19 @@ def _load_library() -> ctypes.CDLL:
     lib.ann_layer_norm_backward.argtypes = [vp, u64, vp, u64, u64, u32, u32, vp, u32, vp, vp, vp, u64, vp, vp, vp, u64, vp]
     lib.ann_row_logprobs.argtypes = [ctypes.POINTER(RowScores), u32, vp, vp, vp, vp, vp, vp, u64, vp]
     lib.ann_row_logprobs_backward.argtypes = [ctypes.POINTER(RowScores), vp, vp, vp, vp, vp, u64, vp, u64, vp, vp, u64, vp]
-    for name in EXPORTED_SYMBOLS[:-6]:
-        getattr(lib, name).restype = i32
+    lib.ann_embedding.argtypes = [vp, u64, u32, u64, u32, vp, u64, ctypes.c_float, vp, u64, u32, vp]
+    lib.ann_embedding_backward.argtypes = [vp, u64, u32, vp, u64, ctypes.c_float, u64, u32, vp, u64, u32, u32, vp, u64, vp]
+    lib.ann_rms_norm.argtypes = [vp, u64, u32, u64, u32, vp, u64, vp, u32, ctypes.c_float, vp, u64, vp, u64, vp, vp]
+    lib.ann_rms_norm_e4m3.argtypes = [vp, u64, u32, u64, u32, vp, u64, vp, u32, ctypes.c_float, vp, u64, vp, u64, u32, vp, u64, vp, vp]
+    lib.ann_rms_norm_backward.argtypes = [vp, u64, vp, u64, u64, u32, u32, vp, u64, vp, u32, vp, vp, u64, vp, vp, u64, vp]
+    sizes = [name for name in EXPORTED_SYMBOLS if name.endswith("_workspace") and name != "ann_reserve_workspace"]
+    for name in EXPORTED_SYMBOLS[:-3]:
+        getattr(lib, name).restype = u64 if name in sizes else i32
+    lib.ann_embedding_backward_workspace.argtypes = [u64, u64, u32]
+    lib.ann_rms_norm_backward_workspace.argtypes = [u64, u32]
     lib.ann_layer_norm_backward_workspace.argtypes = [u64, u32]
     lib.ann_row_logprobs_workspace.argtypes = [u32, u64, u32, u32, u32]
     lib.ann_row_logprobs_backward_workspace.argtypes = [u32, u64, u32, u32]
-    for name in EXPORTED_SYMBOLS[-6:-3]:
-        getattr(lib, name).restype = u64
     lib.ann_default_expansions_per_step.argtypes = [u32, u32]
     lib.ann_default_expansions_per_step.restype = u32
     lib.ann_last_error.restype = ctypes.c_char_p
@@ -277,6 +284,42 @@ def ann_layer_norm_backward(dy, dy_stride, x, x_stride, n, dim, type, weight, we
     _check(_lib.ann_layer_norm_backward(_ptr(dy), dy_stride, _ptr(x), x_stride, n, dim, type, _ptr(weight), weight_type, _ptr(mean),
                                         _ptr(rstd), _ptr(dx), dx_stride, _ptr(dweight), _ptr(dbias), _ptr(workspace), workspace_bytes,
                                         stream))
+
+
+def ann_embedding(table, rows, dim, table_stride, table_type, ids, n, scale, y, y_stride, type, stream=None):
+    _check(_lib.ann_embedding(_ptr(table), rows, dim, table_stride, table_type, _ptr(ids), n, scale, _ptr(y), y_stride, type, stream))
+
+
+def ann_embedding_backward_workspace(n, rows, dim) -> int:
+    return int(_lib.ann_embedding_backward_workspace(n, rows, dim))
+
+
+def ann_embedding_backward(dy, dy_stride, type, ids, n, scale, rows, dim, dtable, dtable_stride, table_type, accumulate=False, workspace=None,
+                           workspace_bytes=0, stream=None):
+    _check(_lib.ann_embedding_backward(_ptr(dy), dy_stride, type, _ptr(ids), n, scale, rows, dim, _ptr(dtable), dtable_stride, table_type,
+                                       int(bool(accumulate)), _ptr(workspace), workspace_bytes, stream))
+
+
+def ann_rms_norm(x, n, dim, x_stride, type, weight, weight_type, eps, y, y_stride, residual=None, residual_stride=0, sum=None, sum_stride=0,
+                 rstd=None, stream=None):
+    _check(_lib.ann_rms_norm(_ptr(x), n, dim, x_stride, type, _ptr(residual), residual_stride, _ptr(weight), weight_type, eps, _ptr(sum),
+                             sum_stride, _ptr(y), y_stride, _ptr(rstd), stream))
+
+
+def ann_rms_norm_e4m3(x, n, dim, x_stride, type, weight, weight_type, eps, y, y_stride, group, scales, scale_stride, residual=None,
+                      residual_stride=0, sum=None, sum_stride=0, rstd=None, stream=None):
+    _check(_lib.ann_rms_norm_e4m3(_ptr(x), n, dim, x_stride, type, _ptr(residual), residual_stride, _ptr(weight), weight_type, eps,
+                                  _ptr(sum), sum_stride, _ptr(y), y_stride, group, _ptr(scales), scale_stride, _ptr(rstd), stream))
+
+
+def ann_rms_norm_backward_workspace(n, dim) -> int:
+    return int(_lib.ann_rms_norm_backward_workspace(n, dim))
+
+
+def ann_rms_norm_backward(dy, dy_stride, h, h_stride, n, dim, type, weight, weight_type, rstd, dx, dx_stride, dsum=None, dsum_stride=0,
+                          dweight=None, workspace=None, workspace_bytes=0, stream=None):
+    _check(_lib.ann_rms_norm_backward(_ptr(dy), dy_stride, _ptr(h), h_stride, n, dim, type, _ptr(dsum), dsum_stride, _ptr(weight),
+                                      weight_type, _ptr(rstd), _ptr(dx), dx_stride, _ptr(dweight), _ptr(workspace), workspace_bytes, stream))
 
 
 def _row_scores(q, nq, q_stride, rows, n, row_stride, d, type, scale, row_bias, targets):

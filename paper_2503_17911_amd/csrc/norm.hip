@@ -19,45 +19,13 @@
 #include <type_traits>
 
 #include "ann_internal.hpp"
-#include "device_utils.hpp"
-#include "scalar_types.hpp"
+#include "row_pieces.hpp"
 
 namespace ann {
 
 constexpr int kItems = 4;              // pieces of a row to a lane
 constexpr uint32_t kNormBlocks = 2048; // workgroups of the forward pass at most: 8 of 256 lanes per compute unit
 constexpr uint32_t kNormParts = 512;   // partial sums of the weights' gradient at most: two workgroups per compute unit
-
-__device__ __forceinline__ float wave_sum(float v, int lanes) {
-  if (lanes >= 2) v += __int_as_float(dpp_i32<kDppQuadXor1>(__float_as_int(v)));
-  if (lanes >= 4) v += __int_as_float(dpp_i32<kDppQuadXor2>(__float_as_int(v)));
-  if (lanes >= 8) v += __int_as_float(dpp_i32<kDppRowHalfMirror>(__float_as_int(v)));
-  if (lanes >= 16) v += __int_as_float(dpp_i32<kDppRowMirror>(__float_as_int(v)));
-  if (lanes >= 32) {
-    const LanePair p = lane_pair<true>(__float_as_uint(v));
-    v = __uint_as_float(p.low) + __uint_as_float(p.high);
-  }
-  if (lanes >= 64) {
-    const LanePair p = lane_pair<false>(__float_as_uint(v));
-    v = __uint_as_float(p.low) + __uint_as_float(p.high);
-  }
-  return v;
-}
-
-// Sums of a and b over the LANES lanes that share a row; every one of them gets both.
-template <int LANES>
-__device__ __forceinline__ void row_sums(float &a, float &b, float2 *room) {
-  a = wave_sum(a, LANES < kWave ? LANES : kWave);
-  b = wave_sum(b, LANES < kWave ? LANES : kWave);
-  if constexpr (LANES > kWave) {
-    __syncthreads();  // the last row's sums have been read
-    if (threadIdx.x % kWave == 0) room[threadIdx.x / kWave] = make_float2(a, b);
-    __syncthreads();
-    a = 0.0f, b = 0.0f;
-#pragma unroll
-    for (int w = 0; w < LANES / kWave; ++w) a += room[w].x, b += room[w].y;
-  }
-}
 
 struct NormArgs {
   const void *x, *dy, *weight, *bias;

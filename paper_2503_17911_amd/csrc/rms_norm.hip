@@ -1,0 +1,500 @@
+// Root-mean-square norm of the rows of a matrix, with the residual's addition before it, and its gradients.
+//
+//   h = x + residual, rounded to the rows' type and kept;  y = h * rstd * w,  rstd = 1 / sqrt(mean(h^2) + eps)
+//   dx = rstd * (a - xh * mean(a * xh)) + dsum,  a = dy * w,  xh = h * rstd;   dw = sum over rows of dy * xh
+//
+// The norm is that of h as it is kept, so that the gradient, which reads h again, is that of the values returned.
+// In 8 bits (e4m3): v = h * rstd * w in fp32, scale = max |v| / 448 over a group of columns (or the row), code = v / scale, rounded once.
+//
+// Bound by memory: every row is read once and stays in the registers of 16, 64, 256 or 512 lanes as the pieces that were
+// loaded (of 16 bytes with any alignment: rows of odd strides are read as wide as the others); sums are fp32.  A group of columns that
+// shares a scale is 4 to 32 lanes side by side: its maximum takes two to five lane exchanges.  Gradients of the weights collect in registers, one
+// part per workgroup, added in a fixed order by a second kernel.
+#include "row_pieces.hpp"
+
+#include <type_traits>
+
+namespace ann {
+
+constexpr int kRmsItems = 4;            // pieces of a row to a lane
+constexpr uint32_t kRmsBlocks = 2048;   // workgroups of a pass over rows at most
+constexpr uint32_t kRmsParts = 512;     // partial sums of the weights' gradient at most
+constexpr float kE4m3Max = 448.0f;
+constexpr float kSmallestMax = 0x1p-100f;  // of a group, as its scale takes it: the scale and its inverse stay normal numbers
+
+struct RmsArgs {
+  const void *x, *residual, *weight, *dy;  // backward: x is h, residual dsum
+  void *sum, *y;                           // backward: y is dx
+  float *rstd, *scales, *partial;          // partial: [workgroups][dim]
+  uint64_t n, x_stride, residual_stride, sum_stride, y_stride, scale_stride, dy_stride;
+  uint32_t dim, group;
+  float eps;
+  bool weight_f32;
+};
+
+template <int LANES>
+constexpr int kRmsThreads = LANES > 256 ? LANES : 256;
+
+// The code of v / scale, of VEC values: 448 is the largest that there is, v / scale is not above it but for its rounding.
+template <int VEC>
+__device__ __forceinline__ RowPiece<uint8_t, VEC> e4m3_codes(const float (&v)[VEC], float inv) {
+  uint32_t words[VEC / 4];
+#pragma unroll
+  for (int w = 0; w < VEC / 4; ++w) {
+    int code = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * w] * inv, v[4 * w + 1] * inv, 0, false);
+    words[w] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * w + 2] * inv, v[4 * w + 3] * inv, code, true);
+  }
+  RowPiece<uint8_t, VEC> o;
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) o.v[e] = (uint8_t)(words[e / 4] >> (e % 4 * 8));
+  return o;
+}
+
+// (No __restrict__: sum may be x or residual, y may be x.)
+template <typename T, int LANES, bool E4M3>
+__global__ __launch_bounds__(kRmsThreads<LANES>) void rms_kernel(RmsArgs g) {
+  __shared__ float room[LANES > kWave ? LANES / kWave : 1];
+  constexpr int VEC = 16 / (int)sizeof(T), kGroups = kRmsThreads<LANES> / LANES;
+  typedef RowPiece<T, VEC> P;
+  const uint32_t lane = threadIdx.x % LANES;
+  float w[kRmsItems][VEC];
+#pragma unroll
+  for (int it = 0; it < kRmsItems; ++it)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      const uint32_t c = (it * LANES + lane) * VEC + e;
+      w[it][e] = g.weight && c < g.dim ? load_param<T>(g.weight, g.weight_f32, c) : 1.0f;
+    }
+  const float inv_dim = 1.0f / (float)g.dim;
+  for (uint64_t row = (uint64_t)blockIdx.x * kGroups + threadIdx.x / LANES; row < g.n; row += (uint64_t)gridDim.x * kGroups) {
+    const T *x = (const T *)g.x + row * g.x_stride;
+    P p[kRmsItems];
+#pragma unroll
+    for (int it = 0; it < kRmsItems; ++it) p[it].load(x, (it * LANES + lane) * VEC, g.dim);
+    if (g.residual) {
+      const T *residual = (const T *)g.residual + row * g.residual_stride;
+      P r[kRmsItems];
+#pragma unroll
+      for (int it = 0; it < kRmsItems; ++it) r[it].load(residual, (it * LANES + lane) * VEC, g.dim);
+#pragma unroll
+      for (int it = 0; it < kRmsItems; ++it)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) p[it].v[e] = from_f32<T>(to_f32(p[it].v[e]) + to_f32(r[it].v[e]));
+      if (g.sum) {
+        T *sum = (T *)g.sum + row * g.sum_stride;
+#pragma unroll
+        for (int it = 0; it < kRmsItems; ++it) p[it].store(sum, (it * LANES + lane) * VEC, g.dim);
+      }
+    }
+    float sq = 0.0f;
+#pragma unroll
+    for (int it = 0; it < kRmsItems; ++it)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) sq = __builtin_fmaf(to_f32(p[it].v[e]), to_f32(p[it].v[e]), sq);
+    sq = row_sum<LANES>(sq, room);
+    const float rstd = 1.0f / sqrtf(__builtin_fmaf(sq, inv_dim, g.eps));
+    if (lane == 0 && g.rstd) g.rstd[row] = rstd;
+    if constexpr (!E4M3) {
+      T *y = (T *)g.y + row * g.y_stride;
+#pragma unroll
+      for (int it = 0; it < kRmsItems; ++it) {
+        P o;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) o.v[e] = from_f32<T>(to_f32(p[it].v[e]) * rstd * w[it][e]);
+        o.store(y, (it * LANES + lane) * VEC, g.dim);
+      }
+    } else {
+      uint8_t *y = (uint8_t *)g.y + row * g.y_stride;
+      float *scales = g.scales + row * g.scale_stride;
+      float v[kRmsItems][VEC], most[kRmsItems], whole = 0.0f;
+#pragma unroll
+      for (int it = 0; it < kRmsItems; ++it) {
+        most[it] = 0.0f;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          v[it][e] = to_f32(p[it].v[e]) * rstd * w[it][e];
+          most[it] = fmaxf(most[it], fabsf(v[it][e]));
+        }
+        whole = fmaxf(whole, most[it]);
+      }
+      if (g.group == 0) whole = row_max<LANES>(whole, room);
+#pragma unroll
+      for (int it = 0; it < kRmsItems; ++it) {
+        const uint32_t c = (it * LANES + lane) * VEC;
+        const float scale = fmaxf(g.group ? lanes_max(most[it], g.group / VEC) : whole, kSmallestMax) / kE4m3Max;
+        if (g.group ? c < g.dim && c % g.group == 0 : c == 0) scales[g.group ? c / g.group : 0] = scale;
+        e4m3_codes(v[it], 1.0f / scale).store(y, c, g.dim);
+      }
+    }
+  }
+}
+
+// Rows longer than a workgroup's registers: passes over the row (all but the first find it in the L2), kept sums included: each lane
+// reads again what it wrote itself.
+template <typename T, bool E4M3>
+__global__ __launch_bounds__(1024) void rms_long_kernel(RmsArgs g) {
+  __shared__ float room[1024 / kWave];
+  constexpr int VEC = 16 / (int)sizeof(T);
+  typedef RowPiece<T, VEC> P;
+  const float inv_dim = 1.0f / (float)g.dim;
+  const uint32_t pieces = (g.dim + VEC - 1) / VEC, rounds = (pieces + 1023) / 1024;
+  for (uint64_t row = blockIdx.x; row < g.n; row += gridDim.x) {
+    const T *x = (const T *)g.x + row * g.x_stride, *residual = g.residual ? (const T *)g.residual + row * g.residual_stride : nullptr;
+    T *sum = g.sum ? (T *)g.sum + row * g.sum_stride : nullptr;
+    // h, from the rows as they came (KEPT: from the sums that are kept, which may have taken their place)
+    const auto piece = [&](uint32_t c, bool kept) {
+      P p;
+      if (kept && sum) {
+        p.load(sum, c, g.dim);
+        return p;
+      }
+      p.load(x, c, g.dim);
+      if (residual) {
+        P r;
+        r.load(residual, c, g.dim);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) p.v[e] = from_f32<T>(to_f32(p.v[e]) + to_f32(r.v[e]));
+        if (sum) p.store(sum, c, g.dim);
+      }
+      return p;
+    };
+    float sq = 0.0f;
+    for (uint32_t c = threadIdx.x * VEC; c < g.dim; c += 1024 * VEC) {
+      const P p = piece(c, false);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) sq = __builtin_fmaf(to_f32(p.v[e]), to_f32(p.v[e]), sq);
+    }
+    sq = row_sum<1024>(sq, room);
+    const float rstd = 1.0f / sqrtf(__builtin_fmaf(sq, inv_dim, g.eps));
+    if (threadIdx.x == 0 && g.rstd) g.rstd[row] = rstd;
+    const auto value = [&](const P &p, uint32_t c, int e) {
+      return to_f32(p.v[e]) * rstd * (g.weight && c + e < g.dim ? load_param<T>(g.weight, g.weight_f32, c + e) : 1.0f);
+    };
+    if constexpr (!E4M3) {
+      T *y = (T *)g.y + row * g.y_stride;
+      for (uint32_t c = threadIdx.x * VEC; c < g.dim; c += 1024 * VEC) {
+        P p = piece(c, true);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) p.v[e] = from_f32<T>(value(p, c, e));
+        p.store(y, c, g.dim);
+      }
+    } else {
+      uint8_t *y = (uint8_t *)g.y + row * g.y_stride;
+      float *scales = g.scales + row * g.scale_stride, whole = 0.0f;
+      if (g.group == 0) {
+        for (uint32_t c = threadIdx.x * VEC; c < g.dim; c += 1024 * VEC) {
+          const P p = piece(c, true);
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) whole = fmaxf(whole, fabsf(value(p, c, e)));
+        }
+        whole = row_max<1024>(whole, room);
+      }
+      for (uint32_t round = 0; round < rounds; ++round) {  // (all lanes take part in a group's maximum)
+        const uint32_t c = (round * 1024 + threadIdx.x) * VEC;
+        const bool in = c < g.dim;
+        float v[VEC], most = 0.0f;
+        P p;
+        if (in) p = piece(c, true);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          v[e] = in ? value(p, c, e) : 0.0f;
+          most = fmaxf(most, fabsf(v[e]));
+        }
+        const float scale = fmaxf(g.group ? lanes_max(most, g.group / VEC) : whole, kSmallestMax) / kE4m3Max;
+        if (in && (g.group ? c % g.group == 0 : c == 0)) scales[g.group ? c / g.group : 0] = scale;
+        if (in) e4m3_codes(v, 1.0f / scale).store(y, c, g.dim);
+      }
+    }
+  }
+}
+
+// PARAMS: the gradient of w is wanted.  (dx may be dy or dsum.)
+template <typename T, int LANES, bool PARAMS>
+__global__ __launch_bounds__(kRmsThreads<LANES>) void rms_grad_kernel(RmsArgs g) {
+  __shared__ float room[LANES > kWave ? LANES / kWave : 1];
+  constexpr int VEC = 16 / (int)sizeof(T), kGroups = kRmsThreads<LANES> / LANES;
+  typedef RowPiece<T, VEC> P;
+  const uint32_t lane = threadIdx.x % LANES;
+  float w[kRmsItems][VEC], dw[kRmsItems][VEC];
+#pragma unroll
+  for (int it = 0; it < kRmsItems; ++it)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      const uint32_t c = (it * LANES + lane) * VEC + e;
+      w[it][e] = g.weight && c < g.dim ? load_param<T>(g.weight, g.weight_f32, c) : 1.0f;
+      dw[it][e] = 0.0f;
+    }
+  const float inv_dim = 1.0f / (float)g.dim;
+  for (uint64_t row = (uint64_t)blockIdx.x * kGroups + threadIdx.x / LANES; row < g.n; row += (uint64_t)gridDim.x * kGroups) {
+    const T *h = (const T *)g.x + row * g.x_stride, *dy = (const T *)g.dy + row * g.dy_stride;
+    const float rstd = g.rstd[row];
+    P ph[kRmsItems], pd[kRmsItems], ps[kRmsItems];
+#pragma unroll
+    for (int it = 0; it < kRmsItems; ++it) ph[it].load(h, (it * LANES + lane) * VEC, g.dim), pd[it].load(dy, (it * LANES + lane) * VEC, g.dim);
+    if (g.residual) {
+      const T *dsum = (const T *)g.residual + row * g.residual_stride;
+#pragma unroll
+      for (int it = 0; it < kRmsItems; ++it) ps[it].load(dsum, (it * LANES + lane) * VEC, g.dim);
+    }
+    float along = 0.0f;
+#pragma unroll
+    for (int it = 0; it < kRmsItems; ++it)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const float xh = to_f32(ph[it].v[e]) * rstd, d = to_f32(pd[it].v[e]);
+        along = __builtin_fmaf(d * w[it][e], xh, along);
+        if constexpr (PARAMS) dw[it][e] = __builtin_fmaf(d, xh, dw[it][e]);
+      }
+    const float mean = row_sum<LANES>(along, room) * inv_dim;
+    T *dx = (T *)g.y + row * g.y_stride;
+#pragma unroll
+    for (int it = 0; it < kRmsItems; ++it) {
+      P o;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const float xh = to_f32(ph[it].v[e]) * rstd, a = to_f32(pd[it].v[e]) * w[it][e], d = __builtin_fmaf(-xh, mean, a);
+        o.v[e] = from_f32<T>(g.residual ? __builtin_fmaf(rstd, d, to_f32(ps[it].v[e])) : rstd * d);
+      }
+      o.store(dx, (it * LANES + lane) * VEC, g.dim);
+    }
+  }
+  if constexpr (PARAMS) {
+    // the groups' sums one after the other: those of a wavefront by lane exchanges, the wavefronts' in LDS
+    constexpr int kWaves = kRmsThreads<LANES> / kWave;
+    __shared__ float acc[LANES <= kWave ? kRmsItems * VEC * LANES : 1];
+    float *out = g.partial + (uint64_t)blockIdx.x * g.dim;
+    if constexpr (LANES <= kWave) {
+      for (int wave = 0; wave < kWaves; ++wave) {
+        if ((int)threadIdx.x / kWave == wave) {
+#pragma unroll
+          for (int it = 0; it < kRmsItems; ++it)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+              float v = dw[it][e];
+              if constexpr (LANES == 16) {
+                LanePair p = lane_pair<true>(__float_as_uint(v));
+                v = __uint_as_float(p.low) + __uint_as_float(p.high);
+                p = lane_pair<false>(__float_as_uint(v));
+                v = __uint_as_float(p.low) + __uint_as_float(p.high);
+              }
+              const int at = (it * LANES + (int)lane) * VEC + e;
+              if (threadIdx.x % kWave < LANES) acc[at] = wave == 0 ? v : acc[at] + v;
+            }
+        }
+        __syncthreads();
+      }
+      for (uint32_t c = threadIdx.x; c < g.dim; c += kRmsThreads<LANES>) out[c] = acc[c];
+    } else {
+#pragma unroll
+      for (int it = 0; it < kRmsItems; ++it)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const uint32_t c = (it * LANES + lane) * VEC + e;
+          if (c < g.dim) out[c] = dw[it][e];
+        }
+    }
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(1024) void rms_grad_long_kernel(RmsArgs g) {
+  __shared__ float room[1024 / kWave];
+  constexpr int VEC = 16 / (int)sizeof(T);
+  typedef RowPiece<T, VEC> P;
+  const float inv_dim = 1.0f / (float)g.dim;
+  float *out = g.partial ? g.partial + (uint64_t)blockIdx.x * g.dim : nullptr;
+  for (uint64_t row = blockIdx.x; row < g.n; row += gridDim.x) {
+    const T *h = (const T *)g.x + row * g.x_stride, *dy = (const T *)g.dy + row * g.dy_stride;
+    const T *dsum = g.residual ? (const T *)g.residual + row * g.residual_stride : nullptr;
+    T *dx = (T *)g.y + row * g.y_stride;
+    const float rstd = g.rstd[row];
+    const auto weight = [&](uint32_t c) { return g.weight && c < g.dim ? load_param<T>(g.weight, g.weight_f32, c) : 1.0f; };
+    float along = 0.0f;
+    for (uint32_t c = threadIdx.x * VEC; c < g.dim; c += 1024 * VEC) {
+      P ph, pd;
+      ph.load(h, c, g.dim), pd.load(dy, c, g.dim);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const float xh = to_f32(ph.v[e]) * rstd, d = to_f32(pd.v[e]);
+        along = __builtin_fmaf(d * weight(c + e), xh, along);
+        // the lane's own columns of the workgroup's own partial sums
+        if (out && c + e < g.dim) out[c + e] = row == blockIdx.x ? d * xh : __builtin_fmaf(d, xh, out[c + e]);
+      }
+    }
+    const float mean = row_sum<1024>(along, room) * inv_dim;
+    for (uint32_t c = threadIdx.x * VEC; c < g.dim; c += 1024 * VEC) {
+      P ph, pd, ps;
+      ph.load(h, c, g.dim), pd.load(dy, c, g.dim);
+      if (dsum) ps.load(dsum, c, g.dim);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const float xh = to_f32(ph.v[e]) * rstd, a = to_f32(pd.v[e]) * weight(c + e), d = __builtin_fmaf(-xh, mean, a);
+        pd.v[e] = from_f32<T>(dsum ? __builtin_fmaf(rstd, d, to_f32(ps.v[e])) : rstd * d);
+      }
+      pd.store(dx, c, g.dim);
+    }
+  }
+}
+
+// The partial sums of 64 columns in the order of the workgroups: 16 runs of them, 16 parts of a run on their way at a time, then the runs.
+template <typename T>
+__global__ __launch_bounds__(1024) void rms_grad_sum_kernel(const float *__restrict__ partial, uint32_t parts, uint32_t dim, void *dweight, bool f32) {
+  __shared__ float runs[16][64];
+  const uint32_t lane = threadIdx.x % 64, run = threadIdx.x / 64, c = blockIdx.x * 64 + lane;
+  float sum = 0.0f;
+  if (c < dim) {
+    const uint32_t end = (run + 1) * parts / 16;
+    for (uint32_t p = run * parts / 16; p < end; p += 16) {
+      float v[16];
+#pragma unroll
+      for (uint32_t u = 0; u < 16; ++u) v[u] = p + u < end ? partial[(uint64_t)(p + u) * dim + c] : 0.0f;
+#pragma unroll
+      for (uint32_t u = 0; u < 16; ++u) sum += v[u];
+    }
+  }
+  runs[run][lane] = sum;
+  __syncthreads();
+  if (run != 0 || c >= dim) return;
+  sum = 0.0f;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) sum += runs[r][lane];
+  store_param<T>(dweight, f32, c, sum);
+}
+
+static uint32_t rms_parts(uint64_t n) { return (uint32_t)(n / 4 < 1 ? 1 : n / 4 < kRmsParts ? n / 4 : kRmsParts); }
+
+// Launches one of the kernels above: the fewest lanes whose pieces hold the row, and that hold a group that shares a scale side by side.
+enum RmsKind { kNorm, kNormE4m3, kGrad };
+
+template <typename T, RmsKind KIND>
+static void launch_rms(const RmsArgs &g, hipStream_t st) {
+  constexpr uint32_t VEC = 16 / sizeof(T), per_lane = kRmsItems * VEC;
+  const auto run = [&](auto lanes) {
+    constexpr int L = decltype(lanes)::value;
+    constexpr int kGroups = kRmsThreads<L> / L;
+    const uint64_t want = (g.n + kGroups - 1) / kGroups;
+    const uint32_t blocks = (uint32_t)(want < kRmsBlocks ? want : kRmsBlocks);
+    if constexpr (KIND == kGrad) {
+      if (g.partial)
+        rms_grad_kernel<T, L, true><<<rms_parts(g.n), kRmsThreads<L>, 0, st>>>(g);
+      else
+        rms_grad_kernel<T, L, false><<<blocks, kRmsThreads<L>, 0, st>>>(g);
+    } else {
+      rms_kernel<T, L, KIND == kNormE4m3><<<blocks, kRmsThreads<L>, 0, st>>>(g);
+    }
+  };
+  const uint32_t rows = (uint32_t)(g.n < kRmsBlocks ? g.n : kRmsBlocks);
+  if (g.dim <= 16 * per_lane && (KIND != kNormE4m3 || g.group <= 16 * VEC))
+    run(std::integral_constant<int, 16>());
+  else if (g.dim <= 64 * per_lane)
+    run(std::integral_constant<int, 64>());
+  else if (g.dim <= 256 * per_lane)
+    run(std::integral_constant<int, 256>());
+  else if (g.dim <= 512 * per_lane)
+    run(std::integral_constant<int, 512>());
+  else if constexpr (KIND == kGrad)
+    rms_grad_long_kernel<T><<<g.partial ? rms_parts(g.n) : rows, 1024, 0, st>>>(g);
+  else
+    rms_long_kernel<T, KIND == kNormE4m3><<<rows, 1024, 0, st>>>(g);
+}
+
+template <RmsKind KIND>
+static ann_status launch_rms_typed(uint32_t type, const RmsArgs &g, hipStream_t st) {
+  if (type == ANN_F32)
+    launch_rms<float, KIND>(g, st);
+  else if (type == ANN_F16)
+    launch_rms<f16_t, KIND>(g, st);
+  else
+    launch_rms<bf16_t, KIND>(g, st);
+  ANN_HIP(hipGetLastError());
+  return ANN_OK;
+}
+
+static ann_status check_rms(const char *what, uint64_t n, uint32_t dim, uint32_t type, uint32_t weight_type, bool weight) {
+  if (type > ANN_BF16) return fail(ANN_EINVAL, "%s: unknown type %u", what, type);
+  if (weight && weight_type != type && weight_type != ANN_F32)
+    return fail(ANN_EINVAL, "%s: weights are of the rows' type or ANN_F32, not %u", what, weight_type);
+  if (dim == 0) return fail(ANN_EINVAL, "%s: dim == 0", what);
+  if (dim > ANN_MAX_NORM_DIM) return fail(ANN_ECAPACITY, "%s: dim = %u exceeds ANN_MAX_NORM_DIM = %u", what, dim, ANN_MAX_NORM_DIM);
+  if (n >= (1ull << 40)) return fail(ANN_ECAPACITY, "%s: n = %llu", what, (unsigned long long)n);
+  return ANN_OK;
+}
+
+static ann_status check_rms_rows(const char *what, const RmsArgs &g) {
+  if (!g.x || !g.y) return fail(ANN_EINVAL, "%s: NULL argument", what);
+  if (g.sum && !g.residual) return fail(ANN_EINVAL, "%s: sum without residual", what);
+  if (g.sum && g.sum == g.y) return fail(ANN_EINVAL, "%s: sum and y are the same rows", what);
+  if (g.x_stride < g.dim || g.y_stride < g.dim || (g.residual && g.residual_stride < g.dim) || (g.sum && g.sum_stride < g.dim))
+    return fail(ANN_EINVAL, "%s: a row stride is shorter than a row", what);
+  if (!(g.eps >= 0.0f)) return fail(ANN_EINVAL, "%s: eps must not be negative", what);
+  return ANN_OK;
+}
+
+}  // namespace ann
+
+using namespace ann;
+
+extern "C" ann_status ann_rms_norm(const void *x, uint64_t n, uint32_t dim, uint64_t x_stride, uint32_t type, const void *residual,
+                                   uint64_t residual_stride, const void *weight, uint32_t weight_type, float eps, void *sum, uint64_t sum_stride,
+                                   void *y, uint64_t y_stride, float *rstd, void *stream) {
+  if (ann_status s = check_rms("ann_rms_norm", n, dim, type, weight_type, weight)) return s;
+  if (n == 0) return ANN_OK;
+  RmsArgs g = {};
+  g.x = x, g.residual = residual, g.weight = weight, g.sum = sum, g.y = y, g.rstd = rstd, g.n = n, g.dim = dim, g.eps = eps;
+  g.x_stride = x_stride, g.residual_stride = residual_stride, g.sum_stride = sum_stride, g.y_stride = y_stride, g.weight_f32 = weight_type == ANN_F32;
+  if (ann_status s = check_rms_rows("ann_rms_norm", g)) return s;
+  return launch_rms_typed<kNorm>(type, g, (hipStream_t)stream);
+}
+
+extern "C" ann_status ann_rms_norm_e4m3(const void *x, uint64_t n, uint32_t dim, uint64_t x_stride, uint32_t type, const void *residual,
+                                        uint64_t residual_stride, const void *weight, uint32_t weight_type, float eps, void *sum,
+                                        uint64_t sum_stride, uint8_t *y, uint64_t y_stride, uint32_t group, float *scales, uint64_t scale_stride,
+                                        float *rstd, void *stream) {
+  if (ann_status s = check_rms("ann_rms_norm_e4m3", n, dim, type, weight_type, weight)) return s;
+  if (group != 0 && group != 32 && group != 64 && group != 128) return fail(ANN_EINVAL, "ann_rms_norm_e4m3: group = %u", group);
+  if (n == 0) return ANN_OK;
+  RmsArgs g = {};
+  g.x = x, g.residual = residual, g.weight = weight, g.sum = sum, g.y = y, g.rstd = rstd, g.n = n, g.dim = dim, g.eps = eps;
+  g.x_stride = x_stride, g.residual_stride = residual_stride, g.sum_stride = sum_stride, g.y_stride = y_stride, g.weight_f32 = weight_type == ANN_F32;
+  g.group = group, g.scales = scales, g.scale_stride = scale_stride;
+  if (ann_status s = check_rms_rows("ann_rms_norm_e4m3", g)) return s;
+  if (!scales) return fail(ANN_EINVAL, "ann_rms_norm_e4m3: scales is NULL");
+  if (y == x || y == residual) return fail(ANN_EINVAL, "ann_rms_norm_e4m3: y cannot take the place of its input");
+  if (scale_stride < (group ? (dim + group - 1) / group : 1)) return fail(ANN_EINVAL, "ann_rms_norm_e4m3: scale_stride is shorter than a row's scales");
+  return launch_rms_typed<kNormE4m3>(type, g, (hipStream_t)stream);
+}
+
+extern "C" uint64_t ann_rms_norm_backward_workspace(uint64_t n, uint32_t dim) { return n == 0 ? 0 : (uint64_t)rms_parts(n) * dim * sizeof(float); }
+
+extern "C" ann_status ann_rms_norm_backward(const void *dy, uint64_t dy_stride, const void *h, uint64_t h_stride, uint64_t n, uint32_t dim,
+                                            uint32_t type, const void *dsum, uint64_t dsum_stride, const void *weight, uint32_t weight_type,
+                                            const float *rstd, void *dx, uint64_t dx_stride, void *dweight, void *workspace,
+                                            uint64_t workspace_bytes, void *stream) {
+  if (ann_status s = check_rms("ann_rms_norm_backward", n, dim, type, weight_type, weight || dweight)) return s;
+  if (n && (!dy || !h || !rstd || !dx)) return fail(ANN_EINVAL, "ann_rms_norm_backward: NULL argument");
+  if (n && (h_stride < dim || dy_stride < dim || dx_stride < dim || (dsum && dsum_stride < dim)))
+    return fail(ANN_EINVAL, "ann_rms_norm_backward: a row stride is shorter than a row");
+  const uint64_t need = dweight ? ann_rms_norm_backward_workspace(n, dim) : 0;
+  if (need && !workspace) return fail(ANN_EINVAL, "ann_rms_norm_backward: workspace is NULL");
+  if (workspace_bytes < need)
+    return fail(ANN_EINVAL, "ann_rms_norm_backward: workspace of %llu bytes, %llu are needed", (unsigned long long)workspace_bytes,
+                (unsigned long long)need);
+  if (need && (uintptr_t)workspace % 16) return fail(ANN_EINVAL, "ann_rms_norm_backward: workspace is not aligned to 16 bytes");
+  const hipStream_t st = (hipStream_t)stream;
+  RmsArgs g = {};
+  g.x = h, g.dy = dy, g.residual = dsum, g.weight = weight, g.y = dx, g.rstd = (float *)rstd, g.partial = dweight ? (float *)workspace : nullptr;
+  g.n = n, g.x_stride = h_stride, g.dy_stride = dy_stride, g.residual_stride = dsum_stride, g.y_stride = dx_stride, g.dim = dim;
+  g.weight_f32 = weight_type == ANN_F32;
+  if (n)
+    if (ann_status s = launch_rms_typed<kGrad>(type, g, st)) return s;
+  if (!dweight) return ANN_OK;
+  const uint32_t parts = n ? rms_parts(n) : 0, grid = (dim + 63) / 64;
+  if (type == ANN_F16)
+    rms_grad_sum_kernel<f16_t><<<grid, 1024, 0, st>>>(g.partial, parts, dim, dweight, g.weight_f32);
+  else if (type == ANN_BF16)
+    rms_grad_sum_kernel<bf16_t><<<grid, 1024, 0, st>>>(g.partial, parts, dim, dweight, g.weight_f32);
+  else
+    rms_grad_sum_kernel<float><<<grid, 1024, 0, st>>>(g.partial, parts, dim, dweight, true);
+  ANN_HIP(hipGetLastError());
+  return ANN_OK;
+}
