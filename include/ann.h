@@ -551,7 +551,7 @@ ann_status ann_embedding(const void *table, uint64_t rows, uint32_t dim, uint64_
 
 /*
  * Gradient of the table:  dtable[r] = scale * sum of dy[i] over the i with ids[i] = r.
- *   dy           [n] rows of `type`; rows of padding are not read.
+ *   dy           [n] rows of `type`; rows of padding do not count, whatever they hold.
  *   dtable       [rows] rows of table_type.  accumulate == 0: every row is written, zeros
  *                where no id names it.  Otherwise the sums are added to what is
  *                there (in fp32, rounded once) and rows that no id names are left alone:

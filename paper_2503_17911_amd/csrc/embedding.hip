@@ -4,20 +4,19 @@
 //
 // Bound by memory.  Forward: a row belongs to 16 or 64 lanes, pieces of 16 bytes of the output with any alignment.  Gradient: the ids
 // are put in order with their positions (id_sort), so that a table's row is a run of entries and its sum has a fixed order; no
-// atomic that a result depends on.  Frequent ids make runs of any length, so runs do not go to lanes: a workgroup takes kChunk entries in
+// atomic that a result depends on.  Frequent ids make runs of any length, so runs do not go to lanes: lanes take a chunk of entries in
 // order, sums them in fp32 and writes the runs that lie within; the ends of runs that cross a border go to the workspace, from where a
 // second kernel joins them in the borders' order.  Rows without an id are filled with zeros beside the sums (a bit to a row
 // says which; few ids: the whole table is filled beside the sorting).
 #include "id_sort.hpp"
 #include "row_pieces.hpp"
 
-#include <type_traits>
-
 namespace ann {
 
-constexpr uint32_t kChunk = 32;           // entries that are summed one after the other
+// Entries that are summed one after the other: few where there are few in all, so that the card has work (5,003 x 100: 28 us by 32 of them).
+static uint32_t chunk_entries(uint64_t n) { return n <= 8192 ? 8 : n <= 16384 ? 16 : 32; }
 constexpr uint32_t kMostChunks = 1 << 15;  // beyond, chunks are longer
-constexpr uint32_t kFetched = 8;          // rows on their way at a time
+constexpr uint32_t kFetched = 8;         // rows on their way at a time
 
 struct EmbedArgs {
   const void *from;  // forward: the table; backward: dy
@@ -27,156 +26,217 @@ struct EmbedArgs {
   uint32_t dim;
   float scale;
   // backward
-  const uint32_t *keys, *positions, *hit;
+  const uint32_t *keys, *positions;
+  const uint8_t *hit;
   float *part;  // [chunks][2][dim]: the end of a run from the chunk before; the beginning of one that goes on in the next
   uint32_t chunk, chunks, accumulate;
 };
 
-// F: the table's type, T: of y
-template <typename F, typename T, int LANES>
-__global__ __launch_bounds__(256) void embed_kernel(EmbedArgs g) {
-  constexpr int VEC = 16 / (int)sizeof(T), kGroups = 256 / LANES, kParts = VEC * (int)sizeof(F) / 16;
+// F: the table's type, T: of y.  A group of LANES lanes takes kUnits pieces to a lane at a time, `slots` of them to a row: so many reads are on
+// their way at once (one after the other: 72 us for 80,000 x 960 fp32 to bf16).
+template <typename F, typename T, int LANES, RowEnd END>
+__global__ __launch_bounds__(256) void embed_kernel(EmbedArgs g, uint32_t slots) {
+  constexpr int VEC = 16 / (int)sizeof(T), kGroups = 256 / LANES, kParts = VEC * (int)sizeof(F) / 16, kEach = VEC / kParts, kUnits = 4;
   const uint32_t lane = threadIdx.x % LANES;
-  for (uint64_t i = (uint64_t)blockIdx.x * kGroups + threadIdx.x / LANES; i < g.n; i += (uint64_t)gridDim.x * kGroups) {
-    const uint32_t id = g.ids[i];
-    const bool there = id < g.rows;
-    const F *from = (const F *)g.from + (there ? id : 0) * g.from_stride;
-    T *to = (T *)g.to + i * g.to_stride;
-    for (uint32_t c = lane * VEC; c < g.dim; c += LANES * VEC) {
-      RowPiece<T, VEC> o;
-      if (there) {
-        RowPiece<F, VEC / kParts> v[kParts];
+  const uint64_t units = g.n * slots;
+  for (uint64_t u0 = ((uint64_t)blockIdx.x * kGroups + threadIdx.x / LANES) * kUnits; u0 < units; u0 += (uint64_t)gridDim.x * kGroups * kUnits) {
+    uint64_t row[kUnits];
+    uint32_t c[kUnits], id[kUnits];
+    row[0] = u0 / slots;
+    uint32_t slot = (uint32_t)(u0 % slots);
 #pragma unroll
-        for (int p = 0; p < kParts; ++p) v[p].load(from, c + p * (VEC / kParts), g.dim);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) o.v[e] = from_f32<T>(to_f32(v[e / (VEC / kParts)].v[e % (VEC / kParts)]) * g.scale);
-      } else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) o.v[e] = (T)0.0f;
+    for (int u = 0; u < kUnits; ++u) {
+      if (u) {
+        const bool next = ++slot == slots;
+        row[u] = row[u - 1] + next;
+        slot = next ? 0 : slot;
       }
-      o.store(to, c, g.dim);
+      c[u] = row[u] < g.n ? (slot * LANES + lane) * VEC : g.dim;
+      id[u] = g.ids[row[u] < g.n ? row[u] : g.n - 1];
+    }
+    RowPiece<F, kEach, END> v[kUnits][kParts];
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const F *from = (const F *)g.from + (id[u] < g.rows ? id[u] : 0) * g.from_stride;  // (there is a row)
+#pragma unroll
+      for (int p = 0; p < kParts; ++p) v[u][p].load(from, c[u] + p * kEach, g.dim);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      float f[VEC];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) f[e] = id[u] < g.rows ? v[u][e / kEach].get(e % kEach) * g.scale : 0.0f;
+      RowPiece<T, VEC, END> o;
+      o.set(f);
+      o.store((T *)g.to + row[u] * g.to_stride, c[u], g.dim);
     }
   }
 }
 
 // Rows of zeros; hit: but those whose bit is set.
 template <typename F>
-__global__ __launch_bounds__(256) void embed_zero_kernel(F *__restrict__ table, uint64_t rows, uint64_t stride, uint32_t dim, const uint32_t *__restrict__ hit) {
+__device__ __forceinline__ void zero_rows(F *table, uint64_t first, uint64_t end, uint64_t stride, uint32_t dim, const uint8_t *hit, uint32_t block,
+                                          uint32_t blocks) {
   constexpr int VEC = 16 / (int)sizeof(F);
+  const uint32_t waves = blockDim.x / kWave;
   RowPiece<F, VEC> zero;
-#pragma unroll
-  for (int e = 0; e < VEC; ++e) zero.v[e] = (F)0.0f;
-  for (uint64_t r = (uint64_t)blockIdx.x * 4 + threadIdx.x / 64; r < rows; r += (uint64_t)gridDim.x * 4) {
-    if (hit && hit[r / 32] >> (r % 32) & 1) continue;
-    for (uint32_t c = threadIdx.x % 64 * VEC; c < dim; c += 64 * VEC) zero.store(table + r * stride, c, dim);
+  zero.clear();
+  for (uint64_t r = first + (uint64_t)block * waves + threadIdx.x / kWave; r < end; r += (uint64_t)blocks * waves) {
+    if (hit && hit[r]) continue;
+    for (uint32_t c = threadIdx.x % kWave * VEC; c < dim; c += kWave * VEC) zero.store(table + r * stride, c, dim);
   }
 }
+template <typename F>
+__global__ __launch_bounds__(256) void embed_zero_kernel(F *table, uint64_t rows, uint64_t stride, uint32_t dim) {
+  zero_rows<F>(table, 0, rows, stride, dim, nullptr, blockIdx.x, gridDim.x);
+}
 
-template <typename F, int VEC>
+// Zeros beside the sorting: few ids, all rows, before any other is written; many, the rows that no id names, `early` of them beside the second
+// pass' counting, which is the shorter of its kernels.
+template <typename F>
+struct ZeroBeside {
+  uint32_t blocks, dim;
+  F *table;
+  uint64_t rows, early, stride;
+  const uint8_t *hit;
+  __device__ __forceinline__ void operator()(uint32_t stage, uint32_t part, uint32_t parts) const {
+    zero_rows<F>(table, stage == 2 ? early : 0, stage == 1 ? early : rows, stride, dim, stage ? hit : nullptr, part, parts);
+  }
+};
+
+template <typename F, int VEC, RowEnd END>
 __device__ __forceinline__ void write_gradient(const EmbedArgs &g, uint32_t row, uint32_t c, const float (&sum)[VEC]) {
   F *to = (F *)g.to + row * g.to_stride;
+  if constexpr (VEC == 1) {
+    to[c] = from_f32<F>(g.accumulate ? __builtin_fmaf(sum[0], g.scale, to_f32(to[c])) : sum[0] * g.scale);
+  } else {
+    constexpr int kEach = 16 / (int)sizeof(F), N = VEC < kEach ? VEC : kEach;
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) {
-    if (c + e >= g.dim) break;
-    const float old = g.accumulate ? to_f32(to[c + e]) : 0.0f;
-    to[c + e] = from_f32<F>(g.accumulate ? __builtin_fmaf(sum[e], g.scale, old) : sum[e] * g.scale);
+    for (int p = 0; p < VEC; p += N) {
+      RowPiece<F, N, END> o;
+      float v[N];
+      if (g.accumulate) o.load(to, c + p, g.dim);
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = g.accumulate ? __builtin_fmaf(sum[p + e], g.scale, o.get(e)) : sum[p + e] * g.scale;
+      o.set(v);
+      o.store(to, c + p, g.dim);
+    }
   }
 }
 
-// T: of dy, F: of the table.  A group of LANES lanes takes a chunk and LANES * VEC columns.
-template <typename T, typename F, int LANES>
-__global__ __launch_bounds__(256) void embed_grad_kernel(EmbedArgs g) {
+// T: of dy, F: of the table.  A group of LANES lanes takes a chunk and LANES * VEC columns.  Workgroups from `summing` on write zeros.
+template <typename T, typename F, int LANES, RowEnd END>
+__global__ __launch_bounds__(256) void embed_grad_kernel(EmbedArgs g, uint32_t summing) {
   constexpr int VEC = 16 / (int)sizeof(T), kGroups = 256 / LANES;
-  const uint32_t tiles = (g.dim + LANES * VEC - 1) / (LANES * VEC);
-  const uint64_t at = (uint64_t)blockIdx.x * kGroups + threadIdx.x / LANES;
-  const uint64_t chunk = at / tiles;
-  const uint32_t c = ((uint32_t)(at % tiles) * LANES + threadIdx.x % LANES) * VEC;
+  if (blockIdx.x >= summing) {
+    zero_rows<F>((F *)g.to, 0, g.rows, g.to_stride, g.dim, g.hit, blockIdx.x - summing, gridDim.x - summing);
+    return;
+  }
+  const uint32_t tiles = (g.dim + LANES * VEC - 1) / (LANES * VEC), lane = threadIdx.x % LANES;
+  const uint32_t at = blockIdx.x * kGroups + threadIdx.x / LANES, chunk = at / tiles;
+  const uint32_t c = (at % tiles * LANES + lane) * VEC;
   if (chunk >= g.chunks) return;
-  const uint64_t begin = chunk * g.chunk, end = begin + g.chunk < g.n ? begin + g.chunk : g.n;
+  const uint32_t begin = chunk * g.chunk, end = begin + g.chunk < g.n ? begin + g.chunk : (uint32_t)g.n;
   uint32_t row = g.keys[begin];
-  bool first = begin != 0 && g.keys[begin - 1] == row;  // the run began before this chunk
   const uint32_t next = end < g.n ? g.keys[end] : 0xFFFFFFFFu;
+  bool first = begin != 0 && g.keys[begin - 1] == row;  // the run began before this chunk
   float sum[VEC];
 #pragma unroll
   for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
   const auto finish = [&](bool goes_on) {
     if (row >= g.rows || c >= g.dim) return;
     if (first || goes_on) {
-      float *to = g.part + (chunk * 2 + (first ? 0 : 1)) * g.dim + c;
+      float *to = g.part + ((uint64_t)chunk * 2 + (first ? 0 : 1)) * g.dim + c;
 #pragma unroll
       for (int e = 0; e < VEC; ++e)
-        if (c + e < g.dim) to[e] = sum[e];
+        if (END == kWholePieces || c + e < g.dim) to[e] = sum[e];
     } else {
-      write_gradient<F, VEC>(g, row, c, sum);
+      write_gradient<F, VEC, END>(g, row, c, sum);
     }
   };
-  for (uint64_t i0 = begin; i0 < end; i0 += kFetched) {
-    RowPiece<T, VEC> v[kFetched];
-    uint32_t key[kFetched];
+  for (uint32_t i0 = begin; i0 < end; i0 += LANES) {
+    // an entry to a lane, handed round
+    const uint32_t mine = i0 + lane < end ? i0 + lane : end - 1;
+    const uint32_t my_key = g.keys[mine], my_position = g.positions[mine];
+    const uint32_t here = end - i0 < LANES ? end - i0 : LANES;
+    for (uint32_t u0 = 0; u0 < here; u0 += kFetched) {
+      RowPiece<T, VEC, END> v[kFetched];
+      uint32_t key[kFetched];
 #pragma unroll
-    for (uint32_t u = 0; u < kFetched; ++u) {
-      const uint64_t i = i0 + u < end ? i0 + u : end - 1;
-      key[u] = g.keys[i];
-      if (key[u] < g.rows) v[u].load((const T *)g.from + g.positions[i] * g.from_stride, c, g.dim);
-    }
-#pragma unroll
-    for (uint32_t u = 0; u < kFetched; ++u) {
-      if (i0 + u >= end || key[u] >= g.rows) continue;  // (what belongs to no row comes last)
-      if (key[u] != row) {
-        finish(false);
-        row = key[u], first = false;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
+      for (uint32_t u = 0; u < kFetched; ++u) {
+        // (behind the last entry: the last one's once more)
+        uint32_t position;
+        if constexpr (LANES == kWave) {
+          key[u] = (uint32_t)__builtin_amdgcn_readlane((int)my_key, (int)(u0 + u)), position = (uint32_t)__builtin_amdgcn_readlane((int)my_position, (int)(u0 + u));
+        } else {
+          const int from = ((int)(lane_id() / LANES * LANES) + (int)(u0 + u)) << 2;
+          key[u] = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)my_key), position = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)my_position);
+        }
+        v[u].load((const T *)g.from + position * g.from_stride, c, g.dim);
       }
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) sum[e] += to_f32(v[u].v[e]);
+      for (uint32_t u = 0; u < kFetched; ++u) {
+        if (u0 + u >= here || key[u] >= g.rows) continue;  // (what belongs to no row comes last)
+        if (key[u] != row) {
+          finish(false);
+          row = key[u], first = false;
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sum[e] += v[u].get(e);
+      }
     }
   }
   finish(row == next);
 }
 
-// Runs that cross borders between chunks, by the chunk in which they begin.  64 columns to a workgroup of four wavefronts, a run of the chunks to each.
+// Runs that cross borders between chunks, by the chunk in which they begin: 256 columns to a workgroup of four wavefronts, which share out
+// the run's chunks.
 template <typename F>
 __global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs g) {
-  __shared__ float room[4][64];
-  const uint64_t chunk = blockIdx.x;
-  const uint64_t border = (chunk + 1) * g.chunk;
-  if (border >= g.n) return;
-  const uint32_t row = g.keys[border];
-  if (row >= g.rows || g.keys[border - 1] != row) return;
-  // (the run begins in this chunk: at its first entry at the earliest)
-  const uint64_t begin = chunk * g.chunk;
-  if (begin != 0 && g.keys[begin - 1] == row) return;
-  // the chunks after this one that begin with it
-  const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  uint64_t last = chunk + 1;
+  __shared__ float room[3][256];
+  const uint32_t chunk = blockIdx.x, border = (chunk + 1) * g.chunk, begin = chunk * g.chunk;
+  // (read side by side: most workgroups end here)
+  const uint32_t before = begin ? g.keys[begin - 1] : 0xFFFFFFFFu, last_key = g.keys[border - 1], row = g.keys[border];
+  if (row >= g.rows || last_key != row || before == row) return;
+  const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = blockIdx.y * 256 + lane;
+  uint32_t last = chunk + 1;  // the last chunk that begins with the run
   for (;;) {
-    const uint64_t next = last + 1 + lane;
-    const uint64_t mine = __ballot(next < g.chunks && g.keys[next * g.chunk] == row);
-    last += __builtin_ctzll(~mine | (mine == ~0ull ? 1ull : 0ull)) + (mine == ~0ull ? 64 : 0);
-    if (mine != ~0ull) break;
+    const uint32_t next = last + 1 + lane;
+    const uint64_t with = __ballot(next < g.chunks && g.keys[next * g.chunk] == row);
+    if (with != ~0ull) {
+      last += __builtin_ctzll(~with);
+      break;
+    }
+    last += 64;
   }
-  const uint64_t count = last - chunk, from = chunk + 1 + count * wave / 4, to = chunk + 1 + count * (wave + 1) / 4;
-  for (uint32_t c0 = 0; c0 < g.dim; c0 += 64) {
-    const uint32_t c = c0 + lane;
-    float sum = 0.0f;
-    if (c < g.dim) {
-      if (wave == 0) sum = g.part[(chunk * 2 + 1) * g.dim + c];
-      for (uint64_t k = from; k < to; k += 8) {
-        float v[8];
+  const uint32_t count = last - chunk, from = chunk + 1 + (uint32_t)((uint64_t)count * wave / 4), to = chunk + 1 + (uint32_t)((uint64_t)count * (wave + 1) / 4);
+  float sum[4];
 #pragma unroll
-        for (uint32_t u = 0; u < 8; ++u) v[u] = k + u < to ? g.part[(k + u) * 2 * g.dim + c] : 0.0f;
+  for (int e = 0; e < 4; ++e) sum[e] = wave == 0 && c + e * 64 < g.dim ? g.part[((uint64_t)chunk * 2 + 1) * g.dim + c + e * 64] : 0.0f;
+  for (uint32_t k = from; k < to; k += 8) {
+    float v[8][4];
 #pragma unroll
-        for (uint32_t u = 0; u < 8; ++u) sum += v[u];
-      }
-    }
-    __syncthreads();
-    room[wave][lane] = sum;
-    __syncthreads();
-    if (wave == 0 && c < g.dim) {
-      const float total[1] = {((sum + room[1][lane]) + room[2][lane]) + room[3][lane]};
-      write_gradient<F, 1>(g, row, c, total);
-    }
+    for (uint32_t u = 0; u < 8; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[u][e] = k + u < to && c + e * 64 < g.dim ? g.part[(uint64_t)(k + u) * 2 * g.dim + c + e * 64] : 0.0f;
+#pragma unroll
+    for (uint32_t u = 0; u < 8; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += v[u][e];
+  }
+  if (wave != 0) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) room[wave - 1][lane + e * 64] = sum[e];
+  }
+  __syncthreads();
+  if (wave != 0) return;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (c + e * 64 >= g.dim) break;
+    const float total[1] = {((sum[e] + room[0][lane + e * 64]) + room[1][lane + e * 64]) + room[2][lane + e * 64]};
+    write_gradient<F, 1, kByElement>(g, row, c + e * 64, total);
   }
 }
 
@@ -190,12 +250,12 @@ static EmbedGradPlan embed_grad_plan(uint64_t n, uint64_t rows, uint32_t dim) {
   EmbedGradPlan p;
   if (n == 0) return p;
   p.sort = id_sort_plan(n, rows);
-  p.chunk = kChunk;
+  p.chunk = chunk_entries(n);
   while ((n + p.chunk - 1) / p.chunk > kMostChunks) p.chunk *= 2;
   p.chunks = (uint32_t)((n + p.chunk - 1) / p.chunk);
   p.part_at = p.sort.bytes;
   p.hit_at = p.part_at + ((uint64_t)p.chunks * 2 * dim * sizeof(float) + 255) / 256 * 256;
-  p.bytes = p.hit_at + ((rows + 31) / 32 * 4 + 255) / 256 * 256;
+  p.bytes = p.hit_at + (n > kSmallSort ? (rows + 255) / 256 * 256 : 0);
   return p;
 }
 
@@ -210,35 +270,41 @@ static ann_status check_embedding(const char *what, uint64_t n, uint64_t rows, u
 
 template <typename T, typename F>
 static ann_status embedding_backward(const EmbedGradPlan &p, EmbedArgs g, char *ws, hipStream_t st) {
-  uint32_t *hit = (uint32_t *)(ws + p.hit_at);
-  const uint32_t zero_blocks = (uint32_t)((g.rows + 3) / 4 < 4096 ? (g.rows + 3) / 4 : 4096);
-  const bool small = g.n <= kSmallSort;
-  // (few ids: all rows, before anything else is written)
-  if (!g.accumulate && g.rows && small) {
-    embed_zero_kernel<F><<<zero_blocks, 256, 0, st>>>((F *)g.to, g.rows, g.to_stride, g.dim, nullptr);
+  uint8_t *hit = (uint8_t *)(ws + p.hit_at);
+  if (g.n == 0 || g.rows == 0) {
+    if (g.rows == 0 || g.accumulate) return ANN_OK;
+    embed_zero_kernel<F><<<(uint32_t)(g.rows < 8192 ? (g.rows + 3) / 4 : 2048), 256, 0, st>>>((F *)g.to, g.rows, g.to_stride, g.dim);
     ANN_HIP(hipGetLastError());
+    return ANN_OK;
   }
-  if (g.n == 0 || g.rows == 0) return ANN_OK;
+  const bool small = g.n <= kSmallSort, beside = !g.accumulate && (small || p.sort.passes > 1), fill = !g.accumulate && !beside;
+  // (two workgroups of 512 lanes to a compute unit, beside the sort's few; with few ids as many of 1,024 lanes as have a row each lane group)
+  const uint64_t most = small ? 256 : 768, by_rows = (g.rows + (small ? 15 : 7)) / (small ? 16 : 8);
+  const uint32_t zero_blocks = (uint32_t)(by_rows < most ? by_rows : most);
+  const ZeroBeside<F> zeros = {beside ? zero_blocks : 0, g.dim, (F *)g.to, g.rows, g.rows * 2 / 5, g.to_stride, hit};
   SortedIds sorted;
-  if (ann_status s = sort_ids(p.sort, g.ids, ws, small || g.accumulate ? nullptr : hit, st, sorted)) return s;
-  if (!g.accumulate && !small) {
-    embed_zero_kernel<F><<<zero_blocks, 256, 0, st>>>((F *)g.to, g.rows, g.to_stride, g.dim, hit);
-    ANN_HIP(hipGetLastError());
-  }
-  g.keys = sorted.keys, g.positions = sorted.positions, g.part = (float *)(ws + p.part_at), g.chunk = p.chunk, g.chunks = p.chunks;
+  if (ann_status s = sort_ids(p.sort, g.ids, ws, small || g.accumulate ? nullptr : hit, zeros, st, sorted)) return s;
+  g.keys = sorted.keys, g.positions = sorted.positions, g.hit = hit, g.part = (float *)(ws + p.part_at), g.chunk = p.chunk, g.chunks = p.chunks;
   constexpr uint32_t VEC = 16 / sizeof(T);
-  const auto sums = [&](auto lanes) {
+  const auto sums = [&](auto lanes, auto end) {
     constexpr uint32_t L = decltype(lanes)::value;
     const uint64_t groups = (uint64_t)p.chunks * ((g.dim + L * VEC - 1) / (L * VEC));
-    embed_grad_kernel<T, F, L><<<(uint32_t)((groups * L + 255) / 256), 256, 0, st>>>(g);
+    const uint32_t summing = (uint32_t)((groups * L + 255) / 256);
+    embed_grad_kernel<T, F, L, decltype(end)::value><<<summing + (fill ? zero_blocks : 0), 256, 0, st>>>(g, summing);
+  };
+  const auto sums_of = [&](auto lanes) {
+    if (g.dim % VEC == 0)
+      sums(lanes, std::integral_constant<RowEnd, kWholePieces>());
+    else
+      sums(lanes, std::integral_constant<RowEnd, kShifted>());
   };
   if (g.dim <= 16 * VEC)
-    sums(std::integral_constant<int, 16>());
+    sums_of(std::integral_constant<int, 16>());
   else
-    sums(std::integral_constant<int, 64>());
+    sums_of(std::integral_constant<int, 64>());
   ANN_HIP(hipGetLastError());
   if (p.chunks > 1) {
-    embed_join_kernel<F><<<p.chunks - 1, 256, 0, st>>>(g);
+    embed_join_kernel<F><<<dim3(p.chunks - 1, (g.dim + 255) / 256), 256, 0, st>>>(g);
     ANN_HIP(hipGetLastError());
   }
   return ANN_OK;
@@ -260,14 +326,29 @@ extern "C" ann_status ann_embedding(const void *table, uint64_t rows, uint32_t d
   const auto run = [&](auto f, auto t) {
     typedef decltype(f) F;
     typedef decltype(t) T;
+    if (rows == 0) {  // (padding alone)
+      embed_zero_kernel<T><<<(uint32_t)(n < 8192 ? (n + 3) / 4 : 2048), 256, 0, st>>>((T *)y, n, y_stride, dim);
+      return;
+    }
     constexpr uint32_t VEC = 16 / sizeof(T);
-    const uint32_t lanes = dim <= 16 * VEC ? 16 : 64;
-    const uint64_t want = (n * lanes + 255) / 256;
-    const uint32_t blocks = (uint32_t)(want < 16384 ? want : 16384);
-    if (lanes == 16)
-      embed_kernel<F, T, 16><<<blocks, 256, 0, st>>>(g);
+    const auto as = [&](auto lanes, auto end) {
+      constexpr uint32_t L = decltype(lanes)::value;
+      const uint32_t slots = (dim + L * VEC - 1) / (L * VEC);
+      const uint64_t groups = (n * slots + 3) / 4, want = (groups * L + 255) / 256;
+      embed_kernel<F, T, L, decltype(end)::value><<<(uint32_t)(want < 65536 ? want : 65536), 256, 0, st>>>(g, slots);
+    };
+    const auto with_lanes = [&](auto lanes) {
+      if (dim % VEC == 0)
+        as(lanes, std::integral_constant<RowEnd, kWholePieces>());
+      else
+        as(lanes, std::integral_constant<RowEnd, kShifted>());
+    };
+    if (dim <= 16 * VEC)
+      with_lanes(std::integral_constant<int, 16>());
+    else if (dim % (64 * VEC) > 32 * VEC || dim % (64 * VEC) == 0 || dim > 512 * VEC)
+      with_lanes(std::integral_constant<int, 64>());
     else
-      embed_kernel<F, T, 64><<<blocks, 256, 0, st>>>(g);
+      with_lanes(std::integral_constant<int, 32>());
   };
   if (type == ANN_F32)
     run(0.0f, 0.0f);

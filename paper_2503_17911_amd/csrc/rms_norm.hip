@@ -16,7 +16,6 @@
 
 namespace ann {
 
-constexpr int kRmsItems = 4;            // pieces of a row to a lane
 constexpr uint32_t kRmsBlocks = 2048;   // workgroups of a pass over rows at most
 constexpr uint32_t kRmsParts = 512;     // partial sums of the weights' gradient at most
 constexpr float kE4m3Max = 448.0f;
@@ -35,31 +34,53 @@ struct RmsArgs {
 template <int LANES>
 constexpr int kRmsThreads = LANES > 256 ? LANES : 256;
 
-// The code of v / scale, of VEC values: 448 is the largest that there is, v / scale is not above it but for its rounding.
+// The codes of v / scale, of the VEC values from column c on: 448 is the largest that there is, v / scale is not above it but for its rounding.
 template <int VEC>
-__device__ __forceinline__ RowPiece<uint8_t, VEC> e4m3_codes(const float (&v)[VEC], float inv) {
-  uint32_t words[VEC / 4];
+__device__ __forceinline__ void store_codes(const float (&v)[VEC], float inv, uint8_t *row, uint32_t c, uint32_t columns) {
+  Words<VEC / 4, 1> o;
 #pragma unroll
   for (int w = 0; w < VEC / 4; ++w) {
-    int code = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * w] * inv, v[4 * w + 1] * inv, 0, false);
-    words[w] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * w + 2] * inv, v[4 * w + 3] * inv, code, true);
+    const int low = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * w] * inv, v[4 * w + 1] * inv, 0, false);
+    o.v[w] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * w + 2] * inv, v[4 * w + 3] * inv, low, true);
   }
-  RowPiece<uint8_t, VEC> o;
+  if (c + VEC <= columns) {
+    *(Words<VEC / 4, 1> *)(row + c) = o;
+  } else {
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) o.v[e] = (uint8_t)(words[e / 4] >> (e % 4 * 8));
-  return o;
+    for (int e = 0; e < VEC; ++e)
+      if (c + e < columns) row[c + e] = (uint8_t)(o.v[e / 4] >> (e % 4 * 8));
+  }
+}
+
+// 1 / sqrt(mean + eps) of a row's squares, whose sum over the row `sum` forms of values times a factor: where it leaves fp32's range, of values
+// times 2^-80 once more (all lanes of a row take the same way).
+template <typename Sum>
+__device__ __forceinline__ float row_rstd(Sum sum, float inv_dim, float eps) {
+  float sq = sum(1.0f);
+  if (sq < INFINITY || sq != sq) return 1.0f / sqrtf(__builtin_fmaf(sq, inv_dim, eps));
+  sq = sum(0x1p-80f);
+  return 0x1p-80f / sqrtf(sq * inv_dim);  // (eps is nothing beside it)
+}
+
+// x + residual, rounded once to T.
+template <typename T, int N, RowEnd END>
+__device__ __forceinline__ void add_rounded(RowPiece<T, N, END> &x, const RowPiece<T, N, END> &residual) {
+  float h[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) h[e] = x.get(e) + residual.get(e);
+  x.set(h);
 }
 
 // (No __restrict__: sum may be x or residual, y may be x.)
-template <typename T, int LANES, bool E4M3>
+template <typename T, int LANES, int ITEMS, RowEnd END, bool E4M3>
 __global__ __launch_bounds__(kRmsThreads<LANES>) void rms_kernel(RmsArgs g) {
   __shared__ float room[LANES > kWave ? LANES / kWave : 1];
   constexpr int VEC = 16 / (int)sizeof(T), kGroups = kRmsThreads<LANES> / LANES;
-  typedef RowPiece<T, VEC> P;
+  typedef RowPiece<T, VEC, END> P;
   const uint32_t lane = threadIdx.x % LANES;
-  float w[kRmsItems][VEC];
+  float w[ITEMS][VEC];
 #pragma unroll
-  for (int it = 0; it < kRmsItems; ++it)
+  for (int it = 0; it < ITEMS; ++it)
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
       const uint32_t c = (it * LANES + lane) * VEC + e;
@@ -68,62 +89,65 @@ __global__ __launch_bounds__(kRmsThreads<LANES>) void rms_kernel(RmsArgs g) {
   const float inv_dim = 1.0f / (float)g.dim;
   for (uint64_t row = (uint64_t)blockIdx.x * kGroups + threadIdx.x / LANES; row < g.n; row += (uint64_t)gridDim.x * kGroups) {
     const T *x = (const T *)g.x + row * g.x_stride;
-    P p[kRmsItems];
+    P p[ITEMS];
 #pragma unroll
-    for (int it = 0; it < kRmsItems; ++it) p[it].load(x, (it * LANES + lane) * VEC, g.dim);
+    for (int it = 0; it < ITEMS; ++it) p[it].load(x, (it * LANES + lane) * VEC, g.dim);
     if (g.residual) {
       const T *residual = (const T *)g.residual + row * g.residual_stride;
-      P r[kRmsItems];
+      P r[ITEMS];
 #pragma unroll
-      for (int it = 0; it < kRmsItems; ++it) r[it].load(residual, (it * LANES + lane) * VEC, g.dim);
+      for (int it = 0; it < ITEMS; ++it) r[it].load(residual, (it * LANES + lane) * VEC, g.dim);
 #pragma unroll
-      for (int it = 0; it < kRmsItems; ++it)
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) p[it].v[e] = from_f32<T>(to_f32(p[it].v[e]) + to_f32(r[it].v[e]));
+      for (int it = 0; it < ITEMS; ++it) add_rounded(p[it], r[it]);
       if (g.sum) {
         T *sum = (T *)g.sum + row * g.sum_stride;
 #pragma unroll
-        for (int it = 0; it < kRmsItems; ++it) p[it].store(sum, (it * LANES + lane) * VEC, g.dim);
+        for (int it = 0; it < ITEMS; ++it) p[it].store(sum, (it * LANES + lane) * VEC, g.dim);
       }
     }
-    float sq = 0.0f;
+    const float rstd = row_rstd(
+        [&](float by) {
+          float sq = 0.0f;
 #pragma unroll
-    for (int it = 0; it < kRmsItems; ++it)
+          for (int it = 0; it < ITEMS; ++it)
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) sq = __builtin_fmaf(to_f32(p[it].v[e]), to_f32(p[it].v[e]), sq);
-    sq = row_sum<LANES>(sq, room);
-    const float rstd = 1.0f / sqrtf(__builtin_fmaf(sq, inv_dim, g.eps));
+            for (int e = 0; e < VEC; ++e) sq = __builtin_fmaf(p[it].get(e) * by, p[it].get(e) * by, sq);
+          return row_sum<LANES>(sq, room);
+        },
+        inv_dim, g.eps);
     if (lane == 0 && g.rstd) g.rstd[row] = rstd;
     if constexpr (!E4M3) {
       T *y = (T *)g.y + row * g.y_stride;
 #pragma unroll
-      for (int it = 0; it < kRmsItems; ++it) {
-        P o;
+      for (int it = 0; it < ITEMS; ++it) {
+        float v[VEC];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) o.v[e] = from_f32<T>(to_f32(p[it].v[e]) * rstd * w[it][e]);
+        for (int e = 0; e < VEC; ++e) v[e] = p[it].get(e) * rstd * w[it][e];
+        P o;
+        o.set(v);
         o.store(y, (it * LANES + lane) * VEC, g.dim);
       }
     } else {
       uint8_t *y = (uint8_t *)g.y + row * g.y_stride;
       float *scales = g.scales + row * g.scale_stride;
-      float v[kRmsItems][VEC], most[kRmsItems], whole = 0.0f;
+      float v[ITEMS][VEC], most[ITEMS], whole = 0.0f;
 #pragma unroll
-      for (int it = 0; it < kRmsItems; ++it) {
+      for (int it = 0; it < ITEMS; ++it) {
         most[it] = 0.0f;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-          v[it][e] = to_f32(p[it].v[e]) * rstd * w[it][e];
+          v[it][e] = p[it].get(e) * rstd * w[it][e];
           most[it] = fmaxf(most[it], fabsf(v[it][e]));
         }
         whole = fmaxf(whole, most[it]);
       }
       if (g.group == 0) whole = row_max<LANES>(whole, room);
 #pragma unroll
-      for (int it = 0; it < kRmsItems; ++it) {
+      for (int it = 0; it < ITEMS; ++it) {
         const uint32_t c = (it * LANES + lane) * VEC;
         const float scale = fmaxf(g.group ? lanes_max(most[it], g.group / VEC) : whole, kSmallestMax) / kE4m3Max;
         if (g.group ? c < g.dim && c % g.group == 0 : c == 0) scales[g.group ? c / g.group : 0] = scale;
-        e4m3_codes(v[it], 1.0f / scale).store(y, c, g.dim);
+        store_codes(v[it], 1.0f / scale, y, c, g.dim);
       }
     }
   }
@@ -152,30 +176,34 @@ __global__ __launch_bounds__(1024) void rms_long_kernel(RmsArgs g) {
       if (residual) {
         P r;
         r.load(residual, c, g.dim);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) p.v[e] = from_f32<T>(to_f32(p.v[e]) + to_f32(r.v[e]));
+        add_rounded(p, r);
         if (sum) p.store(sum, c, g.dim);
       }
       return p;
     };
-    float sq = 0.0f;
-    for (uint32_t c = threadIdx.x * VEC; c < g.dim; c += 1024 * VEC) {
-      const P p = piece(c, false);
+    const float rstd = row_rstd(
+        [&](float by) {
+          float sq = 0.0f;
+          for (uint32_t c = threadIdx.x * VEC; c < g.dim; c += 1024 * VEC) {
+            const P p = piece(c, by != 1.0f);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) sq = __builtin_fmaf(to_f32(p.v[e]), to_f32(p.v[e]), sq);
-    }
-    sq = row_sum<1024>(sq, room);
-    const float rstd = 1.0f / sqrtf(__builtin_fmaf(sq, inv_dim, g.eps));
+            for (int e = 0; e < VEC; ++e) sq = __builtin_fmaf(p.get(e) * by, p.get(e) * by, sq);
+          }
+          return row_sum<1024>(sq, room);
+        },
+        inv_dim, g.eps);
     if (threadIdx.x == 0 && g.rstd) g.rstd[row] = rstd;
     const auto value = [&](const P &p, uint32_t c, int e) {
-      return to_f32(p.v[e]) * rstd * (g.weight && c + e < g.dim ? load_param<T>(g.weight, g.weight_f32, c + e) : 1.0f);
+      return p.get(e) * rstd * (g.weight && c + e < g.dim ? load_param<T>(g.weight, g.weight_f32, c + e) : 1.0f);
     };
     if constexpr (!E4M3) {
       T *y = (T *)g.y + row * g.y_stride;
       for (uint32_t c = threadIdx.x * VEC; c < g.dim; c += 1024 * VEC) {
         P p = piece(c, true);
+        float v[VEC];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) p.v[e] = from_f32<T>(value(p, c, e));
+        for (int e = 0; e < VEC; ++e) v[e] = value(p, c, e);
+        p.set(v);
         p.store(y, c, g.dim);
       }
     } else {
@@ -202,22 +230,22 @@ __global__ __launch_bounds__(1024) void rms_long_kernel(RmsArgs g) {
         }
         const float scale = fmaxf(g.group ? lanes_max(most, g.group / VEC) : whole, kSmallestMax) / kE4m3Max;
         if (in && (g.group ? c % g.group == 0 : c == 0)) scales[g.group ? c / g.group : 0] = scale;
-        if (in) e4m3_codes(v, 1.0f / scale).store(y, c, g.dim);
+        if (in) store_codes(v, 1.0f / scale, y, c, g.dim);
       }
     }
   }
 }
 
 // PARAMS: the gradient of w is wanted.  (dx may be dy or dsum.)
-template <typename T, int LANES, bool PARAMS>
+template <typename T, int LANES, int ITEMS, RowEnd END, bool PARAMS>
 __global__ __launch_bounds__(kRmsThreads<LANES>) void rms_grad_kernel(RmsArgs g) {
   __shared__ float room[LANES > kWave ? LANES / kWave : 1];
   constexpr int VEC = 16 / (int)sizeof(T), kGroups = kRmsThreads<LANES> / LANES;
-  typedef RowPiece<T, VEC> P;
+  typedef RowPiece<T, VEC, END> P;
   const uint32_t lane = threadIdx.x % LANES;
-  float w[kRmsItems][VEC], dw[kRmsItems][VEC];
+  float w[ITEMS][VEC], dw[ITEMS][VEC];
 #pragma unroll
-  for (int it = 0; it < kRmsItems; ++it)
+  for (int it = 0; it < ITEMS; ++it)
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
       const uint32_t c = (it * LANES + lane) * VEC + e;
@@ -228,53 +256,57 @@ __global__ __launch_bounds__(kRmsThreads<LANES>) void rms_grad_kernel(RmsArgs g)
   for (uint64_t row = (uint64_t)blockIdx.x * kGroups + threadIdx.x / LANES; row < g.n; row += (uint64_t)gridDim.x * kGroups) {
     const T *h = (const T *)g.x + row * g.x_stride, *dy = (const T *)g.dy + row * g.dy_stride;
     const float rstd = g.rstd[row];
-    P ph[kRmsItems], pd[kRmsItems], ps[kRmsItems];
+    P ph[ITEMS], pd[ITEMS], ps[ITEMS];
 #pragma unroll
-    for (int it = 0; it < kRmsItems; ++it) ph[it].load(h, (it * LANES + lane) * VEC, g.dim), pd[it].load(dy, (it * LANES + lane) * VEC, g.dim);
+    for (int it = 0; it < ITEMS; ++it) ph[it].load(h, (it * LANES + lane) * VEC, g.dim), pd[it].load(dy, (it * LANES + lane) * VEC, g.dim);
     if (g.residual) {
       const T *dsum = (const T *)g.residual + row * g.residual_stride;
 #pragma unroll
-      for (int it = 0; it < kRmsItems; ++it) ps[it].load(dsum, (it * LANES + lane) * VEC, g.dim);
+      for (int it = 0; it < ITEMS; ++it) ps[it].load(dsum, (it * LANES + lane) * VEC, g.dim);
     }
     float along = 0.0f;
 #pragma unroll
-    for (int it = 0; it < kRmsItems; ++it)
+    for (int it = 0; it < ITEMS; ++it)
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        const float xh = to_f32(ph[it].v[e]) * rstd, d = to_f32(pd[it].v[e]);
+        const float xh = ph[it].get(e) * rstd, d = pd[it].get(e);
         along = __builtin_fmaf(d * w[it][e], xh, along);
         if constexpr (PARAMS) dw[it][e] = __builtin_fmaf(d, xh, dw[it][e]);
       }
     const float mean = row_sum<LANES>(along, room) * inv_dim;
     T *dx = (T *)g.y + row * g.y_stride;
 #pragma unroll
-    for (int it = 0; it < kRmsItems; ++it) {
-      P o;
+    for (int it = 0; it < ITEMS; ++it) {
+      float v[VEC];
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        const float xh = to_f32(ph[it].v[e]) * rstd, a = to_f32(pd[it].v[e]) * w[it][e], d = __builtin_fmaf(-xh, mean, a);
-        o.v[e] = from_f32<T>(g.residual ? __builtin_fmaf(rstd, d, to_f32(ps[it].v[e])) : rstd * d);
+        const float xh = ph[it].get(e) * rstd, a = pd[it].get(e) * w[it][e], d = __builtin_fmaf(-xh, mean, a);
+        v[e] = g.residual ? __builtin_fmaf(rstd, d, ps[it].get(e)) : rstd * d;
       }
+      P o;
+      o.set(v);
       o.store(dx, (it * LANES + lane) * VEC, g.dim);
     }
   }
   if constexpr (PARAMS) {
     // the groups' sums one after the other: those of a wavefront by lane exchanges, the wavefronts' in LDS
     constexpr int kWaves = kRmsThreads<LANES> / kWave;
-    __shared__ float acc[LANES <= kWave ? kRmsItems * VEC * LANES : 1];
+    __shared__ float acc[LANES <= kWave ? ITEMS * VEC * LANES : 1];
     float *out = g.partial + (uint64_t)blockIdx.x * g.dim;
     if constexpr (LANES <= kWave) {
       for (int wave = 0; wave < kWaves; ++wave) {
         if ((int)threadIdx.x / kWave == wave) {
 #pragma unroll
-          for (int it = 0; it < kRmsItems; ++it)
+          for (int it = 0; it < ITEMS; ++it)
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
               float v = dw[it][e];
               if constexpr (LANES == 16) {
-                LanePair p = lane_pair<true>(__float_as_uint(v));
+                const LanePair p = lane_pair<true>(__float_as_uint(v));
                 v = __uint_as_float(p.low) + __uint_as_float(p.high);
-                p = lane_pair<false>(__float_as_uint(v));
+              }
+              if constexpr (LANES <= 32) {
+                const LanePair p = lane_pair<false>(__float_as_uint(v));
                 v = __uint_as_float(p.low) + __uint_as_float(p.high);
               }
               const int at = (it * LANES + (int)lane) * VEC + e;
@@ -286,7 +318,7 @@ __global__ __launch_bounds__(kRmsThreads<LANES>) void rms_grad_kernel(RmsArgs g)
       for (uint32_t c = threadIdx.x; c < g.dim; c += kRmsThreads<LANES>) out[c] = acc[c];
     } else {
 #pragma unroll
-      for (int it = 0; it < kRmsItems; ++it)
+      for (int it = 0; it < ITEMS; ++it)
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
           const uint32_t c = (it * LANES + lane) * VEC + e;
@@ -315,7 +347,7 @@ __global__ __launch_bounds__(1024) void rms_grad_long_kernel(RmsArgs g) {
       ph.load(h, c, g.dim), pd.load(dy, c, g.dim);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        const float xh = to_f32(ph.v[e]) * rstd, d = to_f32(pd.v[e]);
+        const float xh = ph.get(e) * rstd, d = pd.get(e);
         along = __builtin_fmaf(d * weight(c + e), xh, along);
         // the lane's own columns of the workgroup's own partial sums
         if (out && c + e < g.dim) out[c + e] = row == blockIdx.x ? d * xh : __builtin_fmaf(d, xh, out[c + e]);
@@ -326,11 +358,13 @@ __global__ __launch_bounds__(1024) void rms_grad_long_kernel(RmsArgs g) {
       P ph, pd, ps;
       ph.load(h, c, g.dim), pd.load(dy, c, g.dim);
       if (dsum) ps.load(dsum, c, g.dim);
+      float v[VEC];
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        const float xh = to_f32(ph.v[e]) * rstd, a = to_f32(pd.v[e]) * weight(c + e), d = __builtin_fmaf(-xh, mean, a);
-        pd.v[e] = from_f32<T>(dsum ? __builtin_fmaf(rstd, d, to_f32(ps.v[e])) : rstd * d);
+        const float xh = ph.get(e) * rstd, a = pd.get(e) * weight(c + e), d = __builtin_fmaf(-xh, mean, a);
+        v[e] = dsum ? __builtin_fmaf(rstd, d, ps.get(e)) : rstd * d;
       }
+      pd.set(v);
       pd.store(dx, c, g.dim);
     }
   }
@@ -363,39 +397,76 @@ __global__ __launch_bounds__(1024) void rms_grad_sum_kernel(const float *__restr
 
 static uint32_t rms_parts(uint64_t n) { return (uint32_t)(n / 4 < 1 ? 1 : n / 4 < kRmsParts ? n / 4 : kRmsParts); }
 
-// Launches one of the kernels above: the fewest lanes whose pieces hold the row, and that hold a group that shares a scale side by side.
+// Launches one of the kernels above: lanes and pieces to a lane that leave few of them without work, and that hold a group that shares a
+// scale side by side.
 enum RmsKind { kNorm, kNormE4m3, kGrad };
 
 template <typename T, RmsKind KIND>
 static void launch_rms(const RmsArgs &g, hipStream_t st) {
-  constexpr uint32_t VEC = 16 / sizeof(T), per_lane = kRmsItems * VEC;
-  const auto run = [&](auto lanes) {
-    constexpr int L = decltype(lanes)::value;
+  constexpr uint32_t VEC = 16 / sizeof(T);
+  const auto run_as = [&](auto lanes, auto items, auto whole) {
+    constexpr int L = decltype(lanes)::value, ITEMS = decltype(items)::value;
+    constexpr RowEnd END = decltype(whole)::value ? kWholePieces : L <= kWave ? kShifted : kByElement;
     constexpr int kGroups = kRmsThreads<L> / L;
     const uint64_t want = (g.n + kGroups - 1) / kGroups;
     const uint32_t blocks = (uint32_t)(want < kRmsBlocks ? want : kRmsBlocks);
     if constexpr (KIND == kGrad) {
       if (g.partial)
-        rms_grad_kernel<T, L, true><<<rms_parts(g.n), kRmsThreads<L>, 0, st>>>(g);
+        rms_grad_kernel<T, L, ITEMS, END, true><<<rms_parts(g.n), kRmsThreads<L>, 0, st>>>(g);
       else
-        rms_grad_kernel<T, L, false><<<blocks, kRmsThreads<L>, 0, st>>>(g);
+        rms_grad_kernel<T, L, ITEMS, END, false><<<blocks, kRmsThreads<L>, 0, st>>>(g);
     } else {
-      rms_kernel<T, L, KIND == kNormE4m3><<<blocks, kRmsThreads<L>, 0, st>>>(g);
+      rms_kernel<T, L, ITEMS, END, KIND == kNormE4m3><<<blocks, kRmsThreads<L>, 0, st>>>(g);
     }
   };
-  const uint32_t rows = (uint32_t)(g.n < kRmsBlocks ? g.n : kRmsBlocks);
-  if (g.dim <= 16 * per_lane && (KIND != kNormE4m3 || g.group <= 16 * VEC))
-    run(std::integral_constant<int, 16>());
-  else if (g.dim <= 64 * per_lane)
-    run(std::integral_constant<int, 64>());
-  else if (g.dim <= 256 * per_lane)
-    run(std::integral_constant<int, 256>());
-  else if (g.dim <= 512 * per_lane)
-    run(std::integral_constant<int, 512>());
-  else if constexpr (KIND == kGrad)
-    rms_grad_long_kernel<T><<<g.partial ? rms_parts(g.n) : rows, 1024, 0, st>>>(g);
-  else
-    rms_long_kernel<T, KIND == kNormE4m3><<<rows, 1024, 0, st>>>(g);
+  const auto run = [&](auto lanes, auto items) {
+    if (g.dim % VEC == 0)
+      run_as(lanes, items, std::true_type());
+    else
+      run_as(lanes, items, std::false_type());
+  };
+  const std::integral_constant<int, 1> i1;
+  const std::integral_constant<int, 2> i2;
+  const std::integral_constant<int, 3> i3;
+  const std::integral_constant<int, 4> i4;
+  const std::integral_constant<int, 16> l16;
+  const std::integral_constant<int, 32> l32;
+  const std::integral_constant<int, 64> l64;
+  const std::integral_constant<int, 256> l256;
+  const std::integral_constant<int, 512> l512;
+  const uint32_t pieces = (g.dim + VEC - 1) / VEC;
+  const bool side_by_side = KIND != kNormE4m3 || g.group <= 16 * VEC;  // within 16 lanes
+  if (pieces <= 16 && side_by_side)
+    run(l16, i1);
+  else if (pieces <= 32 && side_by_side)
+    run(l16, i2);
+  else if (pieces <= 64)
+    run(l32, i2);
+  else if (pieces <= 96)
+    run(l32, i3);
+  else if (pieces <= 128)
+    run(l32, i4);
+  else if (pieces <= 192)
+    run(l64, i3);
+  else if (pieces <= 256)
+    run(l64, i4);
+  else if (pieces <= 512)
+    run(l256, i2);
+  else if (pieces <= 768)
+    run(l256, i3);
+  else if (pieces <= 1024)
+    run(l256, i4);
+  else if (pieces <= 1536)
+    run(l512, i3);
+  else if (pieces <= 2048)
+    run(l512, i4);
+  else {
+    const uint32_t rows = (uint32_t)(g.n < kRmsBlocks ? g.n : kRmsBlocks);
+    if constexpr (KIND == kGrad)
+      rms_grad_long_kernel<T><<<g.partial ? rms_parts(g.n) : rows, 1024, 0, st>>>(g);
+    else
+      rms_long_kernel<T, KIND == kNormE4m3><<<rows, 1024, 0, st>>>(g);
+  }
 }
 
 template <RmsKind KIND>

@@ -1,6 +1,8 @@
 // What the operators on rows of a matrix share: sums and maxima over the lanes
 // that hold a row, and 16-byte pieces of rows of any alignment and length.
 #pragma once
+#include <type_traits>
+
 #include "ann_internal.hpp"
 #include "device_utils.hpp"
 #include "scalar_types.hpp"
@@ -83,28 +85,93 @@ __device__ __forceinline__ float row_max(float v, float *room) {
   return v;
 }
 
-// N elements from c on of a row of `columns`, with the alignment of one element: one access, or, at the row's end, one for
-// each that there is; what lies behind it is read as zero and not written.
-template <typename T, int N>
+// Elements of type T in words of 32 bits, as they lie in memory.  (Pieces are kept as words: as elements, what two branches load is taken apart
+// and put together again, at twice the registers and the time.)
+template <typename T>
+__device__ __forceinline__ float word_f32(uint32_t w, int half) {
+  if constexpr (sizeof(T) == 4)
+    return __uint_as_float(w);
+  else if constexpr (std::is_same<T, bf16_t>::value)
+    return __uint_as_float(half ? w & 0xFFFF0000u : w << 16);
+  else
+    return to_f32(__builtin_bit_cast(T, (uint16_t)(half ? w >> 16 : w)));
+}
+template <typename T>
+__device__ __forceinline__ uint32_t f32_word(float a, float b) {
+  return (uint32_t)__builtin_bit_cast(uint16_t, from_f32<T>(a)) | (uint32_t)__builtin_bit_cast(uint16_t, from_f32<T>(b)) << 16;
+}
+
+// N words at any address that ALIGN divides.
+template <int N, int ALIGN>
+struct __attribute__((packed, aligned(ALIGN), may_alias)) Words {
+  uint32_t v[N];
+};
+
+// How a row ends: with a whole piece; within one, which is read as the row's last N elements and shifted into place (reads stay in
+// flight side by side; rows shorter than a piece element by element); within one that is read element by element
+// (no element is read by two lanes: for rows in place that several wavefronts share).
+enum RowEnd { kWholePieces, kShifted, kByElement };
+
+// N elements from c on of a row of `columns`, with the alignment of one element; what lies behind the row is read as zero and not written.
+template <typename T, int N, RowEnd END = kByElement>
 struct RowPiece {
-  T v[N];
-  __device__ __forceinline__ void load(const T *row, uint32_t c, uint32_t columns) {
-    typedef Piece<T, N, sizeof(T)> P;
-    if (c + N <= columns) {
-      *(P *)v = *(const P *)(row + c);
-    } else {
+  static constexpr int kPer = 4 / (int)sizeof(T), kWords = N / kPer;  // elements to a word
+  typedef Words<kWords, sizeof(T)> P;
+  typedef typename std::conditional<sizeof(T) == 4, uint32_t, uint16_t>::type U __attribute__((may_alias));
+  uint32_t w[kWords];
+  __device__ __forceinline__ float get(int e) const { return word_f32<T>(w[e / kPer], e % kPer); }
+  __device__ __forceinline__ void set(const float (&v)[N]) {
 #pragma unroll
-      for (int e = 0; e < N; ++e) v[e] = c + e < columns ? row[c + e] : (T)0.0f;
+    for (int k = 0; k < kWords; ++k) {
+      if constexpr (kPer == 1)
+        w[k] = __float_as_uint(v[k]);
+      else
+        w[k] = f32_word<T>(v[2 * k], v[2 * k + 1]);
+    }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int k = 0; k < kWords; ++k) w[k] = 0;
+  }
+  __device__ __forceinline__ void read(const T *at) {
+    const P p = *(const P *)at;
+#pragma unroll
+    for (int k = 0; k < kWords; ++k) w[k] = p.v[k];
+  }
+  __device__ __forceinline__ void load(const T *row, uint32_t c, uint32_t columns) {
+    if (END == kShifted && columns >= N) {
+      const uint32_t from = c + N <= columns ? c : columns - N, by = c - from;  // by elements, N and more: nothing is left
+      read(row + from);
+#pragma unroll
+      for (int step = 1; step <= kWords; step *= 2)
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) w[k] = by / kPer & step ? (k + step < kWords ? w[k + step < kWords ? k + step : 0] : 0) : w[k];
+      if constexpr (kPer == 2) {
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) w[k] = by & 1 ? __builtin_amdgcn_alignbit(k + 1 < kWords ? w[k + 1 < kWords ? k + 1 : 0] : 0, w[k], 16) : w[k];
+      }
+      if (by >= N) clear();
+    } else if (END == kWholePieces ? c < columns : c + N <= columns) {
+      read(row + c);
+    } else {
+      clear();
+      if (END != kWholePieces && c < columns) {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (c + e < columns) w[e / kPer] |= (uint32_t)((const U *)row)[c + e] << (e % kPer * 16);
+      }
     }
   }
   __device__ __forceinline__ void store(T *row, uint32_t c, uint32_t columns) const {
-    typedef Piece<T, N, sizeof(T)> P;
-    if (c + N <= columns) {
-      *(P *)(row + c) = *(const P *)v;
-    } else {
+    if (END == kWholePieces ? c < columns : c + N <= columns) {
+      P p;
+#pragma unroll
+      for (int k = 0; k < kWords; ++k) p.v[k] = w[k];
+      *(P *)(row + c) = p;
+    } else if (END != kWholePieces && c < columns) {
 #pragma unroll
       for (int e = 0; e < N; ++e)
-        if (c + e < columns) row[c + e] = v[e];
+        if (c + e < columns) ((U *)row)[c + e] = (U)(w[e / kPer] >> (e % kPer * 16));
     }
   }
 };

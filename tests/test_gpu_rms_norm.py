@@ -135,11 +135,11 @@ def test_in_place_and_nothing_between_rows_is_written(d, dtype):
 def test_rows_of_zeros_tiny_rows_and_rows_that_are_not_numbers(group):
     import paper_2503_17911_amd as ann
     n, d = 6, 300
-    x = torch.randn(n, d)
+    x = torch.randn(n, d, generator=torch.Generator().manual_seed(4))
     x[1] = 0.0
     x[2] = 1e-30                    # with eps: the values stay that small
     x[3, 5] = float("nan")
-    x[4] *= 1e18                    # (squares below fp32's largest)
+    x[4] *= 1e18                    # (the squares' sum is at the end of fp32's range)
     xd = x.cuda()
     codes, rstd = torch.empty(n, d, dtype=torch.uint8, device="cuda"), torch.empty(n, device="cuda")
     groups = 1 if group == 0 else -(-d // group)
@@ -153,6 +153,27 @@ def test_rows_of_zeros_tiny_rows_and_rows_that_are_not_numbers(group):
         # (the group's largest has the code 448: its step is 32 scales)
         assert ((v[row] - want[row]).abs() <= 2.0 ** -4 * (1 + 1e-5) * want[row].abs() + 2.0 ** -10 * sc[row].max().item()).all()
         assert (v[row].abs().max() - want[row].abs().max()).abs() <= 1e-5 * want[row].abs().max()
+
+
+@pytest.mark.parametrize("d", [100, 5000, 20_000])
+def test_rows_whose_squares_leave_the_range(d):
+    import paper_2503_17911_amd as ann
+    x = torch.randn(4, d, generator=torch.Generator().manual_seed(4))
+    x[1] *= 1e25
+    x[2] *= 5e37
+    x[3, 7] = float("inf")
+    for t, T in ((torch.float32, ann.F32), (torch.bfloat16, ann.BF16)):
+        xt = x.to(t)
+        y, rstd = torch.empty(4, d, dtype=t, device="cuda"), torch.empty(4, device="cuda")
+        ann.ann_rms_norm(xt.cuda(), 4, d, d, T, None, T, 1e-6, y, d, rstd=rstd, stream=stream())
+        want, rstd64 = E.rms_norm(xt, None, 1e-6)
+        # (1 / 5e37 is below fp32's normal numbers: 2^-150 of rounding)
+        assert ((rstd[:3].cpu().double() - rstd64[:3]).abs() <= CHAIN * R.U32 * rstd64[:3] + 2.0 ** -150).all()
+        off = (CHAIN * R.U32 + 2.0 ** -150 / rstd64[:3, None]) * 2 + R.half_step(t)
+        assert ((y[:3].cpu().double() - want[:3]).abs() <= off * want[:3].abs()).all()
+        # a row with an infinite element: nothing of the others is left
+        got = y[3].cpu()
+        assert got[7].isnan() and (got[:7] == 0).all() and (got[8:] == 0).all() and rstd[3] == 0
 
 
 def test_every_code_is_the_nearest():
