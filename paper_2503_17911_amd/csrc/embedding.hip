@@ -2,34 +2,20 @@
 //
 //   y[i] = scale * table[ids[i]];   dtable[r] = scale * sum over i with ids[i] = r of dy[i]
 //
-// Bound by memory.  Forward: a row belongs to 16 or 64 lanes, pieces of 16 bytes of the output with any alignment.  Gradient: the ids
-// are put in order with their positions (id_sort), so that a table's row is a run of entries and its sum has a fixed order; no
-// atomic that a result depends on.  Frequent ids make runs of any length, so runs do not go to lanes: lanes take a chunk of entries in
-// order, sums them in fp32 and writes the runs that lie within; the ends of runs that cross a border go to the workspace, from where a
-// second kernel joins them in the borders' order.  Rows without an id are filled with zeros beside the sums (a bit to a row
-// says which; few ids: the whole table is filled beside the sorting).
-#include "id_sort.hpp"
-#include "row_pieces.hpp"
+// Bound by memory.  Forward: a row belongs to 16, 32 or 64 lanes, pieces of 16 bytes of the output with any alignment.  Gradient: the ids
+// are put in order with their positions (id_sort.hpp), so that a table's row is the sum of a run of entries (row_runs.hpp).  Rows without an id are filled
+// with zeros beside the sorting, which leaves most of the card idle: with few ids the whole table, with many what the first pass over the ids found no id for.
+#include "row_runs.hpp"
 
 namespace ann {
-
-// Entries that are summed one after the other: few where there are few in all, so that the card has work (5,003 x 100: 28 us by 32 of them).
-static uint32_t chunk_entries(uint64_t n) { return n <= 8192 ? 8 : n <= 16384 ? 16 : 32; }
-constexpr uint32_t kMostChunks = 1 << 15;  // beyond, chunks are longer
-constexpr uint32_t kFetched = 8;         // rows on their way at a time
 
 struct EmbedArgs {
   const void *from;  // forward: the table; backward: dy
   void *to;          // forward: y; backward: dtable
   const uint32_t *ids;
   uint64_t n, rows, from_stride, to_stride;
-  uint32_t dim;
+  uint32_t dim, accumulate;
   float scale;
-  // backward
-  const uint32_t *keys, *positions;
-  const uint8_t *hit;
-  float *part;  // [chunks][2][dim]: the end of a run from the chunk before; the beginning of one that goes on in the next
-  uint32_t chunk, chunks, accumulate;
 };
 
 // F: the table's type, T: of y.  A group of LANES lanes takes kUnits pieces to a lane at a time, `slots` of them to a row: so many reads are on
@@ -104,145 +90,46 @@ struct ZeroBeside {
   }
 };
 
-template <typename F, int VEC, RowEnd END>
-__device__ __forceinline__ void write_gradient(const EmbedArgs &g, uint32_t row, uint32_t c, const float (&sum)[VEC]) {
-  F *to = (F *)g.to + row * g.to_stride;
-  if constexpr (VEC == 1) {
-    to[c] = from_f32<F>(g.accumulate ? __builtin_fmaf(sum[0], g.scale, to_f32(to[c])) : sum[0] * g.scale);
-  } else {
-    constexpr int kEach = 16 / (int)sizeof(F), N = VEC < kEach ? VEC : kEach;
-#pragma unroll
-    for (int p = 0; p < VEC; p += N) {
-      RowPiece<F, N, END> o;
-      float v[N];
-      if (g.accumulate) o.load(to, c + p, g.dim);
-#pragma unroll
-      for (int e = 0; e < N; ++e) v[e] = g.accumulate ? __builtin_fmaf(sum[p + e], g.scale, o.get(e)) : sum[p + e] * g.scale;
-      o.set(v);
-      o.store(to, c + p, g.dim);
-    }
-  }
-}
-
-// T: of dy, F: of the table.  A group of LANES lanes takes a chunk and LANES * VEC columns.  Workgroups from `summing` on write zeros.
-template <typename T, typename F, int LANES, RowEnd END>
-__global__ __launch_bounds__(256) void embed_grad_kernel(EmbedArgs g, uint32_t summing) {
-  constexpr int VEC = 16 / (int)sizeof(T), kGroups = 256 / LANES;
-  if (blockIdx.x >= summing) {
-    zero_rows<F>((F *)g.to, 0, g.rows, g.to_stride, g.dim, g.hit, blockIdx.x - summing, gridDim.x - summing);
-    return;
-  }
-  const uint32_t tiles = (g.dim + LANES * VEC - 1) / (LANES * VEC), lane = threadIdx.x % LANES;
-  const uint32_t at = blockIdx.x * kGroups + threadIdx.x / LANES, chunk = at / tiles;
-  const uint32_t c = (at % tiles * LANES + lane) * VEC;
-  if (chunk >= g.chunks) return;
-  const uint32_t begin = chunk * g.chunk, end = begin + g.chunk < g.n ? begin + g.chunk : (uint32_t)g.n;
-  uint32_t row = g.keys[begin];
-  const uint32_t next = end < g.n ? g.keys[end] : 0xFFFFFFFFu;
-  bool first = begin != 0 && g.keys[begin - 1] == row;  // the run began before this chunk
-  float sum[VEC];
-#pragma unroll
-  for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
-  const auto finish = [&](bool goes_on) {
-    if (row >= g.rows || c >= g.dim) return;
-    if (first || goes_on) {
-      float *to = g.part + ((uint64_t)chunk * 2 + (first ? 0 : 1)) * g.dim + c;
-#pragma unroll
-      for (int e = 0; e < VEC; ++e)
-        if (END == kWholePieces || c + e < g.dim) to[e] = sum[e];
+// What the sums of dy over runs of equal ids are and where they go.  T: of dy, F: of the table.
+template <typename T, typename F>
+struct TableGradient {
+  static constexpr bool kWeighted = false, kScalar = false;
+  const T *dy;
+  F *table;
+  const uint8_t *hit;
+  uint64_t dy_stride, stride, rows;
+  uint32_t dim, accumulate;
+  float scale;
+  __device__ __forceinline__ const T *row(uint32_t position) const { return dy + position * dy_stride; }
+  __device__ __forceinline__ float weight(uint32_t) const { return 1.0f; }
+  __device__ __forceinline__ float scalar(uint32_t) const { return 0.0f; }
+  __device__ __forceinline__ void write_scalar(uint32_t, uint32_t, float) const {}
+  __device__ __forceinline__ void beside(uint32_t block, uint32_t blocks) const { zero_rows<F>(table, 0, rows, stride, dim, hit, block, blocks); }
+  template <int VEC, RowEnd END>
+  __device__ __forceinline__ void write(uint32_t id, uint32_t, uint32_t c, const float (&sum)[VEC]) const {
+    F *to = table + id * stride;
+    if constexpr (VEC == 1) {
+      to[c] = from_f32<F>(accumulate ? __builtin_fmaf(sum[0], scale, to_f32(to[c])) : sum[0] * scale);
     } else {
-      write_gradient<F, VEC, END>(g, row, c, sum);
-    }
-  };
-  for (uint32_t i0 = begin; i0 < end; i0 += LANES) {
-    // an entry to a lane, handed round
-    const uint32_t mine = i0 + lane < end ? i0 + lane : end - 1;
-    const uint32_t my_key = g.keys[mine], my_position = g.positions[mine];
-    const uint32_t here = end - i0 < LANES ? end - i0 : LANES;
-    for (uint32_t u0 = 0; u0 < here; u0 += kFetched) {
-      RowPiece<T, VEC, END> v[kFetched];
-      uint32_t key[kFetched];
+      constexpr int kEach = 16 / (int)sizeof(F), N = VEC < kEach ? VEC : kEach;
 #pragma unroll
-      for (uint32_t u = 0; u < kFetched; ++u) {
-        // (behind the last entry: the last one's once more)
-        uint32_t position;
-        if constexpr (LANES == kWave) {
-          key[u] = (uint32_t)__builtin_amdgcn_readlane((int)my_key, (int)(u0 + u)), position = (uint32_t)__builtin_amdgcn_readlane((int)my_position, (int)(u0 + u));
-        } else {
-          const int from = ((int)(lane_id() / LANES * LANES) + (int)(u0 + u)) << 2;
-          key[u] = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)my_key), position = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)my_position);
-        }
-        v[u].load((const T *)g.from + position * g.from_stride, c, g.dim);
-      }
+      for (int p = 0; p < VEC; p += N) {
+        // (a piece at the row's end is read element by element: what another lane writes is not read)
+        RowPiece<F, N, END == kWholePieces ? kWholePieces : kByElement> o;
+        float v[N];
+        if (accumulate) o.load(to, c + p, dim);
 #pragma unroll
-      for (uint32_t u = 0; u < kFetched; ++u) {
-        if (u0 + u >= here || key[u] >= g.rows) continue;  // (what belongs to no row comes last)
-        if (key[u] != row) {
-          finish(false);
-          row = key[u], first = false;
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
-        }
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) sum[e] += v[u].get(e);
+        for (int e = 0; e < N; ++e) v[e] = accumulate ? __builtin_fmaf(sum[p + e], scale, o.get(e)) : sum[p + e] * scale;
+        o.set(v);
+        o.store(to, c + p, dim);
       }
     }
   }
-  finish(row == next);
-}
-
-// Runs that cross borders between chunks, by the chunk in which they begin: 256 columns to a workgroup of four wavefronts, which share out
-// the run's chunks.
-template <typename F>
-__global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs g) {
-  __shared__ float room[3][256];
-  const uint32_t chunk = blockIdx.x, border = (chunk + 1) * g.chunk, begin = chunk * g.chunk;
-  // (read side by side: most workgroups end here)
-  const uint32_t before = begin ? g.keys[begin - 1] : 0xFFFFFFFFu, last_key = g.keys[border - 1], row = g.keys[border];
-  if (row >= g.rows || last_key != row || before == row) return;
-  const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = blockIdx.y * 256 + lane;
-  uint32_t last = chunk + 1;  // the last chunk that begins with the run
-  for (;;) {
-    const uint32_t next = last + 1 + lane;
-    const uint64_t with = __ballot(next < g.chunks && g.keys[next * g.chunk] == row);
-    if (with != ~0ull) {
-      last += __builtin_ctzll(~with);
-      break;
-    }
-    last += 64;
-  }
-  const uint32_t count = last - chunk, from = chunk + 1 + (uint32_t)((uint64_t)count * wave / 4), to = chunk + 1 + (uint32_t)((uint64_t)count * (wave + 1) / 4);
-  float sum[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) sum[e] = wave == 0 && c + e * 64 < g.dim ? g.part[((uint64_t)chunk * 2 + 1) * g.dim + c + e * 64] : 0.0f;
-  for (uint32_t k = from; k < to; k += 8) {
-    float v[8][4];
-#pragma unroll
-    for (uint32_t u = 0; u < 8; ++u)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[u][e] = k + u < to && c + e * 64 < g.dim ? g.part[(uint64_t)(k + u) * 2 * g.dim + c + e * 64] : 0.0f;
-#pragma unroll
-    for (uint32_t u = 0; u < 8; ++u)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[e] += v[u][e];
-  }
-  if (wave != 0) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) room[wave - 1][lane + e * 64] = sum[e];
-  }
-  __syncthreads();
-  if (wave != 0) return;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (c + e * 64 >= g.dim) break;
-    const float total[1] = {((sum[e] + room[0][lane + e * 64]) + room[1][lane + e * 64]) + room[2][lane + e * 64]};
-    write_gradient<F, 1, kByElement>(g, row, c + e * 64, total);
-  }
-}
+};
 
 struct EmbedGradPlan {
   IdSortPlan sort;
-  uint32_t chunk = 0, chunks = 0;
+  RunsPlan runs;
   uint64_t part_at = 0, hit_at = 0, bytes = 0;
 };
 
@@ -250,11 +137,9 @@ static EmbedGradPlan embed_grad_plan(uint64_t n, uint64_t rows, uint32_t dim) {
   EmbedGradPlan p;
   if (n == 0) return p;
   p.sort = id_sort_plan(n, rows);
-  p.chunk = chunk_entries(n);
-  while ((n + p.chunk - 1) / p.chunk > kMostChunks) p.chunk *= 2;
-  p.chunks = (uint32_t)((n + p.chunk - 1) / p.chunk);
+  p.runs = runs_plan(n, dim);
   p.part_at = p.sort.bytes;
-  p.hit_at = p.part_at + ((uint64_t)p.chunks * 2 * dim * sizeof(float) + 255) / 256 * 256;
+  p.hit_at = p.part_at + p.runs.part_bytes;
   p.bytes = p.hit_at + (n > kSmallSort ? (rows + 255) / 256 * 256 : 0);
   return p;
 }
@@ -284,30 +169,9 @@ static ann_status embedding_backward(const EmbedGradPlan &p, EmbedArgs g, char *
   const ZeroBeside<F> zeros = {beside ? zero_blocks : 0, g.dim, (F *)g.to, g.rows, g.rows * 2 / 5, g.to_stride, hit};
   SortedIds sorted;
   if (ann_status s = sort_ids(p.sort, g.ids, ws, small || g.accumulate ? nullptr : hit, zeros, st, sorted)) return s;
-  g.keys = sorted.keys, g.positions = sorted.positions, g.hit = hit, g.part = (float *)(ws + p.part_at), g.chunk = p.chunk, g.chunks = p.chunks;
-  constexpr uint32_t VEC = 16 / sizeof(T);
-  const auto sums = [&](auto lanes, auto end) {
-    constexpr uint32_t L = decltype(lanes)::value;
-    const uint64_t groups = (uint64_t)p.chunks * ((g.dim + L * VEC - 1) / (L * VEC));
-    const uint32_t summing = (uint32_t)((groups * L + 255) / 256);
-    embed_grad_kernel<T, F, L, decltype(end)::value><<<summing + (fill ? zero_blocks : 0), 256, 0, st>>>(g, summing);
-  };
-  const auto sums_of = [&](auto lanes) {
-    if (g.dim % VEC == 0)
-      sums(lanes, std::integral_constant<RowEnd, kWholePieces>());
-    else
-      sums(lanes, std::integral_constant<RowEnd, kShifted>());
-  };
-  if (g.dim <= 16 * VEC)
-    sums_of(std::integral_constant<int, 16>());
-  else
-    sums_of(std::integral_constant<int, 64>());
-  ANN_HIP(hipGetLastError());
-  if (p.chunks > 1) {
-    embed_join_kernel<F><<<dim3(p.chunks - 1, (g.dim + 255) / 256), 256, 0, st>>>(g);
-    ANN_HIP(hipGetLastError());
-  }
-  return ANN_OK;
+  const Runs runs = {sorted.keys, sorted.positions, (uint32_t)g.n, (uint32_t)g.rows, p.runs.chunk, p.runs.chunks, g.dim, (float *)(ws + p.part_at), g.dim};
+  const TableGradient<T, F> work = {(const T *)g.from, (F *)g.to, hit, g.from_stride, g.to_stride, g.rows, g.dim, g.accumulate, g.scale};
+  return sum_runs<T>(runs, work, fill ? zero_blocks : 0, st);
 }
 
 }  // namespace ann
