@@ -698,6 +698,48 @@ ann_status ann_row_logprobs_backward(const ann_row_scores *scores, const float *
 uint64_t ann_row_logprobs_backward_workspace(uint32_t nq, uint64_t n, uint32_t d, uint32_t type);
 
 /*
+ * Distillation: the loss that a model is trained with where another, its teacher, says what it
+ * answers: k rows and their log probabilities for every query, such as the alternatives
+ * that ann_row_logprobs gives for the teacher's queries (over the teacher's rows, the same in number and order).
+ *   given_ids, given_logprobs  [nq][k]; entries whose id is not below n (ANN_PAD_ID)
+ *                or whose log probability is -infinity do not count.
+ *   loss[i]      = sum_e t_ie (given_logprobs[i][e] - logprobs[i][e]),  t = exp(given_logprobs);
+ *                the divergence of the softmax over all rows from the teacher's, as far as its list goes.
+ *                +infinity where a row that counts is left out; 0 where none counts.
+ *   lse[i]       as ann_row_logprobs returns it.
+ *   logprobs     [nq][k] the log probabilities of the given rows under the softmax of all rows'
+ *                scores; 0 where the id is not below n, -infinity where the row is left out.
+ * The teacher's temperature is in its log probabilities, this model's in `scale`.  The weights
+ * t need not sum to one.  A row may be given twice: its weights add.
+ * scores->targets is NULL.  1 <= k <= ANN_MAX_ALTERNATIVES.  What ann_row_logprobs says of scores that
+ * are not finite holds here; sums of the loss are fp64.  nq = 0 does nothing.
+ * Errors as ann_row_logprobs.
+ */
+ann_status ann_row_distillation(const ann_row_scores *scores, uint32_t k, const uint32_t *given_ids,
+                                const float *given_logprobs, float *loss, float *lse, float *logprobs, void *workspace,
+                                uint64_t workspace_bytes, void *stream);
+uint64_t ann_row_distillation_workspace(uint32_t nq, uint64_t n, uint32_t d, uint32_t type, uint32_t k);
+
+/*
+ * Gradients of  sum_i g_loss[i] * loss[i]  from the forward pass' lse and logprobs; with T_i = sum_e t_ie,
+ *   G[i][j] = g_loss[i] (T_i p[i][j] - sum of t_ie over the e with given_ids[i][e] = j)
+ *   dq[i]    = scale * sum_j G[i][j] x_j         drows[j] = scale * sum_i G[i][j] q_i
+ *   drow_bias[j] = sum_i G[i][j]
+ * dq, drows (of `type`, with their strides) and drow_bias ([n] fp32) each may be NULL where not wanted.
+ * The part of G that all rows have is rounded and multiplied as ann_row_logprobs_backward
+ * does it (power of two of f16: by the largest finite |g_loss T|); that of the given rows is added in fp32,
+ * with what the rounding left at these rows.  Rows left out get zero, a query whose lse is -infinity too.
+ * The workspace holds a number to a row and sums of fp32 rows for the smaller of n and nq * k of them,
+ * beside what ann_row_logprobs_backward asks for.  Errors as ann_row_distillation.
+ */
+ann_status ann_row_distillation_backward(const ann_row_scores *scores, uint32_t k, const uint32_t *given_ids,
+                                         const float *given_logprobs, const float *lse, const float *logprobs,
+                                         const float *g_loss, void *dq, uint64_t dq_stride, void *drows,
+                                         uint64_t drows_stride, float *drow_bias, void *workspace,
+                                         uint64_t workspace_bytes, void *stream);
+uint64_t ann_row_distillation_backward_workspace(uint32_t nq, uint64_t n, uint32_t d, uint32_t type, uint32_t k);
+
+/*
  * The number of expansions per step that mode 1 uses when
  * ann_search_params.expansions_per_step is 0, for a pool of ef entries on a
  * graph of the given degree (the multi-expansion mode is this library's own,

@@ -35,7 +35,8 @@ EXPORTED_SYMBOLS = ["ann_sq_train", "ann_sq_train_truncated", "ann_sq_encode", "
                     "ann_entry_scan", "ann_build_prs", "ann_build_prs_ratio", "ann_build_row_norms", "ann_schedule_queries", "ann_reserve_workspace",
                     "ann_search_batch_static", "ann_layer_norm", "ann_layer_norm_backward", "ann_row_logprobs", "ann_row_logprobs_backward",
                     "ann_embedding", "ann_embedding_backward", "ann_rms_norm", "ann_rms_norm_e4m3", "ann_rms_norm_backward",
-                    "ann_embedding_backward_workspace", "ann_rms_norm_backward_workspace", "ann_layer_norm_backward_workspace", "ann_row_logprobs_workspace", "ann_row_logprobs_backward_workspace",
+                    "ann_row_distillation", "ann_row_distillation_backward", "ann_row_distillation_workspace",
+                    "ann_row_distillation_backward_workspace", "ann_embedding_backward_workspace", "ann_rms_norm_backward_workspace", "ann_layer_norm_backward_workspace", "ann_row_logprobs_workspace", "ann_row_logprobs_backward_workspace",
                     "ann_default_expansions_per_step", "ann_last_error", "ann_version"]
 
 
@@ -114,6 +115,10 @@ def _load_library() -> ctypes.CDLL:
         getattr(lib, name).restype = u64 if name in sizes else i32
     lib.ann_embedding_backward_workspace.argtypes = [u64, u64, u32]
     lib.ann_rms_norm_backward_workspace.argtypes = [u64, u32]
+    lib.ann_row_distillation.argtypes = [ctypes.POINTER(RowScores), u32, vp, vp, vp, vp, vp, vp, u64, vp]
+    lib.ann_row_distillation_backward.argtypes = [ctypes.POINTER(RowScores), u32, vp, vp, vp, vp, vp, vp, u64, vp, u64, vp, vp, u64, vp]
+    lib.ann_row_distillation_workspace.argtypes = [u32, u64, u32, u32, u32]
+    lib.ann_row_distillation_backward_workspace.argtypes = [u32, u64, u32, u32, u32]
     lib.ann_layer_norm_backward_workspace.argtypes = [u64, u32]
     lib.ann_row_logprobs_workspace.argtypes = [u32, u64, u32, u32, u32]
     lib.ann_row_logprobs_backward_workspace.argtypes = [u32, u64, u32, u32]
@@ -347,3 +352,26 @@ def ann_row_logprobs_backward(q, nq, q_stride, rows, n, row_stride, d, type, *, 
     _check(_lib.ann_row_logprobs_backward(_row_scores(q, nq, q_stride, rows, n, row_stride, d, type, scale, row_bias, targets), _ptr(lse),
                                           _ptr(entropy), _ptr(g_logprob), _ptr(g_entropy), _ptr(dq), dq_stride, _ptr(drows), drows_stride,
                                           _ptr(drow_bias), _ptr(workspace), workspace_bytes, stream))
+
+
+def ann_row_distillation_workspace(nq, n, d, type, k) -> int:
+    return int(_lib.ann_row_distillation_workspace(nq, n, d, type, k))
+
+
+def ann_row_distillation(q, nq, q_stride, rows, n, row_stride, d, type, *, k, given_ids, given_logprobs, loss, lse, logprobs, scale=1.0,
+                         row_bias=None, workspace=None, workspace_bytes=0, stream=None):
+    _check(_lib.ann_row_distillation(_row_scores(q, nq, q_stride, rows, n, row_stride, d, type, scale, row_bias, None), k, _ptr(given_ids),
+                                     _ptr(given_logprobs), _ptr(loss), _ptr(lse), _ptr(logprobs), _ptr(workspace), workspace_bytes, stream))
+
+
+def ann_row_distillation_backward_workspace(nq, n, d, type, k) -> int:
+    return int(_lib.ann_row_distillation_backward_workspace(nq, n, d, type, k))
+
+
+def ann_row_distillation_backward(q, nq, q_stride, rows, n, row_stride, d, type, *, k, given_ids, given_logprobs, lse, logprobs, g_loss,
+                                  scale=1.0, row_bias=None, dq=None, dq_stride=0, drows=None, drows_stride=0, drow_bias=None,
+                                  workspace=None, workspace_bytes=0, stream=None):
+    _check(_lib.ann_row_distillation_backward(_row_scores(q, nq, q_stride, rows, n, row_stride, d, type, scale, row_bias, None), k,
+                                              _ptr(given_ids), _ptr(given_logprobs), _ptr(lse), _ptr(logprobs), _ptr(g_loss), _ptr(dq),
+                                              dq_stride, _ptr(drows), drows_stride, _ptr(drow_bias), _ptr(workspace), workspace_bytes,
+                                              stream))

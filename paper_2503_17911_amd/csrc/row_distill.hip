@@ -1,0 +1,274 @@
+// Distillation: how far the softmax of all rows' scores is from a teacher's k likeliest rows and their probabilities, and its gradients.
+//
+//   t_ie = exp(given_ie),  loss_i = sum_e t_ie (given_ie - log p_i[id_ie]),  T_i = sum_e t_ie
+//   G[i][j] = g_i (T_i p_ij - sum of t_ie over the entries e with id_ie = j),   dq = scale G X,  dX = scale G^T Q,  dbias = sum_i G_i
+//
+// Forward: the log of the softmax' sum over all rows is that of the rows' log probabilities; the given rows' scores are formed again (fp64 sums).
+// Backward: G has a part at all rows and one at k rows of each query.  The first is what the rows' log probabilities have, with the weight
+// -g_i T_i: its kernels.  The second is added in fp32 to the products' results before these are rounded, together with what the
+// rounding of the first part's elements to 16 bits left at the same rows: where the student is near the teacher the two nearly cancel, and the
+// rounding of g T p alone would be all that is left (the element as the product took it is formed again from the forward pass' log
+// probability; it differs by 1e-6 of itself, so that the remainder is another step's in one of some thousand elements, which then errs by a rounding to
+// 16 bits as all others do).  For dq that is a sum of k rows to a query.  For the rows the entries are put in the order of their ids
+// and summed by runs, so that a row that many teachers name costs no more than others.
+#include "row_logprobs.hpp"
+#include "row_runs.hpp"
+
+#include <math.h>
+
+namespace ann {
+
+// Of an entry: its log probability under the student (0: no row is given, -infinity: the row is left out), and of a query: its loss.  16 lanes to an entry.
+template <typename T>
+__global__ __launch_bounds__(256) void distill_loss_kernel(ScoreTable g, uint32_t k, const uint32_t *__restrict__ ids, const float *__restrict__ given,
+                                                           const float *__restrict__ lse, float *__restrict__ loss, float *__restrict__ logprobs) {
+  constexpr int VEC = 16 / (int)sizeof(T);
+  __shared__ double terms[ANN_MAX_ALTERNATIVES];
+  const uint32_t q = blockIdx.x, lane = threadIdx.x % 16;
+  const float l = lse[q];
+  for (uint32_t e = threadIdx.x / 16; e < k; e += 16) {
+    const uint32_t id = ids[(uint64_t)q * k + e];
+    const float bias = id < g.n && g.bias ? g.bias[id] : 0.0f;
+    double sum = 0.0;
+    if (id < g.n && bias != -INFINITY) {
+      const T *x = (const T *)g.rows + id * g.row_stride, *y = (const T *)g.q + q * g.q_stride;
+      for (uint32_t c = lane * VEC; c < g.d; c += 16 * VEC) {
+        RowPiece<T, VEC, kShifted> a, b;
+        a.load(x, c, g.d), b.load(y, c, g.d);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) sum += (double)a.get(i) * (double)b.get(i);
+      }
+    }
+    sum = group_sum_f64<16>(sum);
+    if (lane != 0) continue;
+    float logp = 0.0f;
+    if (id < g.n) logp = bias == -INFINITY ? -INFINITY : (float)(sum * (double)g.scale + (double)bias - (double)l);
+    logprobs[(uint64_t)q * k + e] = logp;
+    const double t = id < g.n ? (double)given[(uint64_t)q * k + e] : -INFINITY;
+    terms[e] = t == -INFINITY ? 0.0 : exp(t) * (t - (double)logp);
+  }
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  double sum = 0.0;
+  for (uint32_t e = 0; e < k; ++e) sum += terms[e];
+  loss[q] = (float)sum;
+}
+
+struct GivenArgs {
+  ScoreTable g;
+  uint32_t k;
+  const uint32_t *ids;
+  const float *given, *logprobs, *lse, *g_loss;
+  float *whole;     // [nq]: -g T
+  uint32_t *rows;   // [nq][k]: the entries' ids; ANN_PAD_ID where none counts
+  float *weights;   // [nq][k]: -g t
+  float *more;      // [nq][k]: that and what the rounding left
+  uint32_t *slots;  // [n]: filled with ANN_PAD_ID (NULL: not wanted)
+};
+
+// A query's entries, one to a lane of a wavefront; workgroups behind the queries' only fill.
+__global__ __launch_bounds__(256) void distill_given_kernel(GivenArgs a) {
+  if (a.slots)
+    for (uint64_t j = (uint64_t)blockIdx.x * 256 + threadIdx.x; j < a.g.n; j += (uint64_t)gridDim.x * 256) a.slots[j] = ANN_PAD_ID;
+  const uint32_t q = blockIdx.x * 4 + threadIdx.x / kWave, e = lane_id();
+  if (q >= a.g.nq) return;
+  const uint64_t at = (uint64_t)q * a.k + e;
+  const bool in = e < a.k, none = a.lse[q] == -INFINITY;
+  uint32_t id = in ? a.ids[at] : ANN_PAD_ID;
+  const float given = in && id < a.g.n ? a.given[at] : -INFINITY;
+  if (given == -INFINITY) id = ANN_PAD_ID;  // (no weight: it does not count, whatever its row)
+  const float g = a.g_loss[q];
+  const double t = id < a.g.n ? exp((double)given) : 0.0, all = group_sum_f64<kWave>(t);
+  // no row left for this query, the row left out: no gradient
+  if (none || (id < a.g.n && a.g.bias && a.g.bias[id] == -INFINITY)) id = ANN_PAD_ID;
+  if (e == 0) a.whole[q] = none ? 0.0f : -(float)((double)g * all);
+  if (in) a.rows[at] = id, a.weights[at] = -(float)((double)g * t);
+}
+
+// What the rounding of the first part's element left is taken once for a row that is given twice.  T: the type that G is rounded to.
+template <typename T>
+__global__ __launch_bounds__(256) void distill_more_kernel(GivenArgs a, const float *__restrict__ scaling) {
+  const uint32_t q = blockIdx.x * 4 + threadIdx.x / kWave, e = lane_id();
+  if (q >= a.g.nq) return;
+  const uint64_t at = (uint64_t)q * a.k + e;
+  const bool in = e < a.k;
+  const uint32_t id = in ? a.rows[at] : ANN_PAD_ID;
+  bool again = false;
+  for (uint32_t o = 0; o < a.k; ++o) again |= (uint32_t)__builtin_amdgcn_readlane((int)id, (int)o) == id && o < e;
+  if (!in) return;
+  float more = a.weights[at];
+  if (sizeof(T) == 2 && id < a.g.n && !again) {
+    const float by = scaling ? scaling[0] : 1.0f, back = scaling ? scaling[1] : 1.0f;
+    const float v = -(expf(a.logprobs[at]) * (a.whole[q] * by));
+    more = __builtin_fmaf(v - to_f32(from_f32<T>(v)), back, more);
+  }
+  a.more[at] = more;
+}
+
+// The second part's sums over the queries, by rows: weights of q, and of the bias.
+template <typename T>
+struct GivenSums {
+  static constexpr bool kWeighted = true, kScalar = true;
+  const T *q;
+  uint64_t q_stride;
+  const float *more, *weights;
+  uint32_t *slots;
+  float *sums;
+  uint32_t k, ld, dim, d;
+  bool by_row;  // a sum lies at its row's number; otherwise at that of the run's first entry
+  __device__ __forceinline__ const T *row(uint32_t position) const { return q + position / k * q_stride; }
+  __device__ __forceinline__ float weight(uint32_t position) const { return more[position]; }
+  __device__ __forceinline__ float scalar(uint32_t position) const { return weights[position]; }
+  __device__ __forceinline__ float *at(uint32_t id, uint32_t start) const { return sums + (uint64_t)(by_row ? id : start) * ld; }
+  __device__ __forceinline__ void write_scalar(uint32_t id, uint32_t start, float sum) const {
+    at(id, start)[d] = sum;
+    slots[id] = by_row ? id : start;
+  }
+  template <int VEC, RowEnd END>
+  __device__ __forceinline__ void write(uint32_t id, uint32_t start, uint32_t c, const float (&sum)[VEC]) const {
+    float *to = at(id, start) + c;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e)
+      if (VEC == 1 || END == kWholePieces || c + e < dim) to[e] = sum[e];
+  }
+  __device__ __forceinline__ void beside(uint32_t, uint32_t) const {}
+};
+
+struct DistillPlan {
+  IdSortPlan sort;
+  RunsPlan runs;
+  bool by_row = false;
+  uint32_t ld = 0;  // of the sums and their parts: d + 1, in pieces of 16 bytes
+  uint64_t backward_bytes = 0, whole_at = 0, rows_at = 0, weights_at = 0, more_at = 0, scaling_at = 0, slots_at = 0, sort_at = 0, part_at = 0, sums_at = 0;
+  Parts parts;
+};
+
+// Room for the rows' side is there whether it is wanted or not.
+static DistillPlan distill_plan(uint32_t nq, uint64_t n, uint32_t d, uint32_t type, uint32_t k) {
+  DistillPlan p;
+  if (nq == 0 || n == 0) return p;
+  const uint64_t entries = (uint64_t)nq * k;
+  p.backward_bytes = scores_backward_bytes(nq, n, d, type);
+  p.parts.take(p.backward_bytes);
+  p.whole_at = p.parts.take(nq * 4ull);
+  p.rows_at = p.parts.take(entries * 4), p.weights_at = p.parts.take(entries * 4), p.more_at = p.parts.take(entries * 4);
+  p.scaling_at = p.parts.take(2 * sizeof(float));
+  p.slots_at = p.parts.take(n * 4);
+  p.sort = id_sort_plan(entries, n);
+  p.sort_at = p.parts.take(p.sort.bytes);
+  p.ld = (d + 1 + 3) / 4 * 4;
+  p.runs = runs_plan(entries, p.ld);
+  p.part_at = p.parts.take(p.runs.part_bytes);
+  p.by_row = n <= entries;
+  p.sums_at = p.parts.take((p.by_row ? n : entries) * p.ld * sizeof(float));
+  return p;
+}
+
+template <typename T>
+static ann_status distill_rows(const DistillPlan &p, const GivenArgs &a, bool rows, bool few, char *ws, GradArgs &to, hipStream_t st) {
+  SortedIds sorted;
+  if (ann_status s = sort_ids(p.sort, a.rows, ws + p.sort_at, nullptr, NothingBeside(), st, sorted)) return s;
+  const uint32_t dim = rows ? a.g.d : 0;
+  const Runs runs = {sorted.keys, sorted.positions, a.g.nq * a.k, a.g.n, p.runs.chunk, p.runs.chunks, dim, (float *)(ws + p.part_at), p.ld};
+  // (few queries: the product takes along what G's rounding left)
+  const GivenSums<T> work = {(const T *)a.g.q, a.g.q_stride, few ? a.weights : a.more, a.weights, a.slots, (float *)(ws + p.sums_at), a.k, p.ld, dim, a.g.d, p.by_row};
+  if (ann_status s = sum_runs<T>(runs, work, 0, st)) return s;
+  to.slots = a.slots, to.sums = work.sums, to.more_ld = p.ld;
+  return ANN_OK;
+}
+
+static ann_status check_distillation(const char *what, const ann_row_scores *s, uint32_t k, const uint32_t *ids, const float *given) {
+  if (ann_status e = check_scores(what, s)) return e;
+  if (k == 0) return fail(ANN_EINVAL, "%s: k == 0", what);
+  if (k > ANN_MAX_ALTERNATIVES) return fail(ANN_ECAPACITY, "%s: k = %u exceeds ANN_MAX_ALTERNATIVES = %u", what, k, ANN_MAX_ALTERNATIVES);
+  if (s->targets) return fail(ANN_EINVAL, "%s: targets belong to the rows' log probabilities", what);
+  if (s->nq && (!ids || !given)) return fail(ANN_EINVAL, "%s: given_ids or given_logprobs is NULL", what);
+  return ANN_OK;
+}
+
+}  // namespace ann
+
+using namespace ann;
+
+static uint64_t forward_bytes(uint32_t nq, uint64_t n, uint32_t d, uint32_t type) { return (ann_row_logprobs_workspace(nq, n, d, type, 0) + 255) / 256 * 256; }
+
+extern "C" uint64_t ann_row_distillation_workspace(uint32_t nq, uint64_t n, uint32_t d, uint32_t type, uint32_t k) {
+  if (n > kMaxRows || nq >= kMaxQueries || d == 0 || type > ANN_BF16 || k > ANN_MAX_ALTERNATIVES || nq == 0) return 0;
+  return forward_bytes(nq, n, d, type) + nq * 4ull;
+}
+
+extern "C" ann_status ann_row_distillation(const ann_row_scores *scores, uint32_t k, const uint32_t *given_ids, const float *given_logprobs, float *loss,
+                                           float *lse, float *logprobs, void *workspace, uint64_t workspace_bytes, void *stream) {
+  if (ann_status s = check_distillation("ann_row_distillation", scores, k, given_ids, given_logprobs)) return s;
+  const uint32_t nq = scores->nq;
+  if (nq == 0) return ANN_OK;
+  if (!loss || !lse || !logprobs) return fail(ANN_EINVAL, "ann_row_distillation: loss, lse or logprobs is NULL");
+  const uint64_t need = ann_row_distillation_workspace(nq, scores->n, scores->d, scores->type, k), before = need - nq * 4ull;
+  if (ann_status s = check_workspace("ann_row_distillation", workspace, workspace_bytes, need)) return s;
+  if (ann_status s = ann_row_logprobs(scores, 0, (float *)((char *)workspace + before), nullptr, lse, nullptr, nullptr, workspace, before, stream)) return s;
+  const ScoreTable g = score_table(*scores);
+  const hipStream_t st = (hipStream_t)stream;
+  if (scores->type == ANN_F32)
+    distill_loss_kernel<float><<<nq, 256, 0, st>>>(g, k, given_ids, given_logprobs, lse, loss, logprobs);
+  else if (scores->type == ANN_F16)
+    distill_loss_kernel<f16_t><<<nq, 256, 0, st>>>(g, k, given_ids, given_logprobs, lse, loss, logprobs);
+  else
+    distill_loss_kernel<bf16_t><<<nq, 256, 0, st>>>(g, k, given_ids, given_logprobs, lse, loss, logprobs);
+  ANN_HIP(hipGetLastError());
+  return ANN_OK;
+}
+
+extern "C" uint64_t ann_row_distillation_backward_workspace(uint32_t nq, uint64_t n, uint32_t d, uint32_t type, uint32_t k) {
+  if (n > kMaxRows || nq >= kMaxQueries || d == 0 || type > ANN_BF16 || k > ANN_MAX_ALTERNATIVES || k == 0) return 0;
+  return distill_plan(nq, n, d, type, k).parts.bytes;
+}
+
+extern "C" ann_status ann_row_distillation_backward(const ann_row_scores *scores, uint32_t k, const uint32_t *given_ids, const float *given_logprobs,
+                                                    const float *lse, const float *logprobs, const float *g_loss, void *dq, uint64_t dq_stride,
+                                                    void *drows, uint64_t drows_stride, float *drow_bias, void *workspace,
+                                                    uint64_t workspace_bytes, void *stream) {
+  const char *what = "ann_row_distillation_backward";
+  if (ann_status s = check_distillation(what, scores, k, given_ids, given_logprobs)) return s;
+  if (scores->nq && (!lse || !logprobs || !g_loss)) return fail(ANN_EINVAL, "%s: lse, logprobs or g_loss is NULL", what);
+  if (dq && dq_stride < scores->d) return fail(ANN_EINVAL, "%s: dq_stride is shorter than a row", what);
+  if (drows && drows_stride < scores->d) return fail(ANN_EINVAL, "%s: drows_stride is shorter than a row", what);
+  const uint32_t nq = scores->nq, type = scores->type;
+  const DistillPlan p = distill_plan(nq, scores->n, scores->d, type, k);
+  if (ann_status s = check_workspace(what, workspace, workspace_bytes, p.parts.bytes)) return s;
+  char *ws = (char *)workspace;
+  const hipStream_t st = (hipStream_t)stream;
+  GradArgs a = {};
+  a.g = score_table(*scores), a.lse = lse, a.every = true;
+  const GradOut o = {dq, drows, drow_bias, dq_stride, drows_stride};
+  if (nq && scores->n) {
+    const bool rows_side = drows || drow_bias;
+    GivenArgs v = {};
+    v.g = a.g, v.k = k, v.ids = given_ids, v.given = given_logprobs, v.logprobs = logprobs, v.lse = lse, v.g_loss = g_loss;
+    v.whole = (float *)(ws + p.whole_at), v.rows = (uint32_t *)(ws + p.rows_at), v.weights = (float *)(ws + p.weights_at), v.more = (float *)(ws + p.more_at);
+    v.slots = rows_side ? (uint32_t *)(ws + p.slots_at) : nullptr;
+    const uint32_t of_queries = (nq + 3) / 4, filling = rows_side ? (uint32_t)((scores->n + 4095) / 4096 < 2048 ? (scores->n + 4095) / 4096 : 2048) : 0;
+    distill_given_kernel<<<of_queries > filling ? of_queries : filling, 256, 0, st>>>(v);
+    ANN_HIP(hipGetLastError());
+    a.g_logprob = v.whole;
+    if (type == ANN_F16) {
+      float *scaling = (float *)(ws + p.scaling_at);
+      if (ann_status s = launch_grad_scaling(a, scaling, st)) return s;
+      a.scaling = scaling;
+      distill_more_kernel<f16_t><<<of_queries, 256, 0, st>>>(v, scaling);
+    } else if (type == ANN_BF16) {
+      distill_more_kernel<bf16_t><<<of_queries, 256, 0, st>>>(v, nullptr);
+    } else {
+      distill_more_kernel<float><<<of_queries, 256, 0, st>>>(v, nullptr);
+    }
+    ANN_HIP(hipGetLastError());
+    a.given = k, a.ids = v.rows, a.more = v.more;
+    if (rows_side) {
+      const bool few = type == ANN_F32 || nq <= kFewQueries;
+      ann_status s = type == ANN_F32   ? distill_rows<float>(p, v, drows, few, ws, a, st)
+                     : type == ANN_F16 ? distill_rows<f16_t>(p, v, drows, few, ws, a, st)
+                                       : distill_rows<bf16_t>(p, v, drows, few, ws, a, st);
+      if (s) return s;
+    }
+  }
+  return scores_backward(type, a, o, ws, st);
+}

@@ -36,15 +36,11 @@ constexpr uint32_t kWideSlots = 512;            // of a wide one: two
 template <typename T>
 constexpr int kGradWaves = sizeof(T) == 2 ? 3 : 2;
 
-constexpr uint32_t kFewQueries = 256;  // up to so many, the rows' gradient takes all of G's remainders
-
-struct GradArgs {
-  ScoreTable g;
-  const uint32_t *targets;
-  const float *lse, *entropy, *g_logprob, *g_entropy;
-  const float *scaling;  // [2]: what G is multiplied by before it is rounded, and its inverse (f16)
-  float *rest;           // [nq]: what the rounding of the given row's element left (16 bits)
-};
+// What is added to a row's gradient (column d: its bias'), after G's rounding.
+__device__ __forceinline__ float more_of_row(const GradArgs &a, uint32_t row, uint32_t c) {
+  const uint32_t slot = a.slots[row];
+  return slot == ANN_PAD_ID ? 0.0f : a.sums[(uint64_t)slot * a.more_ld + c];
+}
 
 // scaling[0]: the power of two for G, scaling[1]: its inverse.  A query counts as it does in G: with g_logprob where a row is given, not at
 // all without a row left (or with statistics that are NaN).  Weights that are not finite spoil their own query, not the scale of the others.
@@ -53,7 +49,7 @@ __global__ __launch_bounds__(1024) void grad_scaling_kernel(GradArgs a, float *_
   float most = 0.0f;
   for (uint32_t i = threadIdx.x; i < a.g.nq; i += 1024) {
     if (!(a.lse[i] > -INFINITY)) continue;
-    const bool given = a.targets && a.targets[i] < a.g.n;
+    const bool given = a.every || (a.targets && a.targets[i] < a.g.n);
     const float g = a.g_logprob && given ? fabsf(a.g_logprob[i]) : 0.0f;
     const float h = a.g_entropy ? fabsf(a.g_entropy[i]) * (fabsf(a.entropy[i]) + 0.375f) : 0.0f;
     if (g < INFINITY && h < INFINITY) most = fmaxf(most, fminf(g + h, 3.402823466e38f));
@@ -98,7 +94,7 @@ __global__ __launch_bounds__(256) void grad_scores_kernel(GradArgs a, uint32_t r
     float lse = there ? a.lse[q] : 0.0f;
     const bool none = !there || lse == -INFINITY;
     if (none) lse = 0.0f;
-    const float gl = none || !a.g_logprob || target >= g.n ? 0.0f : a.g_logprob[q];
+    const float gl = none || !a.g_logprob || (target >= g.n && !a.every) ? 0.0f : a.g_logprob[q];
     const float gh = ENTROPY && !none ? a.g_entropy[q] : 0.0f, h = ENTROPY && !none ? a.entropy[q] : 0.0f;
     const uint32_t hit = target - (first + mw);  // row of the target within the wavefront's 64, if below 64
 #pragma unroll
@@ -228,6 +224,20 @@ __global__ __launch_bounds__(THREADS) void grad_queries_sum_kernel(GradArgs a, c
         for (int u = 0; u < 8; ++u) sum += v[u];
       }
       for (; s < end; ++s) sum += p[s * all];
+      if (a.given) {  // (shared out over the runs like the splits)
+        const float to = a.scaling ? a.scaling[0] : 1.0f;
+        for (uint32_t e0 = run; e0 < a.given; e0 += 8 * RUNS) {
+          float x[8], more[8];
+#pragma unroll
+          for (uint32_t u = 0; u < 8; ++u) {
+            const uint32_t e = e0 + u * RUNS, id = e < a.given ? a.ids[q * a.given + e] : ANN_PAD_ID;
+            more[u] = id < g.n ? a.more[q * a.given + e] * to : 0.0f;
+            x[u] = id < g.n ? to_f32(((const T *)g.rows)[id * g.row_stride + c]) : 0.0f;
+          }
+#pragma unroll
+          for (uint32_t u = 0; u < 8; ++u) sum = __builtin_fmaf(more[u], x[u], sum);
+        }
+      }
     }
     if constexpr (RUNS > 1) {
       __syncthreads();  // (the columns before have been read)
@@ -320,7 +330,9 @@ __global__ __launch_bounds__(256, RESTS ? 2 : kGradWaves<T>) void grad_rows_kern
             part[((uint64_t)split * rows + row) * g.d + c] = acc[i][j][r];
           } else {
             const bool left_out = g.bias && g.bias[row0 + row] == -INFINITY;  // (zero, whatever the queries hold)
-            out[(uint64_t)(row0 + row) * stride + c] = from_f32<T>(left_out ? 0.0f : acc[i][j][r] * by);
+            float v = acc[i][j][r] * by;
+            if (a.slots) v = __builtin_fmaf(g.scale, more_of_row(a, row0 + row, c), v);
+            out[(uint64_t)(row0 + row) * stride + c] = from_f32<T>(left_out ? 0.0f : v);
           }
         }
       }
@@ -329,16 +341,19 @@ __global__ __launch_bounds__(256, RESTS ? 2 : kGradWaves<T>) void grad_rows_kern
 
 // The splits' parts, in their order.
 template <typename T>
-__global__ __launch_bounds__(256) void grad_rows_sum_kernel(ScoreTable g, uint32_t row0, uint32_t rows, const float *__restrict__ part, uint32_t splits, T *__restrict__ out,
-                                                            uint64_t stride, const float *__restrict__ scaling) {
+__global__ __launch_bounds__(256) void grad_rows_sum_kernel(GradArgs a, uint32_t row0, uint32_t rows, const float *__restrict__ part, uint32_t splits, T *__restrict__ out,
+                                                            uint64_t stride) {
+  const ScoreTable &g = a.g;
   const uint64_t all = (uint64_t)rows * g.d, at = (uint64_t)blockIdx.x * 256 + threadIdx.x;
   if (at >= all) return;
-  const float by = scaling ? g.scale * scaling[1] : g.scale;
+  const float by = a.scaling ? g.scale * a.scaling[1] : g.scale;
   float sum = 0.0f;
   for (uint32_t s = 0; s < splits; ++s) sum += part[s * all + at];
   const uint64_t row = row0 + at / g.d;
   const bool left_out = g.bias && g.bias[row] == -INFINITY;
-  out[row * stride + at % g.d] = from_f32<T>(left_out ? 0.0f : sum * by);
+  float v = sum * by;
+  if (a.slots) v = __builtin_fmaf(g.scale, more_of_row(a, (uint32_t)row, (uint32_t)(at % g.d)), v);
+  out[row * stride + at % g.d] = from_f32<T>(left_out ? 0.0f : v);
 }
 
 // Adds v with what the last addition lost: over many queries like terms lose with one sign (1.7e-4 of the sum of a million).
@@ -350,12 +365,13 @@ __device__ __forceinline__ void add_carried(float &sum, float &lost, float v) {
 }
 
 // drow_bias[row0 + j] = sum of the parts, in their order
-__global__ __launch_bounds__(256) void grad_bias_kernel(const float *__restrict__ row_sums, uint32_t parts, uint32_t ld, uint32_t row0, uint32_t rows,
+__global__ __launch_bounds__(256) void grad_bias_kernel(GradArgs a, const float *__restrict__ row_sums, uint32_t parts, uint32_t ld, uint32_t row0, uint32_t rows,
                                                         float *__restrict__ out) {
   const uint32_t j = blockIdx.x * 256 + threadIdx.x;
   if (j >= rows) return;
   float sum = 0.0f, lost = 0.0f;
   for (uint32_t p = 0; p < parts; ++p) add_carried(sum, lost, row_sums[(uint64_t)p * ld + j]);
+  if (a.slots) add_carried(sum, lost, more_of_row(a, row0 + j, a.g.d));
   out[row0 + j] = sum;
 }
 
@@ -413,7 +429,7 @@ __global__ __launch_bounds__(256, 2) void grad_short_kernel(GradArgs a, uint32_t
     const float lse = is ? a.lse[q] : -INFINITY;
     lse2 = lse == -INFINITY ? -INFINITY : BIAS ? -lse : -lse * kLog2e;
     const bool none = lse == -INFINITY;
-    gl = none || !a.g_logprob || target >= g.n ? 0.0f : -scaling * a.g_logprob[q];
+    gl = none || !a.g_logprob || (target >= g.n && !a.every) ? 0.0f : -scaling * a.g_logprob[q];
     gh = ENTROPY && !none ? -scaling * a.g_entropy[q] : 0.0f;
     h = ENTROPY && !none ? a.entropy[q] : 0.0f;
   };
@@ -574,7 +590,11 @@ __global__ __launch_bounds__(256, 2) void grad_short_kernel(GradArgs a, uint32_t
   if (OWN_ROWS && drow_bias) {
     const LanePair p = lane_pair<false>(__float_as_uint(sum));
     sum = __uint_as_float(p.low) + __uint_as_float(p.high);
-    if (lane < 32 && mine < g.n) drow_bias[mine] = sum / scaling;
+    if (lane < 32 && mine < g.n) {
+      sum /= scaling;
+      if (a.slots) sum += more_of_row(a, mine, g.d);
+      drow_bias[mine] = sum;
+    }
   }
   if (OWN_ROWS && !drows) return;
   const float by = a.scaling ? g.scale * a.scaling[1] : g.scale;
@@ -587,7 +607,9 @@ __global__ __launch_bounds__(256, 2) void grad_short_kernel(GradArgs a, uint32_t
       if (l >= owned || column >= g.d) continue;
       if constexpr (OWN_ROWS) {
         const bool left_out = BIAS && g.bias[l] == -INFINITY;  // (zero, whatever the queries hold)
-        drows[l * stride + column] = from_f32<T>(left_out ? 0.0f : acc[b][r] * by);
+        float v = acc[b][r] * by;
+        if (a.slots) v = __builtin_fmaf(g.scale, more_of_row(a, l, column), v);
+        drows[l * stride + column] = from_f32<T>(left_out ? 0.0f : v);
       } else {
         part[((uint64_t)split * g.nq + l) * g.d + column] = acc[b][r];
       }
@@ -657,11 +679,11 @@ static BackwardPlan backward_plan(uint32_t nq, uint64_t n, uint32_t d, uint32_t 
   return p;
 }
 
-struct GradOut {
-  void *dq, *drows;
-  float *drow_bias;
-  uint64_t dq_stride, drows_stride;
-};
+ann_status launch_grad_scaling(const GradArgs &a, float *scaling, hipStream_t st) {
+  grad_scaling_kernel<<<1, 1024, 0, st>>>(a, scaling);
+  ANN_HIP(hipGetLastError());
+  return ANN_OK;
+}
 
 template <typename T>
 static ann_status backward(const GradArgs &args, const BackwardPlan &p, const GradOut &o, char *ws, hipStream_t st) {
@@ -671,10 +693,9 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
   T *G = (T *)(ws + p.g_at), *rests = sizeof(T) == 2 && g.nq && g.nq <= kFewQueries && o.drows ? (T *)(ws + p.rests_at) : nullptr;
   float *part = (float *)(ws + p.part_at), *sums = (float *)(ws + p.sums_at);
   a.rest = (float *)(ws + p.rest_at);
-  if (sizeof(T) == 2 && std::is_same<T, f16_t>::value && g.nq && g.n) {
+  if (std::is_same<T, f16_t>::value && g.nq && g.n && !a.scaling) {
     float *scaling = (float *)(ws + p.scaling_at);
-    grad_scaling_kernel<<<1, 1024, 0, st>>>(a, scaling);
-    ANN_HIP(hipGetLastError());
+    if (ann_status s = launch_grad_scaling(a, scaling, st)) return s;
     a.scaling = scaling;
   }
   if (p.slices) {
@@ -774,14 +795,14 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
       if (p.row_splits > 1) {
         with_split(std::true_type());
         ANN_HIP(hipGetLastError());
-        grad_rows_sum_kernel<T><<<(uint32_t)(((uint64_t)rows * g.d + 255) / 256), 256, 0, st>>>(g, row0, rows, row_part, p.row_splits, (T *)o.drows, o.drows_stride, a.scaling);
+        grad_rows_sum_kernel<T><<<(uint32_t)(((uint64_t)rows * g.d + 255) / 256), 256, 0, st>>>(a, row0, rows, row_part, p.row_splits, (T *)o.drows, o.drows_stride);
       } else {
         with_split(std::false_type());
       }
       ANN_HIP(hipGetLastError());
     }
     if (o.drow_bias) {
-      grad_bias_kernel<<<(rows + 255) / 256, 256, 0, st>>>(sums, p.q_tiles * 2, ld, row0, rows, o.drow_bias);
+      grad_bias_kernel<<<(rows + 255) / 256, 256, 0, st>>>(a, sums, p.q_tiles * 2, ld, row0, rows, o.drow_bias);
       ANN_HIP(hipGetLastError());
     }
   }
@@ -790,6 +811,15 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
     ANN_HIP(hipGetLastError());
   }
   return ANN_OK;
+}
+
+uint64_t scores_backward_bytes(uint32_t nq, uint64_t n, uint32_t d, uint32_t type) { return backward_plan(nq, n, d, type).parts.bytes; }
+
+ann_status scores_backward(uint32_t type, const GradArgs &a, const GradOut &o, void *workspace, hipStream_t st) {
+  const BackwardPlan p = backward_plan(a.g.nq, a.g.n, a.g.d, type);
+  if (type == ANN_F32) return backward<float>(a, p, o, (char *)workspace, st);
+  if (type == ANN_F16) return backward<f16_t>(a, p, o, (char *)workspace, st);
+  return backward<bf16_t>(a, p, o, (char *)workspace, st);
 }
 
 }  // namespace ann
@@ -809,13 +839,11 @@ extern "C" ann_status ann_row_logprobs_backward(const ann_row_scores *scores, co
   if (scores->nq && g_entropy && !entropy) return fail(ANN_EINVAL, "ann_row_logprobs_backward: g_entropy without entropy");
   if (dq && dq_stride < scores->d) return fail(ANN_EINVAL, "ann_row_logprobs_backward: dq_stride is shorter than a row");
   if (drows && drows_stride < scores->d) return fail(ANN_EINVAL, "ann_row_logprobs_backward: drows_stride is shorter than a row");
-  const BackwardPlan p = backward_plan(scores->nq, scores->n, scores->d, scores->type);
-  if (ann_status s = check_workspace("ann_row_logprobs_backward", workspace, workspace_bytes, p.parts.bytes)) return s;
+  if (ann_status s = check_workspace("ann_row_logprobs_backward", workspace, workspace_bytes, scores_backward_bytes(scores->nq, scores->n, scores->d, scores->type)))
+    return s;
   GradArgs a = {};
   a.g = score_table(*scores);
   a.targets = scores->targets, a.lse = lse, a.entropy = entropy, a.g_logprob = g_logprob, a.g_entropy = g_entropy;
   const GradOut o = {dq, drows, drow_bias, dq_stride, drows_stride};
-  if (scores->type == ANN_F32) return backward<float>(a, p, o, (char *)workspace, (hipStream_t)stream);
-  if (scores->type == ANN_F16) return backward<f16_t>(a, p, o, (char *)workspace, (hipStream_t)stream);
-  return backward<bf16_t>(a, p, o, (char *)workspace, (hipStream_t)stream);
+  return scores_backward(scores->type, a, o, workspace, (hipStream_t)stream);
 }

@@ -86,3 +86,44 @@ def test_workspaces():
     assert 0 < ann.ann_rms_norm_backward_workspace(1, 100) <= ann.ann_rms_norm_backward_workspace(1 << 30, 100) < 1 << 20
     # 16 bytes of order to an id, and parts whose number has an end
     assert ann.ann_embedding_backward_workspace(100_000_000, 50_000, 1000) < 16 * 100_000_000 + (1 << 29)
+
+
+SCORES = dict(q=16, nq=2, q_stride=8, rows=16, n=4, row_stride=8, d=8, type=ann.BF16, k=2, given_ids=16, given_logprobs=16, workspace=256, workspace_bytes=1 << 30)
+DISTILL = dict(SCORES, loss=16, lse=16, logprobs=16)
+DISTILL_BACK = dict(SCORES, lse=16, logprobs=16, g_loss=16, dq=16, dq_stride=8, drows=16, drows_stride=8)
+DISTILL_COMMON = [
+    (dict(q=None), ann.EINVAL, "q is NULL"), (dict(rows=None), ann.EINVAL, "rows is NULL"), (dict(d=0), ann.EINVAL, "d == 0"), (dict(type=3), ann.EINVAL, "type"),
+    (dict(q_stride=7), ann.EINVAL, "stride"), (dict(scale=math.inf), ann.EINVAL, "scale"), (dict(k=0), ann.EINVAL, "k == 0"),
+    (dict(k=ann.MAX_ALTERNATIVES + 1), ann.ECAPACITY, "ANN_MAX_ALTERNATIVES"), (dict(given_ids=None), ann.EINVAL, "given_ids"),
+    (dict(given_logprobs=None), ann.EINVAL, "given_ids"), (dict(lse=None), ann.EINVAL, "lse"), (dict(logprobs=None), ann.EINVAL, "lse"),
+    (dict(n=1 << 31), ann.ECAPACITY, "2^31"), (dict(nq=1 << 24), ann.ECAPACITY, "2^24"), (dict(workspace=None), ann.EINVAL, "workspace"),
+    (dict(workspace_bytes=7), ann.EINVAL, "needed"), (dict(workspace=264), ann.EINVAL, "aligned"),
+]
+
+
+@pytest.mark.parametrize("change, status, words", DISTILL_COMMON + [(dict(loss=None), ann.EINVAL, "loss")])
+def test_row_distillation_refuses(change, status, words):
+    refused(status, words, ann.ann_row_distillation, **{**DISTILL, **change})
+
+
+@pytest.mark.parametrize("change, status, words", DISTILL_COMMON + [
+    (dict(g_loss=None), ann.EINVAL, "g_loss"), (dict(dq_stride=7), ann.EINVAL, "dq_stride"), (dict(drows_stride=7), ann.EINVAL, "drows_stride"),
+])
+def test_row_distillation_backward_refuses(change, status, words):
+    refused(status, words, ann.ann_row_distillation_backward, **{**DISTILL_BACK, **change})
+
+
+def test_targets_are_refused():
+    import ctypes
+    scores = ann.RowScores(q=16, rows=16, n=4, q_stride=8, row_stride=8, nq=2, d=8, type=ann.BF16, scale=1.0, row_bias=None, targets=16)
+    assert ann._lib.ann_row_distillation(ctypes.byref(scores), 2, 16, 16, 16, 16, 16, 256, 1 << 30, None) == ann.EINVAL
+    assert ann._lib.ann_row_distillation_backward(ctypes.byref(scores), 2, 16, 16, 16, 16, 16, 16, 8, 16, 8, None, 256, 1 << 30, None) == ann.EINVAL
+
+
+def test_distillation_of_no_queries_is_no_work():
+    ann.ann_row_distillation(**{**DISTILL, "nq": 0, "q": None, "loss": None, "lse": None, "logprobs": None, "workspace": None, "workspace_bytes": 0})
+    for t in (ann.F32, ann.F16, ann.BF16):
+        assert ann.ann_row_distillation_workspace(0, 100, 8, t, 1) == ann.ann_row_distillation_backward_workspace(0, 100, 8, t, 1) == 0
+        # sums for the smaller of the rows and the entries
+        few, many = (ann.ann_row_distillation_backward_workspace(nq, 1_000_000, 128, t, 8) for nq in (100, 10_000))
+        assert few < 1 << 29 and many < 1 << 31
