@@ -85,24 +85,66 @@ __global__ __launch_bounds__(256) void distill_given_kernel(GivenArgs a) {
   if (in) a.rows[at] = id, a.weights[at] = -(float)((double)g * t);
 }
 
-// What the rounding of the first part's element left is taken once for a row that is given twice.  T: the type that G is rounded to.
-template <typename T>
-__global__ __launch_bounds__(256) void distill_more_kernel(GivenArgs a, const float *__restrict__ scaling) {
-  const uint32_t q = blockIdx.x * 4 + threadIdx.x / kWave, e = lane_id();
-  if (q >= a.g.nq) return;
-  const uint64_t at = (uint64_t)q * a.k + e;
-  const bool in = e < a.k;
-  const uint32_t id = in ? a.rows[at] : ANN_PAD_ID;
-  bool again = false;
-  for (uint32_t o = 0; o < a.k; ++o) again |= (uint32_t)__builtin_amdgcn_readlane((int)id, (int)o) == id && o < e;
-  if (!in) return;
-  float more = a.weights[at];
-  if (sizeof(T) == 2 && id < a.g.n && !again) {
-    const float by = scaling ? scaling[0] : 1.0f, back = scaling ? scaling[1] : 1.0f;
-    const float v = -(expf(a.logprobs[at]) * (a.whole[q] * by));
-    more = __builtin_fmaf(v - to_f32(from_f32<T>(v)), back, more);
+// An entry's weight and what the rounding of the first part's element left, which is taken once for a row that is given twice; and their sum over the
+// query's entries of more * row: a workgroup to a query, 256 columns in pieces at a time, kGivenRuns runs of entries side by side.  T: the type
+// that G is rounded to.  part NULL: the entries alone.
+constexpr uint32_t kGivenRuns = 8, kGivenLanes = 32;
+template <typename T, RowEnd END>
+__global__ __launch_bounds__(kGivenRuns * kGivenLanes) void distill_more_kernel(GivenArgs a, const float *__restrict__ scaling, float *__restrict__ part) {
+  constexpr int VEC = 16 / (int)sizeof(T), kEach = ANN_MAX_ALTERNATIVES / kGivenRuns;
+  __shared__ float more_of[ANN_MAX_ALTERNATIVES], room[kGivenRuns][kGivenLanes * VEC + 4];
+  __shared__ uint32_t id_of[ANN_MAX_ALTERNATIVES];
+  const uint32_t q = blockIdx.x, lane = threadIdx.x % kGivenLanes, run = threadIdx.x / kGivenLanes;
+  const float by = scaling ? scaling[0] : 1.0f, back = scaling ? scaling[1] : 1.0f;
+  if (threadIdx.x < kWave) {
+    const uint32_t e = threadIdx.x;
+    const uint64_t at = (uint64_t)q * a.k + e;
+    const uint32_t id = e < a.k ? a.rows[at] : ANN_PAD_ID;
+    bool again = false;
+    for (uint32_t o = 0; o < a.k; ++o) again |= (uint32_t)__builtin_amdgcn_readlane((int)id, (int)o) == id && o < e;
+    float more = 0.0f;
+    if (e < a.k) {
+      more = a.weights[at];
+      if (sizeof(T) == 2 && id < a.g.n && !again) {
+        const float v = -(expf(a.logprobs[at]) * (a.whole[q] * by));
+        more = __builtin_fmaf(v - to_f32(from_f32<T>(v)), back, more);
+      }
+      a.more[at] = more;
+    }
+    more_of[e] = more * by, id_of[e] = id;
   }
-  a.more[at] = more;
+  if (!part) return;
+  __syncthreads();
+  const uint32_t begin = a.k * run / kGivenRuns, end = a.k * (run + 1) / kGivenRuns;
+  for (uint32_t c0 = 0; c0 < a.g.d; c0 += kGivenLanes * VEC) {
+    const uint32_t c = c0 + lane * VEC;
+    RowPiece<T, VEC, END> x[kEach];
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+      const uint32_t id = begin + u < end ? id_of[begin + u] : ANN_PAD_ID;
+      x[u].load((const T *)a.g.rows + (id < a.g.n ? id : 0) * a.g.row_stride, id < a.g.n ? c : a.g.d, a.g.d);  // (no row: nothing is read as a number)
+    }
+    float sum[VEC];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) sum[v] = 0.0f;
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+      const uint32_t id = begin + u < end ? id_of[begin + u] : ANN_PAD_ID;
+      const float more = begin + u < end ? more_of[begin + u] : 0.0f;
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) sum[v] = id < a.g.n ? __builtin_fmaf(more, x[u].get(v), sum[v]) : sum[v];
+    }
+    __syncthreads();  // (the columns before have been read)
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) room[run][lane * VEC + v] = sum[v];
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < kGivenLanes * VEC && c0 + i < a.g.d; i += kGivenRuns * kGivenLanes) {
+      float all = room[0][i];
+#pragma unroll
+      for (uint32_t r = 1; r < kGivenRuns; ++r) all += room[r][i];
+      part[(uint64_t)q * a.g.d + c0 + i] = all;
+    }
+  }
 }
 
 // The second part's sums over the queries, by rows: weights of q, and of the bias.
@@ -148,7 +190,7 @@ static DistillPlan distill_plan(uint32_t nq, uint64_t n, uint32_t d, uint32_t ty
   DistillPlan p;
   if (nq == 0 || n == 0) return p;
   const uint64_t entries = (uint64_t)nq * k;
-  p.backward_bytes = scores_backward_bytes(nq, n, d, type);
+  p.backward_bytes = scores_backward_bytes(nq, n, d, type, true);
   p.parts.take(p.backward_bytes);
   p.whole_at = p.parts.take(nq * 4ull);
   p.rows_at = p.parts.take(entries * 4), p.weights_at = p.parts.take(entries * 4), p.more_at = p.parts.take(entries * 4);
@@ -250,18 +292,27 @@ extern "C" ann_status ann_row_distillation_backward(const ann_row_scores *scores
     distill_given_kernel<<<of_queries > filling ? of_queries : filling, 256, 0, st>>>(v);
     ANN_HIP(hipGetLastError());
     a.g_logprob = v.whole;
+    float *scaling = nullptr, *part = dq ? scores_backward_more_part(nq, scores->n, scores->d, type, ws) : nullptr;
     if (type == ANN_F16) {
-      float *scaling = (float *)(ws + p.scaling_at);
+      scaling = (float *)(ws + p.scaling_at);
       if (ann_status s = launch_grad_scaling(a, scaling, st)) return s;
       a.scaling = scaling;
-      distill_more_kernel<f16_t><<<of_queries, 256, 0, st>>>(v, scaling);
-    } else if (type == ANN_BF16) {
-      distill_more_kernel<bf16_t><<<of_queries, 256, 0, st>>>(v, nullptr);
-    } else {
-      distill_more_kernel<float><<<of_queries, 256, 0, st>>>(v, nullptr);
     }
+    const auto add_up = [&](auto t) {
+      typedef decltype(t) T;
+      if (scores->d % (16 / sizeof(T)) == 0)
+        distill_more_kernel<T, kWholePieces><<<nq, kGivenRuns * kGivenLanes, 0, st>>>(v, scaling, part);
+      else
+        distill_more_kernel<T, kShifted><<<nq, kGivenRuns * kGivenLanes, 0, st>>>(v, scaling, part);
+    };
+    if (type == ANN_F32)
+      add_up(0.0f);
+    else if (type == ANN_F16)
+      add_up(f16_t());
+    else
+      add_up(bf16_t());
     ANN_HIP(hipGetLastError());
-    a.given = k, a.ids = v.rows, a.more = v.more;
+    a.more_part = true;
     if (rows_side) {
       const bool few = type == ANN_F32 || nq <= kFewQueries;
       ann_status s = type == ANN_F32   ? distill_rows<float>(p, v, drows, few, ws, a, st)

@@ -24,19 +24,16 @@ inline ScoreTable score_table(const ann_row_scores &s) {
 }
 
 // What the gradients of the scores are asked for.  With `every`, g_logprob is a weight of every query's probabilities, whether a row is given
-// or not (targets: NULL), and what more is given for single elements of G, after its rounding, is added in fp32:
-//   of_queries   to dq[q]: more[q][e] * rows[ids[q][e]] for the `given` entries of every query (ids not below n: none)
-//   of_rows      to drows[j] (and drow_bias[j], its column d): sums[slots[j]] of more_ld elements, where slots[j] is not ANN_PAD_ID
+// or not (targets: NULL), and what more there is to single elements of G, after its rounding, is added in fp32:
+//   more_part    to dq: another part of its sums, which is in the workspace already (times what G is multiplied by)
+//   slots        to drows[j] (and drow_bias[j], its column d): sums[slots[j]] of more_ld elements, where slots[j] is not ANN_PAD_ID
 struct GradArgs {
   ScoreTable g;
   const uint32_t *targets;
   const float *lse, *entropy, *g_logprob, *g_entropy;
   const float *scaling;  // [2]: what G is multiplied by before it is rounded, and its inverse (f16)
   float *rest;           // [nq]: what the rounding of the given row's element left (16 bits)
-  bool every;
-  uint32_t given;
-  const uint32_t *ids;
-  const float *more;
+  bool every, more_part;
   const uint32_t *slots;
   const float *sums;
   uint32_t more_ld;
@@ -50,7 +47,8 @@ struct GradOut {
 
 constexpr uint32_t kFewQueries = 256;  // up to so many, the rows' gradient takes all of G's remainders
 
-uint64_t scores_backward_bytes(uint32_t nq, uint64_t n, uint32_t d, uint32_t type);
+uint64_t scores_backward_bytes(uint32_t nq, uint64_t n, uint32_t d, uint32_t type, bool more);
+float *scores_backward_more_part(uint32_t nq, uint64_t n, uint32_t d, uint32_t type, void *workspace);  // [nq][d]; there are queries and rows
 // scaling: of f16, [2]; written by launch_grad_scaling.
 ann_status launch_grad_scaling(const GradArgs &a, float *scaling, hipStream_t st);
 // a.scaling of f16: NULL to have it found (in the workspace).

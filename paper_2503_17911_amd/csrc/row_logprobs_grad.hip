@@ -41,6 +41,23 @@ __device__ __forceinline__ float more_of_row(const GradArgs &a, uint32_t row, ui
   const uint32_t slot = a.slots[row];
   return slot == ANN_PAD_ID ? 0.0f : a.sums[(uint64_t)slot * a.more_ld + c];
 }
+// The same for blocks of 32 rows from row0 on (those below `rows`) x 32 columns, block b at column c0 + b * columns; times `by`.  (Reads side by side:
+// one after the other they took 115 us of 381 for 50,000 x 768.)
+template <int BLOCKS>
+__device__ __forceinline__ void add_more(const GradArgs &a, uint32_t row0, uint32_t rows, uint32_t c0, float by, f32x16 (&acc)[BLOCKS]) {
+  uint32_t slot[16];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) slot[r] = row0 + block_row(r) < rows ? a.slots[row0 + block_row(r)] : ANN_PAD_ID;
+#pragma unroll
+  for (int b = 0; b < BLOCKS; ++b) {
+    const uint32_t c = c0 + b * 32 + lane_id() % 32;
+    float more[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) more[r] = slot[r] != ANN_PAD_ID && c < a.g.d ? a.sums[(uint64_t)slot[r] * a.more_ld + c] : 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[b][r] = __builtin_fmaf(more[r], by, acc[b][r]);
+  }
+}
 
 // scaling[0]: the power of two for G, scaling[1]: its inverse.  A query counts as it does in G: with g_logprob where a row is given, not at
 // all without a row left (or with statistics that are NaN).  Weights that are not finite spoil their own query, not the scale of the others.
@@ -224,20 +241,6 @@ __global__ __launch_bounds__(THREADS) void grad_queries_sum_kernel(GradArgs a, c
         for (int u = 0; u < 8; ++u) sum += v[u];
       }
       for (; s < end; ++s) sum += p[s * all];
-      if (a.given) {  // (shared out over the runs like the splits)
-        const float to = a.scaling ? a.scaling[0] : 1.0f;
-        for (uint32_t e0 = run; e0 < a.given; e0 += 8 * RUNS) {
-          float x[8], more[8];
-#pragma unroll
-          for (uint32_t u = 0; u < 8; ++u) {
-            const uint32_t e = e0 + u * RUNS, id = e < a.given ? a.ids[q * a.given + e] : ANN_PAD_ID;
-            more[u] = id < g.n ? a.more[q * a.given + e] * to : 0.0f;
-            x[u] = id < g.n ? to_f32(((const T *)g.rows)[id * g.row_stride + c]) : 0.0f;
-          }
-#pragma unroll
-          for (uint32_t u = 0; u < 8; ++u) sum = __builtin_fmaf(more[u], x[u], sum);
-        }
-      }
     }
     if constexpr (RUNS > 1) {
       __syncthreads();  // (the columns before have been read)
@@ -316,6 +319,10 @@ __global__ __launch_bounds__(256, RESTS ? 2 : kGradWaves<T>) void grad_rows_kern
       }
     }
   }
+  if (!SPLIT && a.slots) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) add_more<2>(a, row0 + rt * kTile + wave / 2 * 64 + i * 32, g.n, ct * kTile + wave % 2 * 64, a.scaling ? a.scaling[0] : 1.0f, acc[i]);
+  }
   const float by = a.scaling ? g.scale * a.scaling[1] : g.scale;
 #pragma unroll
   for (int i = 0; i < 2; ++i)
@@ -330,9 +337,7 @@ __global__ __launch_bounds__(256, RESTS ? 2 : kGradWaves<T>) void grad_rows_kern
             part[((uint64_t)split * rows + row) * g.d + c] = acc[i][j][r];
           } else {
             const bool left_out = g.bias && g.bias[row0 + row] == -INFINITY;  // (zero, whatever the queries hold)
-            float v = acc[i][j][r] * by;
-            if (a.slots) v = __builtin_fmaf(g.scale, more_of_row(a, row0 + row, c), v);
-            out[(uint64_t)(row0 + row) * stride + c] = from_f32<T>(left_out ? 0.0f : v);
+            out[(uint64_t)(row0 + row) * stride + c] = from_f32<T>(left_out ? 0.0f : acc[i][j][r] * by);
           }
         }
       }
@@ -597,6 +602,7 @@ __global__ __launch_bounds__(256, 2) void grad_short_kernel(GradArgs a, uint32_t
     }
   }
   if (OWN_ROWS && !drows) return;
+  if (OWN_ROWS && a.slots) add_more<KS / 2>(a, own0, g.n, 0, scaling, acc);
   const float by = a.scaling ? g.scale * a.scaling[1] : g.scale;
 #pragma unroll
   for (int b = 0; b < KS / 2; ++b) {
@@ -607,9 +613,7 @@ __global__ __launch_bounds__(256, 2) void grad_short_kernel(GradArgs a, uint32_t
       if (l >= owned || column >= g.d) continue;
       if constexpr (OWN_ROWS) {
         const bool left_out = BIAS && g.bias[l] == -INFINITY;  // (zero, whatever the queries hold)
-        float v = acc[b][r] * by;
-        if (a.slots) v = __builtin_fmaf(g.scale, more_of_row(a, l, column), v);
-        drows[l * stride + column] = from_f32<T>(left_out ? 0.0f : v);
+        drows[l * stride + column] = from_f32<T>(left_out ? 0.0f : acc[b][r] * by);
       } else {
         part[((uint64_t)split * g.nq + l) * g.d + column] = acc[b][r];
       }
@@ -627,7 +631,8 @@ struct BackwardPlan {
   Parts parts;
 };
 
-static BackwardPlan backward_plan(uint32_t nq, uint64_t n, uint32_t d, uint32_t type) {
+// more: room for another part of the queries' sums, behind the splits'.
+static BackwardPlan backward_plan(uint32_t nq, uint64_t n, uint32_t d, uint32_t type, bool more) {
   BackwardPlan p;
   if (nq == 0 || n == 0) return p;
   p.q_tiles = (nq + kTile - 1) / kTile;
@@ -635,7 +640,7 @@ static BackwardPlan backward_plan(uint32_t nq, uint64_t n, uint32_t d, uint32_t 
     p.slices = d <= 64 ? 4 : d <= 96 ? 6 : 8;
     const uint32_t tiles = (uint32_t)((n + kPassing - 1) / kPassing), want = ((kShortTarget + p.q_tiles - 1) / p.q_tiles + 7) / 8 * 8;
     p.splits = want < tiles ? want : tiles;
-    p.part_at = p.parts.take((uint64_t)p.splits * nq * d * sizeof(float));
+    p.part_at = p.parts.take((uint64_t)(p.splits + more) * nq * d * sizeof(float));
     p.scaling_at = p.parts.take(2 * sizeof(float));
     p.rest_at = p.parts.take(nq * sizeof(float));
     return p;
@@ -664,7 +669,7 @@ static BackwardPlan backward_plan(uint32_t nq, uint64_t n, uint32_t d, uint32_t 
   }
   p.g_at = p.parts.take(p.chunk * row_bytes);
   if (type != ANN_F32 && nq <= kFewQueries) p.rests_at = p.parts.take(p.chunk * row_bytes);
-  p.part_at = p.parts.take((uint64_t)p.splits * nq * d * sizeof(float));
+  p.part_at = p.parts.take((uint64_t)(p.splits + more) * nq * d * sizeof(float));
   // (one chunk whose tiles leave compute units with one workgroup or none: runs of queries, of 64 at least)
   const uint32_t row_tiles = p.chunk / kTile * c_tiles;
   if (chunks == 1 && row_tiles < 512) {
@@ -730,10 +735,11 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
     ANN_HIP(hipGetLastError());
     if (o.dq) {
       // (256 splits of 256 queries: 15.5 us by two wavefronts to a query)
-      if (p.splits >= 64)
-        grad_queries_sum_kernel<T, 128, 8, 1024><<<g.nq, 1024, 0, st>>>(a, part, p.splits, (T *)o.dq, o.dq_stride);
+      const uint32_t splits = p.splits + (a.more_part ? 1 : 0);
+      if (splits >= 64)
+        grad_queries_sum_kernel<T, 128, 8, 1024><<<g.nq, 1024, 0, st>>>(a, part, splits, (T *)o.dq, o.dq_stride);
       else
-        grad_queries_sum_kernel<T, 128, 1, 256><<<(g.nq + 1) / 2, 256, 0, st>>>(a, part, p.splits, (T *)o.dq, o.dq_stride);
+        grad_queries_sum_kernel<T, 128, 1, 256><<<(g.nq + 1) / 2, 256, 0, st>>>(a, part, splits, (T *)o.dq, o.dq_stride);
       ANN_HIP(hipGetLastError());
     }
     return ANN_OK;
@@ -807,16 +813,21 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
     }
   }
   if (o.dq && g.nq) {
-    grad_queries_sum_kernel<T, 256, 1, 256><<<g.nq, 256, 0, st>>>(a, part, g.n ? p.splits : 0, (T *)o.dq, o.dq_stride);
+    grad_queries_sum_kernel<T, 256, 1, 256><<<g.nq, 256, 0, st>>>(a, part, g.n ? p.splits + (a.more_part ? 1 : 0) : 0, (T *)o.dq, o.dq_stride);
     ANN_HIP(hipGetLastError());
   }
   return ANN_OK;
 }
 
-uint64_t scores_backward_bytes(uint32_t nq, uint64_t n, uint32_t d, uint32_t type) { return backward_plan(nq, n, d, type).parts.bytes; }
+uint64_t scores_backward_bytes(uint32_t nq, uint64_t n, uint32_t d, uint32_t type, bool more) { return backward_plan(nq, n, d, type, more).parts.bytes; }
+
+float *scores_backward_more_part(uint32_t nq, uint64_t n, uint32_t d, uint32_t type, void *workspace) {
+  const BackwardPlan p = backward_plan(nq, n, d, type, true);
+  return (float *)((char *)workspace + p.part_at) + (uint64_t)p.splits * nq * d;
+}
 
 ann_status scores_backward(uint32_t type, const GradArgs &a, const GradOut &o, void *workspace, hipStream_t st) {
-  const BackwardPlan p = backward_plan(a.g.nq, a.g.n, a.g.d, type);
+  const BackwardPlan p = backward_plan(a.g.nq, a.g.n, a.g.d, type, a.more_part);
   if (type == ANN_F32) return backward<float>(a, p, o, (char *)workspace, st);
   if (type == ANN_F16) return backward<f16_t>(a, p, o, (char *)workspace, st);
   return backward<bf16_t>(a, p, o, (char *)workspace, st);
@@ -828,7 +839,7 @@ using namespace ann;
 
 extern "C" uint64_t ann_row_logprobs_backward_workspace(uint32_t nq, uint64_t n, uint32_t d, uint32_t type) {
   if (n > kMaxRows || nq >= kMaxQueries || d == 0 || type > ANN_BF16) return 0;
-  return backward_plan(nq, n, d, type).parts.bytes;
+  return backward_plan(nq, n, d, type, false).parts.bytes;
 }
 
 extern "C" ann_status ann_row_logprobs_backward(const ann_row_scores *scores, const float *lse, const float *entropy, const float *g_logprob,
@@ -839,7 +850,7 @@ extern "C" ann_status ann_row_logprobs_backward(const ann_row_scores *scores, co
   if (scores->nq && g_entropy && !entropy) return fail(ANN_EINVAL, "ann_row_logprobs_backward: g_entropy without entropy");
   if (dq && dq_stride < scores->d) return fail(ANN_EINVAL, "ann_row_logprobs_backward: dq_stride is shorter than a row");
   if (drows && drows_stride < scores->d) return fail(ANN_EINVAL, "ann_row_logprobs_backward: drows_stride is shorter than a row");
-  if (ann_status s = check_workspace("ann_row_logprobs_backward", workspace, workspace_bytes, scores_backward_bytes(scores->nq, scores->n, scores->d, scores->type)))
+  if (ann_status s = check_workspace("ann_row_logprobs_backward", workspace, workspace_bytes, scores_backward_bytes(scores->nq, scores->n, scores->d, scores->type, false)))
     return s;
   GradArgs a = {};
   a.g = score_table(*scores);
