@@ -63,55 +63,66 @@ struct GivenArgs {
   uint32_t *rows;   // [nq][k]: the entries' ids; ANN_PAD_ID where none counts
   float *weights;   // [nq][k]: -g t
   float *more;      // [nq][k]: that and what the rounding left
-  uint32_t *slots;  // [n]: filled with ANN_PAD_ID (NULL: not wanted)
+  uint32_t *slots;  // [n]: filled with ANN_PAD_ID (NULL where not wanted)
 };
 
-// A query's entries, one to a lane of a wavefront; workgroups behind the queries' only fill.
-__global__ __launch_bounds__(256) void distill_given_kernel(GivenArgs a) {
-  if (a.slots)
-    for (uint64_t j = (uint64_t)blockIdx.x * 256 + threadIdx.x; j < a.g.n; j += (uint64_t)gridDim.x * 256) a.slots[j] = ANN_PAD_ID;
-  const uint32_t q = blockIdx.x * 4 + threadIdx.x / kWave, e = lane_id();
-  if (q >= a.g.nq) return;
+// Of a query's entries, one to a lane of a wavefront: id (ANN_PAD_ID: it does not count), -g t, and -g T of the query.
+struct Entry {
+  uint32_t id;
+  float weight, whole;
+};
+__device__ __forceinline__ Entry given_entry(const GivenArgs &a, uint32_t q, uint32_t e) {
   const uint64_t at = (uint64_t)q * a.k + e;
   const bool in = e < a.k, none = a.lse[q] == -INFINITY;
   uint32_t id = in ? a.ids[at] : ANN_PAD_ID;
   const float given = in && id < a.g.n ? a.given[at] : -INFINITY;
-  if (given == -INFINITY) id = ANN_PAD_ID;  // (no weight: it does not count, whatever its row)
+  if (given == -INFINITY) id = ANN_PAD_ID;  // (no weight, whatever its row)
   const float g = a.g_loss[q];
   const double t = id < a.g.n ? exp((double)given) : 0.0, all = group_sum_f64<kWave>(t);
   // no row left for this query, the row left out: no gradient
   if (none || (id < a.g.n && a.g.bias && a.g.bias[id] == -INFINITY)) id = ANN_PAD_ID;
-  if (e == 0) a.whole[q] = none ? 0.0f : -(float)((double)g * all);
-  if (in) a.rows[at] = id, a.weights[at] = -(float)((double)g * t);
+  return {id < a.g.n ? id : ANN_PAD_ID, -(float)((double)g * t), none ? 0.0f : -(float)((double)g * all)};
+}
+
+// The queries' weights alone, before the power of two that they ask for (f16).
+__global__ __launch_bounds__(256) void distill_whole_kernel(GivenArgs a) {
+  const uint32_t q = blockIdx.x * 4 + threadIdx.x / kWave;
+  if (q >= a.g.nq) return;
+  const Entry entry = given_entry(a, q, lane_id());
+  if (lane_id() == 0) a.whole[q] = entry.whole;
 }
 
 // An entry's weight and what the rounding of the first part's element left, which is taken once for a row that is given twice; and their sum over the
-// query's entries of more * row: a workgroup to a query, 256 columns in pieces at a time, kGivenRuns runs of entries side by side.  T: the type
-// that G is rounded to.  part NULL: the entries alone.
+// query's entries of more * row: a workgroup to a query, kGivenLanes pieces of columns at a time, kGivenRuns runs of entries side by side.  T: the type
+// that G is rounded to.  part NULL: the entries alone.  Workgroups behind the queries' only fill the slots.
 constexpr uint32_t kGivenRuns = 8, kGivenLanes = 32;
 template <typename T, RowEnd END>
 __global__ __launch_bounds__(kGivenRuns * kGivenLanes) void distill_more_kernel(GivenArgs a, const float *__restrict__ scaling, float *__restrict__ part) {
   constexpr int VEC = 16 / (int)sizeof(T), kEach = ANN_MAX_ALTERNATIVES / kGivenRuns;
   __shared__ float more_of[ANN_MAX_ALTERNATIVES], room[kGivenRuns][kGivenLanes * VEC + 4];
   __shared__ uint32_t id_of[ANN_MAX_ALTERNATIVES];
+  if (a.slots)
+    for (uint64_t j = (uint64_t)blockIdx.x * 256 + threadIdx.x; j < a.g.n; j += (uint64_t)gridDim.x * 256) a.slots[j] = ANN_PAD_ID;
   const uint32_t q = blockIdx.x, lane = threadIdx.x % kGivenLanes, run = threadIdx.x / kGivenLanes;
+  if (q >= a.g.nq) return;
   const float by = scaling ? scaling[0] : 1.0f, back = scaling ? scaling[1] : 1.0f;
   if (threadIdx.x < kWave) {
     const uint32_t e = threadIdx.x;
     const uint64_t at = (uint64_t)q * a.k + e;
-    const uint32_t id = e < a.k ? a.rows[at] : ANN_PAD_ID;
+    const Entry entry = given_entry(a, q, e);
     bool again = false;
-    for (uint32_t o = 0; o < a.k; ++o) again |= (uint32_t)__builtin_amdgcn_readlane((int)id, (int)o) == id && o < e;
+    for (uint32_t o = 0; o < a.k; ++o) again |= (uint32_t)__builtin_amdgcn_readlane((int)entry.id, (int)o) == entry.id && o < e;
     float more = 0.0f;
     if (e < a.k) {
-      more = a.weights[at];
-      if (sizeof(T) == 2 && id < a.g.n && !again) {
-        const float v = -(expf(a.logprobs[at]) * (a.whole[q] * by));
+      more = entry.weight;
+      if (sizeof(T) == 2 && entry.id < a.g.n && !again) {
+        const float v = -(expf(a.logprobs[at]) * (entry.whole * by));
         more = __builtin_fmaf(v - to_f32(from_f32<T>(v)), back, more);
       }
-      a.more[at] = more;
+      a.rows[at] = entry.id, a.weights[at] = entry.weight, a.more[at] = more;
     }
-    more_of[e] = more * by, id_of[e] = id;
+    if (e == 0) a.whole[q] = entry.whole;
+    more_of[e] = more * by, id_of[e] = entry.id;
   }
   if (!part) return;
   __syncthreads();
@@ -288,22 +299,22 @@ extern "C" ann_status ann_row_distillation_backward(const ann_row_scores *scores
     v.g = a.g, v.k = k, v.ids = given_ids, v.given = given_logprobs, v.logprobs = logprobs, v.lse = lse, v.g_loss = g_loss;
     v.whole = (float *)(ws + p.whole_at), v.rows = (uint32_t *)(ws + p.rows_at), v.weights = (float *)(ws + p.weights_at), v.more = (float *)(ws + p.more_at);
     v.slots = rows_side ? (uint32_t *)(ws + p.slots_at) : nullptr;
-    const uint32_t of_queries = (nq + 3) / 4, filling = rows_side ? (uint32_t)((scores->n + 4095) / 4096 < 2048 ? (scores->n + 4095) / 4096 : 2048) : 0;
-    distill_given_kernel<<<of_queries > filling ? of_queries : filling, 256, 0, st>>>(v);
-    ANN_HIP(hipGetLastError());
+    const uint32_t filling = rows_side ? (uint32_t)((scores->n + 4095) / 4096 < 2048 ? (scores->n + 4095) / 4096 : 2048) : 0, blocks = nq > filling ? nq : filling;
     a.g_logprob = v.whole;
     float *scaling = nullptr, *part = dq ? scores_backward_more_part(nq, scores->n, scores->d, type, ws) : nullptr;
     if (type == ANN_F16) {
       scaling = (float *)(ws + p.scaling_at);
+      distill_whole_kernel<<<(nq + 3) / 4, 256, 0, st>>>(v);
+      ANN_HIP(hipGetLastError());
       if (ann_status s = launch_grad_scaling(a, scaling, st)) return s;
       a.scaling = scaling;
     }
     const auto add_up = [&](auto t) {
       typedef decltype(t) T;
       if (scores->d % (16 / sizeof(T)) == 0)
-        distill_more_kernel<T, kWholePieces><<<nq, kGivenRuns * kGivenLanes, 0, st>>>(v, scaling, part);
+        distill_more_kernel<T, kWholePieces><<<blocks, kGivenRuns * kGivenLanes, 0, st>>>(v, scaling, part);
       else
-        distill_more_kernel<T, kShifted><<<nq, kGivenRuns * kGivenLanes, 0, st>>>(v, scaling, part);
+        distill_more_kernel<T, kShifted><<<blocks, kGivenRuns * kGivenLanes, 0, st>>>(v, scaling, part);
     };
     if (type == ANN_F32)
       add_up(0.0f);
