@@ -231,36 +231,58 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortPass p, Be
   }
 }
 
-// Up to kSmallSort entries: an entry's place is the number of entries before it in the order, counted against all of them.  n^2 comparisons
-// of two instructions are 1.3 us of the card for 5,000 entries (one workgroup's radix sort: 16 us).  A workgroup takes 16 entries, the keys in LDS; 64 slices of
-// the keys to its lanes, the slices' counts are joined in LDS.
+// Up to kSmallSort entries: an entry's place is the number of entries before it in the order, counted against all of them (one workgroup's
+// radix sort of 5,000 took 16 us, the passes of many some 27).  A workgroup takes 32 entries, two to a lane, so that a key read from LDS serves both; 64 slices of
+// the keys to its lanes, whose counts are joined in LDS.
+constexpr uint32_t kSmallOwn = 32;
 template <typename Beside>
 __global__ __launch_bounds__(kSmallThreads) void sort_small_kernel(SortPass p, Beside beside) {
-  constexpr uint32_t kOwn = 16, kSlices = kSmallThreads / kOwn;
-  __shared__ __attribute__((aligned(16))) uint32_t keys[kSmallSort];
-  __shared__ uint32_t counts[kOwn];
+  constexpr uint32_t kLanes = kSmallOwn / 2, kSlices = kSmallThreads / kLanes;
+  __shared__ __attribute__((aligned(16))) uint32_t keys[kSmallSort + 8 * kSlices];
+  __shared__ uint32_t counts[kSmallOwn];
   if (blockIdx.x >= p.blocks) return beside(0, blockIdx.x - p.blocks, gridDim.x - p.blocks);
-  const uint32_t slice_keys = ((p.n + kSlices - 1) / kSlices + 3) / 4 * 4, padded = slice_keys * kSlices;
-  for (uint32_t i = threadIdx.x; i < padded && i < kSmallSort; i += kSmallThreads) keys[i] = i < p.n ? sort_key(p, i) : 0xFFFFFFFFu;
-  if (threadIdx.x < kOwn) counts[threadIdx.x] = 0;
-  __syncthreads();
-  const uint32_t i = blockIdx.x * kOwn + threadIdx.x % kOwn, begin = threadIdx.x / kOwn * slice_keys, end = begin + slice_keys;
-  if (i < p.n) {
-    const uint32_t key = keys[i];
-    uint32_t before = 0;
-    if (i >= end || i < begin) {
-      const uint32_t below = key + (i >= end);  // (equal ids before it stay before it; ids are at most 2^31)
-      for (uint32_t j = begin; j < end; j += 4) {
-        const uint4 k = *(const uint4 *)(keys + j);
-        before += (k.x < below) + (k.y < below) + (k.z < below) + (k.w < below);
-      }
-    } else {
-      for (uint32_t j = begin; j < end; ++j) before += keys[j] < key + (j < i);
-    }
-    atomicAdd(&counts[threadIdx.x % kOwn], before);
+  const uint32_t slice_keys = ((p.n + kSlices - 1) / kSlices + 3) / 8 * 8 + 4, padded = slice_keys * kSlices;  // (pieces of 16 bytes, an odd number: slices side by side lie in other banks)
+  for (uint32_t i0 = threadIdx.x; i0 < padded; i0 += 8 * kSmallThreads) {  // (eight on their way: one after the other they took longer than all else)
+    uint32_t k[8];
+#pragma unroll
+    for (uint32_t u = 0; u < 8; ++u) k[u] = i0 + u * kSmallThreads < p.n ? sort_key(p, i0 + u * kSmallThreads) : 0xFFFFFFFFu;
+#pragma unroll
+    for (uint32_t u = 0; u < 8; ++u)
+      if (i0 + u * kSmallThreads < padded) keys[i0 + u * kSmallThreads] = k[u];
   }
+  if (threadIdx.x < kSmallOwn) counts[threadIdx.x] = 0;
   __syncthreads();
-  if (threadIdx.x < kOwn && i < p.n) {
+  const uint32_t begin = threadIdx.x / kLanes * slice_keys, end = begin + slice_keys;
+  uint32_t own[2], key[2], before[2] = {0, 0};
+  bool mixed = false;  // a slice with entries before and behind one of the lane's
+#pragma unroll
+  for (int o = 0; o < 2; ++o) {
+    own[o] = blockIdx.x * kSmallOwn + threadIdx.x % kLanes + o * kLanes;
+    key[o] = own[o] < p.n ? keys[own[o]] : 0;
+    mixed |= own[o] >= begin && own[o] < end;
+  }
+  if (!mixed) {
+    const uint32_t below[2] = {key[0] + (own[0] >= end), key[1] + (own[1] >= end)};  // (equal ids before it stay before it; ids are at most 2^31)
+#pragma unroll 4
+    for (uint32_t j = begin; j < end; j += 4) {
+      const uint4 k = *(const uint4 *)(keys + j);
+#pragma unroll
+      for (int o = 0; o < 2; ++o) before[o] += (k.x < below[o]) + (k.y < below[o]) + (k.z < below[o]) + (k.w < below[o]);
+    }
+  } else {
+#pragma unroll 4
+    for (uint32_t j = begin; j < end; j += 4) {
+      const uint4 k = *(const uint4 *)(keys + j);
+#pragma unroll
+      for (int o = 0; o < 2; ++o)
+        before[o] += (k.x < key[o] + (j < own[o])) + (k.y < key[o] + (j + 1 < own[o])) + (k.z < key[o] + (j + 2 < own[o])) + (k.w < key[o] + (j + 3 < own[o]));
+    }
+  }
+#pragma unroll
+  for (int o = 0; o < 2; ++o) atomicAdd(&counts[threadIdx.x % kLanes + o * kLanes], before[o]);
+  __syncthreads();
+  const uint32_t i = blockIdx.x * kSmallOwn + threadIdx.x;
+  if (threadIdx.x < kSmallOwn && i < p.n) {
     const uint32_t to = counts[threadIdx.x];
     p.out_keys[to] = keys[i], p.out_at[to] = i;
   }
@@ -272,7 +294,7 @@ static ann_status sort_ids(const IdSortPlan &plan, const uint32_t *ids, void *wo
   const auto word = [&](uint64_t at) { return (uint32_t *)(ws + at); };
   SortPass p = {};
   p.n = plan.n, p.rows = plan.rows, p.bits = plan.bits, p.rounds = plan.rounds, p.counts = word(plan.counts_at), p.totals = word(plan.totals_at);
-  p.blocks = plan.n <= kSmallSort ? (plan.n + 15) / 16 : plan.blocks;
+  p.blocks = plan.n <= kSmallSort ? (plan.n + kSmallOwn - 1) / kSmallOwn : plan.blocks;
   int to = 0;
   for (uint32_t pass = 0; pass < plan.passes; ++pass, to ^= 1) {
     p.keys = pass == 0 ? ids : word(plan.keys_at[to ^ 1]), p.at = pass == 0 ? nullptr : word(plan.at_at[to ^ 1]);

@@ -352,12 +352,13 @@ __global__ __launch_bounds__(256) void grad_rows_sum_kernel(GradArgs a, uint32_t
   const uint64_t all = (uint64_t)rows * g.d, at = (uint64_t)blockIdx.x * 256 + threadIdx.x;
   if (at >= all) return;
   const float by = a.scaling ? g.scale * a.scaling[1] : g.scale;
+  const uint64_t row = row0 + at / g.d;
+  const float more = a.slots ? more_of_row(a, (uint32_t)row, (uint32_t)(at % g.d)) : 0.0f;
   float sum = 0.0f;
   for (uint32_t s = 0; s < splits; ++s) sum += part[s * all + at];
-  const uint64_t row = row0 + at / g.d;
   const bool left_out = g.bias && g.bias[row] == -INFINITY;
   float v = sum * by;
-  if (a.slots) v = __builtin_fmaf(g.scale, more_of_row(a, (uint32_t)row, (uint32_t)(at % g.d)), v);
+  if (a.slots) v = __builtin_fmaf(g.scale, more, v);
   out[row * stride + at % g.d] = from_f32<T>(left_out ? 0.0f : v);
 }
 

@@ -85,8 +85,8 @@ def check(ann, n, rows, d, law, dtype, ttype, pad, shift):
     need = ann.ann_embedding_backward_workspace(n, rows, d)
     ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")   # (NaN wherever it is read before it is written)
     half, tiny = R.half_step(tt), R.smallest_step(tt)
-    # as many additions as the row has terms, and at most eight to join its parts
-    off = ((count + 8) * R.U32)[:, None] * size
+    # as many additions as the row has terms, and at most sixteen to join its parts
+    off = ((count + 16) * R.U32)[:, None] * size
     for accumulate in (False, True):
         out = torch.full((rows, d + pad), 7.0, dtype=tt, device="cuda")
         if accumulate:
