@@ -13,6 +13,13 @@ from pathlib import Path
 
 import os
 
+# PyTorch brings a HIP runtime of its own.  Where it is there, it is loaded first and the library uses the same one: with the library first, a process
+# holds two, and calls on torch's tensors find no device.
+try:
+    import torch  # noqa: F401
+except ImportError:
+    pass
+
 _PKG = Path(__file__).resolve().parent
 # ANN_LIBRARY_PATH selects another build of the same library (e.g. one compiled
 # with extra instrumentation); the default is the in-tree build.
