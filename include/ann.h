@@ -575,7 +575,8 @@ uint64_t ann_embedding_backward_workspace(uint64_t n, uint64_t rows, uint32_t di
  *                NULL where not wanted, and without a residual.
  *   rstd         [n] fp32, for the backward pass; NULL allowed.
  * sum may be x or residual, y may be x or residual (same strides); sum and y are not
- * the same rows.  n = 0 does nothing.  dim <= ANN_MAX_NORM_DIM.
+ * the same rows.  Squares may leave fp32's range: every row of finite elements has its rstd (a row with an infinite element: 0).
+ * n = 0 does nothing.  dim <= ANN_MAX_NORM_DIM.
  * Errors: ANN_EINVAL (NULL x or y, dim == 0, types, strides, sum without residual or over y, eps negative
  * or NaN), ANN_ECAPACITY.
  */
@@ -591,7 +592,7 @@ ann_status ann_rms_norm(const void *x, uint64_t n, uint32_t dim, uint64_t x_stri
  *   group        32, 64 or 128 columns (the last group of a row may be shorter), or 0: one scale to a row.
  *   scales       [n] rows of ceil(dim / group) (group 0: one) fp32.
  * y is not x or residual.  Values that are not numbers get the code for that and do not
- * count for their group's scale.  Otherwise as ann_rms_norm; ANN_EINVAL also for
+ * count for their group's scale; infinite ones (weights that are) make it infinite.  Otherwise as ann_rms_norm; ANN_EINVAL also for
  * another group, scales NULL or scale_stride shorter than a row's scales.
  */
 ann_status ann_rms_norm_e4m3(const void *x, uint64_t n, uint32_t dim, uint64_t x_stride, uint32_t type,
@@ -704,7 +705,8 @@ uint64_t ann_row_logprobs_backward_workspace(uint32_t nq, uint64_t n, uint32_t d
  *   given_ids, given_logprobs  [nq][k]; entries whose id is not below n (ANN_PAD_ID)
  *                or whose log probability is -infinity do not count.
  *   loss[i]      = sum_e t_ie (given_logprobs[i][e] - logprobs[i][e]),  t = exp(given_logprobs);
- *                the divergence of the softmax over all rows from the teacher's, as far as its list goes.
+ *                the divergence of the softmax over all rows from the teacher's, as far as its list goes (where the
+ *                t sum to less than one, it is smallest, T log T with their sum T, where the model gives the listed rows all its probability).
  *                +infinity where a row that counts is left out; 0 where none counts.
  *   lse[i]       as ann_row_logprobs returns it.
  *   logprobs     [nq][k] the log probabilities of the given rows under the softmax of all rows'

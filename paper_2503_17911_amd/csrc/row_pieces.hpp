@@ -162,6 +162,17 @@ struct RowPiece {
       }
     }
   }
+  // Past the caches.
+  __device__ __forceinline__ void store_past(T *row, uint32_t c, uint32_t columns) const {
+    typedef uint32_t Vector __attribute__((ext_vector_type(4)));
+    typedef Vector Unaligned __attribute__((aligned(2), may_alias));
+    if (kWords == 4 && (END == kWholePieces ? c < columns : c + N <= columns)) {
+      const Vector v = {w[0], w[1 % kWords], w[2 % kWords], w[3 % kWords]};
+      __builtin_nontemporal_store(v, (Unaligned *)(row + c));
+    } else {
+      store(row, c, columns);
+    }
+  }
   __device__ __forceinline__ void store(T *row, uint32_t c, uint32_t columns) const {
     if (END == kWholePieces ? c < columns : c + N <= columns) {
       P p;

@@ -155,3 +155,56 @@ def test_same_bits_again_on_other_streams_and_in_graphs():
             graph.replay()
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(want[:2], graphed[:2])), replay
+
+
+def test_many_tokens():
+    """More than the sort's blocks take in eight rounds, and more chunks than there may be of the shortest; ones are summed exactly."""
+    import paper_2503_17911_amd as ann
+    n, rows = 17_500_000, 5000
+    g = torch.Generator(device="cuda").manual_seed(1)
+    ids = (torch.exp(torch.rand(n, generator=g, device="cuda") * math.log(rows + 1.0)) - 1).int()
+    out = torch.empty(rows, 1, device="cuda")
+    need = ann.ann_embedding_backward_workspace(n, rows, 1)
+    ann.ann_embedding_backward(torch.ones(n, 1, device="cuda", dtype=torch.bfloat16), 1, ann.BF16, ids, n, 1.0, rows, 1, out, 1, ann.F32,
+                               workspace=torch.empty(need, dtype=torch.uint8, device="cuda"), workspace_bytes=need, stream=stream())
+    count = torch.bincount(ids[ids < rows], minlength=rows)
+    assert count.max() > 1 << 20 and torch.equal(out[:, 0].double(), count.double())
+
+
+def test_offsets_beyond_32_bits():
+    """Rows of the table, of y and of dy that lie more than 2^32 elements from the first."""
+    import paper_2503_17911_amd as ann
+    d, stride, rows = 8, 1 << 22, 1100
+    far = torch.empty(rows * stride, dtype=torch.bfloat16, device="cuda")   # 9.2 GB, of which every row's first elements are used
+    table = far.view(rows, stride)
+    table[:, :d] = torch.randn(rows, d, device="cuda").bfloat16()
+    near = table[:, :d].contiguous()
+    ids = torch.randperm(rows, device="cuda").int()
+    y, y_far = torch.empty(rows, d, dtype=torch.bfloat16, device="cuda"), table[:, 64:]
+    ann.ann_embedding(near, rows, d, d, ann.BF16, ids, rows, 2.0, y, d, ann.BF16, stream())
+    ann.ann_embedding(table, rows, d, stride, ann.BF16, ids, rows, 2.0, y_far, stride, ann.BF16, stream())
+    assert torch.equal(y, y_far[:, :d]) and torch.equal(y, (2 * near.float())[ids.long()].bfloat16())
+    need = ann.ann_embedding_backward_workspace(rows, rows, d)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    grad, grad_far = torch.empty_like(y), table[:, 128:]
+    ann.ann_embedding_backward(y, d, ann.BF16, ids, rows, 0.5, rows, d, grad, d, ann.BF16, workspace=ws, workspace_bytes=need, stream=stream())
+    ann.ann_embedding_backward(y_far, stride, ann.BF16, ids, rows, 0.5, rows, d, grad_far, stride, ann.BF16, workspace=ws, workspace_bytes=need, stream=stream())
+    assert torch.equal(grad, near) and torch.equal(grad_far[:, :d], near)
+
+
+def test_rows_without_a_token_stay_as_they_are_between_batches():
+    """Several batches into one gradient, the table's rows among them that it is also scored against: each is rounded into the table's type once."""
+    import paper_2503_17911_amd as ann
+    rows, d = 64, 40
+    out = torch.randn(rows, d, device="cuda").bfloat16()
+    want = out.clone()
+    for n in (0, 5, 300):
+        ids, dy = on_gpu(tokens(n, rows, "even", n)), torch.randint(-4, 5, (n, d), device="cuda").bfloat16()
+        need = ann.ann_embedding_backward_workspace(n, rows, d)
+        ann.ann_embedding_backward(dy, d, ann.BF16, ids, n, 1.0, rows, d, out, d, ann.BF16, accumulate=True,
+                                   workspace=torch.empty(max(need, 1), dtype=torch.uint8, device="cuda"), workspace_bytes=need, stream=stream())
+        there = (ids >= 0) & (ids < rows)
+        add = torch.zeros(rows, d, device="cuda").index_add_(0, ids[there].long(), dy[there].float())   # (whole numbers: exact)
+        hit = torch.bincount(ids[there].long(), minlength=rows) > 0
+        want = torch.where(hit[:, None], (want.float() + add).bfloat16(), want)
+        assert torch.equal(out, want)

@@ -329,3 +329,62 @@ def test_same_bits_again_on_other_streams_and_in_graphs():
             graph.replay()
             torch.cuda.synchronize()
             assert all(torch.equal(a, c) for a, c in zip(want[:6], graphed[:6])), replay
+
+
+@pytest.mark.parametrize("dtype, nq, n, d", [("f32", 3000, 50_000, 136), ("f16", 5000, 60_000, 144), ("bf16", 300, 20_000, 1000)])
+def test_several_chunks_of_rows(dtype, nq, n, d):
+    """More scores than are kept at a time: against 64 bits on the GPU, by the sums' sizes."""
+    import paper_2503_17911_amd as ann
+    g = torch.Generator(device="cuda").manual_seed(1)
+    k, scale, t = 12, 8.0, R.DTYPES[dtype]
+    q, rows = (unit(torch.randn(m, d, generator=g, device="cuda")).to(t) for m in (nq, n))
+    b = torch.randn(n, generator=g, device="cuda")
+    ids, given = torch.randint(n, (nq, k), generator=g, device="cuda").int(), -2.0 - torch.rand(nq, k, generator=g, device="cuda")
+    ids[:, 0] = 7
+    loss, lse, logprobs = torch.empty(nq, device="cuda"), torch.empty(nq, device="cuda"), torch.empty(nq, k, device="cuda")
+    T = types(ann)[t]
+    table = dict(q=q, nq=nq, q_stride=d, rows=rows, n=n, row_stride=d, d=d, type=T, scale=scale, row_bias=b, k=k, given_ids=ids, given_logprobs=given, lse=lse,
+                 logprobs=logprobs, stream=stream())
+    need, needb = ann.ann_row_distillation_workspace(nq, n, d, T, k), ann.ann_row_distillation_backward_workspace(nq, n, d, T, k)
+    ann.ann_row_distillation(**table, loss=loss, workspace=dirty(need), workspace_bytes=need)
+    gl = torch.rand(nq, generator=g, device="cuda") + 0.5
+    dq, drows, db = torch.empty_like(q), torch.empty_like(rows), torch.empty(n, device="cuda")
+    ann.ann_row_distillation_backward(**table, g_loss=gl, dq=dq, dq_stride=d, drows=drows, drows_stride=d, drow_bias=db, workspace=dirty(needb), workspace_bytes=needb)
+    q64, x64 = q.double(), rows.double()
+    z = torch.mm(q64, x64.t().contiguous()) * scale + b.double()
+    lse64 = torch.logsumexp(z, 1)
+    assert ((lse.double() - lse64).abs() <= 1e-5).all()
+    logp = (z - lse64[:, None]).gather(1, ids.long())
+    w = given.double().exp()
+    want = (w * (given.double() - logp)).sum(1)
+    assert ((loss.double() - want).abs() <= 1e-5 * w.sum(1) + 2 * R.U32 * want.abs()).all()
+    A = (z - lse.double()[:, None]).exp_() * (gl.double() * w.sum(1))[:, None]
+    del z
+    B = torch.zeros_like(A).scatter_add_(1, ids.long(), -gl.double()[:, None] * w)
+    # a score errs by some 1e-5, sums of up to 60,000 terms by their own; 16 bits round every element of the first part and the result
+    half = R.half_step(t)
+    kept = half if dtype != "f32" else 2.0 ** -23
+    G, size = A + B, A.abs() * (kept + 2e-5) + B.abs() * 2e-5
+    for got, exact, off in ((dq, torch.mm(G, x64), torch.mm(size, x64.abs())), (drows, torch.mm(G.t().contiguous(), q64), torch.mm(size.t().contiguous(), q64.abs()))):
+        assert ((got.double() - scale * exact).abs() <= (half * scale * exact.abs() + R.smallest_step(t) + scale * off) * (1 + half)).all()
+    assert ((db.double() - G.sum(0)).abs() <= ((A.abs() + B.abs()) * 2e-5).sum(0)).all()
+
+
+def test_offsets_beyond_32_bits():
+    import paper_2503_17911_amd as ann
+    nq, n, d, k, stride = 6, 1100, 64, 5, 1 << 22
+    far = torch.empty(n * stride, dtype=torch.bfloat16, device="cuda").view(n, stride)   # 9.2 GB
+    far[:, :d] = unit(torch.randn(n, d, device="cuda")).bfloat16()
+    near = far[:, :d].contiguous()
+    q, ids, given = near[-nq:].clone(), torch.randint(n, (nq, k), device="cuda").int(), torch.full((nq, k), -1.8, device="cuda")
+    got = []
+    for rows, s, drows, ds in ((near, d, torch.empty_like(near), d), (far, stride, far[:, 128:], stride)):
+        out = [torch.empty(nq, device="cuda"), torch.empty(nq, device="cuda"), torch.empty(nq, k, device="cuda"), torch.empty_like(q)]
+        table = dict(q=q, nq=nq, q_stride=d, rows=rows, n=n, row_stride=s, d=d, type=ann.BF16, scale=20.0, k=k, given_ids=ids, given_logprobs=given, lse=out[1],
+                     logprobs=out[2], stream=stream())
+        need, needb = ann.ann_row_distillation_workspace(nq, n, d, ann.BF16, k), ann.ann_row_distillation_backward_workspace(nq, n, d, ann.BF16, k)
+        ann.ann_row_distillation(**table, loss=out[0], workspace=dirty(need), workspace_bytes=need)
+        ann.ann_row_distillation_backward(**table, g_loss=torch.ones(nq, device="cuda"), dq=out[3], dq_stride=d, drows=drows, drows_stride=ds, workspace=dirty(needb),
+                                          workspace_bytes=needb)
+        got.append(out + [drows[:, :d].clone()])
+    assert all(torch.equal(a, c) for a, c in zip(*got)) and (got[0][4] != 0).any()
