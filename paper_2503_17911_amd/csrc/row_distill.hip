@@ -325,7 +325,7 @@ extern "C" ann_status ann_row_distillation_backward(const ann_row_scores *scores
     ANN_HIP(hipGetLastError());
     a.more_part = true;
     if (rows_side) {
-      const bool few = type == ANN_F32 || nq <= kFewQueries;
+      const bool few = type == ANN_F32 || nq <= kFewGradQueries;
       ann_status s = type == ANN_F32   ? distill_rows<float>(p, v, drows, few, ws, a, st)
                      : type == ANN_F16 ? distill_rows<f16_t>(p, v, drows, few, ws, a, st)
                                        : distill_rows<bf16_t>(p, v, drows, few, ws, a, st);

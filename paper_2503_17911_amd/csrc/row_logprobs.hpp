@@ -45,7 +45,7 @@ struct GradOut {
   uint64_t dq_stride, drows_stride;
 };
 
-constexpr uint32_t kFewQueries = 256;  // up to so many, the rows' gradient takes all of G's remainders
+constexpr uint32_t kFewGradQueries = 256;  // up to so many, the rows' gradient takes all of G's remainders
 
 uint64_t scores_backward_bytes(uint32_t nq, uint64_t n, uint32_t d, uint32_t type, bool more);
 float *scores_backward_more_part(uint32_t nq, uint64_t n, uint32_t d, uint32_t type, void *workspace);  // [nq][d]; there are queries and rows

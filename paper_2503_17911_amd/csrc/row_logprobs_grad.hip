@@ -19,7 +19,7 @@
 // What its rounding leaves goes to dq in fp32: that element outweighs all others
 // and rows of a cluster are alike, so that dq, their difference, erred by 0.6 % (bf16) with it, 0.17 % is the rounding of dq.
 // The rows' gradient has few terms that count, often the given row's one alone: G's rounding would add to the result's (0.24 % instead of
-// 0.17 % in bf16).  So what it leaves is taken along: where queries are few (kFewQueries) of every element, in 16 bits more, otherwise of the
+// 0.17 % in bf16).  So what it leaves is taken along: where queries are few (kFewGradQueries) of every element, in 16 bits more, otherwise of the
 // given rows' elements.  Where no given row's element outweighs the others (the entropy's gradient alone) G's rounding stays in the
 // results: up to 0.20 % in dq and 0.22 % in the rows' gradient in bf16, 2.4e-4 and 2.9e-4 in f16.
 #include "row_logprobs.hpp"
@@ -586,7 +586,7 @@ __global__ __launch_bounds__(256, 2) void grad_short_kernel(GradArgs a, uint32_t
           }
       };
       multiply(G);
-      if (OWN_ROWS && (hits || g.nq <= kFewQueries)) {  // what the rounding left, in 16 bits more
+      if (OWN_ROWS && (hits || g.nq <= kFewGradQueries)) {  // what the rounding left, in 16 bits more
 #pragma unroll
         for (int r = 0; r < 16; ++r) G[r / 8][r % 8] = from_f32<T>(s[r] - to_f32((T)G[r / 8][r % 8]));
         multiply(G);
@@ -669,7 +669,7 @@ static BackwardPlan backward_plan(uint32_t nq, uint64_t n, uint32_t d, uint32_t 
     if (p.splits > most) p.splits = most;
   }
   p.g_at = p.parts.take(p.chunk * row_bytes);
-  if (type != ANN_F32 && nq <= kFewQueries) p.rests_at = p.parts.take(p.chunk * row_bytes);
+  if (type != ANN_F32 && nq <= kFewGradQueries) p.rests_at = p.parts.take(p.chunk * row_bytes);
   p.part_at = p.parts.take((uint64_t)(p.splits + more) * nq * d * sizeof(float));
   // (one chunk whose tiles leave compute units with one workgroup or none: runs of queries, of 64 at least)
   const uint32_t row_tiles = p.chunk / kTile * c_tiles;
@@ -696,7 +696,7 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
   GradArgs a = args;
   const ScoreTable &g = a.g;
   const uint32_t c_tiles = (g.d + kTile - 1) / kTile;
-  T *G = (T *)(ws + p.g_at), *rests = sizeof(T) == 2 && g.nq && g.nq <= kFewQueries && o.drows ? (T *)(ws + p.rests_at) : nullptr;
+  T *G = (T *)(ws + p.g_at), *rests = sizeof(T) == 2 && g.nq && g.nq <= kFewGradQueries && o.drows ? (T *)(ws + p.rests_at) : nullptr;
   float *part = (float *)(ws + p.part_at), *sums = (float *)(ws + p.sums_at);
   a.rest = (float *)(ws + p.rest_at);
   if (std::is_same<T, f16_t>::value && g.nq && g.n && !a.scaling) {
