@@ -112,67 +112,96 @@ __global__ __launch_bounds__(256) void runs_kernel(Runs g, Work work, uint32_t s
   finish(id == next);
 }
 
-// Runs that cross borders between chunks, by the chunk in which they begin: 256 columns to a workgroup of eight wavefronts, which share out
-// the run's chunks (one id that a tenth of 200,000 entries have: 23 us by four).
-constexpr uint32_t kJoinWaves = 8;
+// Runs that cross borders between chunks, by the chunk in which they begin, 256 columns at a time: a wavefront to a border, which joins the runs of
+// few chunks alone; those of many are shared out over the workgroup's wavefronts afterwards, one after the other.  (A workgroup to a border:
+// 12 us for 2,500 borders of which one in two begins nothing or a run of two chunks; with four wavefronts 23 us where one id in ten is alike.)
+constexpr uint32_t kJoinWaves = 8, kJoinAlone = 8;
 template <typename Work>
 __global__ __launch_bounds__(kJoinWaves * 64) void runs_join_kernel(Runs g, Work work) {
   __shared__ float room[kJoinWaves - 1][256];
-  const uint32_t chunk = blockIdx.x, border = (chunk + 1) * g.chunk, begin = chunk * g.chunk;
-  // (read side by side: most workgroups end here)
-  const uint32_t before = begin ? g.keys[begin - 1] : 0xFFFFFFFFu, begins = g.keys[begin], ends = g.keys[border - 1], id = g.keys[border];
-  if (id >= g.ids || ends != id || (before == id && begins == id)) return;
+  __shared__ uint32_t starts[kJoinWaves], counts[kJoinWaves];
   const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = blockIdx.y * 256 + lane, columns = g.dim + (Work::kScalar ? 1 : 0);
-  uint32_t last = chunk + 1;  // the last chunk that begins with the run
-  for (;;) {
-    const uint32_t next = last + 1 + lane;
-    const uint64_t with = __ballot(next < g.chunks && g.keys[(uint64_t)next * g.chunk] == id);
-    if (with != ~0ull) {
-      last += __builtin_ctzll(~with);
-      break;
+  // sums of parts from .. to - 1 of the chunks behind `chunk`, and its own
+  const auto add_parts = [&](float (&sum)[4], uint32_t from, uint32_t to) {
+    for (uint32_t k = from; k < to; k += 8) {
+      float v[8][4];
+#pragma unroll
+      for (uint32_t u = 0; u < 8; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[u][e] = k + u < to && c + e * 64 < columns ? g.part[(uint64_t)(k + u) * 2 * g.part_ld + c + e * 64] : 0.0f;
+#pragma unroll
+      for (uint32_t u = 0; u < 8; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += v[u][e];
     }
-    last += 64;
-  }
-  uint32_t start = begin;  // the run's first entry
-  for (uint32_t i0 = begin;; i0 += 64) {
-    const uint64_t with = __ballot(i0 + lane < border && g.keys[i0 + lane] == id);
-    if (with) {
-      start = i0 + __builtin_ctzll(with);
-      break;
-    }
-  }
-  const uint32_t count = last - chunk, from = chunk + 1 + (uint32_t)((uint64_t)count * wave / kJoinWaves);
-  const uint32_t to = chunk + 1 + (uint32_t)((uint64_t)count * (wave + 1) / kJoinWaves);
-  float sum[4];
+  };
+  const auto begin_with = [&](float (&sum)[4], uint32_t chunk, bool own) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) sum[e] = wave == 0 && c + e * 64 < columns ? g.part[((uint64_t)chunk * 2 + 1) * g.part_ld + c + e * 64] : 0.0f;
-  for (uint32_t k = from; k < to; k += 8) {
-    float v[8][4];
-#pragma unroll
-    for (uint32_t u = 0; u < 8; ++u)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[u][e] = k + u < to && c + e * 64 < columns ? g.part[(uint64_t)(k + u) * 2 * g.part_ld + c + e * 64] : 0.0f;
-#pragma unroll
-    for (uint32_t u = 0; u < 8; ++u)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[e] += v[u][e];
-  }
-  if (wave != 0) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) room[wave - 1][lane + e * 64] = sum[e];
-  }
-  __syncthreads();
-  if (wave != 0) return;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (c + e * 64 >= columns) break;
-    float total[1] = {sum[e]};
-#pragma unroll
-    for (uint32_t w = 0; w < kJoinWaves - 1; ++w) total[0] += room[w][lane + e * 64];
+    for (int e = 0; e < 4; ++e) sum[e] = own && c + e * 64 < columns ? g.part[((uint64_t)chunk * 2 + 1) * g.part_ld + c + e * 64] : 0.0f;
+  };
+  const auto write = [&](uint32_t id, uint32_t start, int e, float v) {
+    const float total[1] = {v};
+    if (c + e * 64 >= columns) return;
     if (Work::kScalar && c + e * 64 == g.dim)
-      work.write_scalar(id, start, total[0]);
+      work.write_scalar(id, start, v);
     else
       work.template write<1, kByElement>(id, start, c + e * 64, total);
+  };
+  const uint32_t mine = blockIdx.x * kJoinWaves + wave;  // the border behind this chunk
+  uint32_t start = 0, count = 0;                         // of a run that begins in it and goes on: its first entry, and the chunks that it goes on in
+  if (mine + 1 < g.chunks) {
+    const uint32_t border = (mine + 1) * g.chunk, begin = mine * g.chunk;
+    const uint32_t before = begin ? g.keys[begin - 1] : 0xFFFFFFFFu, ends = g.keys[border - 1], id = g.keys[border];  // (read side by side)
+    if (id < g.ids && ends == id && before != id) {
+      count = 1;
+      for (;;) {
+        const uint64_t next = (uint64_t)mine + 1 + count + lane;
+        const uint64_t with = __ballot(next < g.chunks && g.keys[next * g.chunk] == id);
+        if (with != ~0ull) {
+          count += __builtin_ctzll(~with);
+          break;
+        }
+        count += 64;
+      }
+      for (uint32_t i0 = begin;; i0 += 64) {
+        const uint64_t with = __ballot(i0 + lane < border && g.keys[i0 + lane] == id);
+        if (with) {
+          start = i0 + __builtin_ctzll(with);
+          break;
+        }
+      }
+      if (count <= kJoinAlone) {
+        float sum[4];
+        begin_with(sum, mine, true);
+        add_parts(sum, mine + 1, mine + 1 + count);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) write(id, start, e, sum[e]);
+        count = 0;
+      }
+    }
+  }
+  if (lane == 0) starts[wave] = start, counts[wave] = count;
+  __syncthreads();
+  for (uint32_t w = 0; w < kJoinWaves; ++w) {
+    const uint32_t chunk = blockIdx.x * kJoinWaves + w, of = counts[w];
+    if (of == 0) continue;
+    float sum[4];
+    begin_with(sum, chunk, wave == 0);
+    add_parts(sum, chunk + 1 + (uint32_t)((uint64_t)of * wave / kJoinWaves), chunk + 1 + (uint32_t)((uint64_t)of * (wave + 1) / kJoinWaves));
+    if (wave != 0) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) room[wave - 1][lane + e * 64] = sum[e];
+    }
+    __syncthreads();
+    if (wave == 0) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+#pragma unroll
+        for (uint32_t o = 0; o < kJoinWaves - 1; ++o) sum[e] += room[o][lane + e * 64];
+        write(g.keys[(uint64_t)(chunk + 1) * g.chunk], starts[w], e, sum[e]);
+      }
+    }
+    __syncthreads();
   }
 }
 
@@ -198,7 +227,7 @@ static ann_status sum_runs(const Runs &g, const Work &work, uint32_t beside, hip
     sums_of(std::integral_constant<int, 64>());
   ANN_HIP(hipGetLastError());
   if (g.chunks > 1) {
-    runs_join_kernel<<<dim3(g.chunks - 1, (g.dim + (Work::kScalar ? 1 : 0) + 255) / 256), kJoinWaves * 64, 0, st>>>(g, work);
+    runs_join_kernel<<<dim3((g.chunks - 1 + kJoinWaves - 1) / kJoinWaves, (g.dim + (Work::kScalar ? 1 : 0) + 255) / 256), kJoinWaves * 64, 0, st>>>(g, work);
     ANN_HIP(hipGetLastError());
   }
   return ANN_OK;
