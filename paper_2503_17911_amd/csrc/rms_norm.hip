@@ -52,6 +52,28 @@ __device__ __forceinline__ void store_codes(const float (&v)[VEC], float inv, ui
   }
 }
 
+// The weights of VEC columns from c on; whatever, behind the last column.
+template <typename T, int VEC, RowEnd END>
+__device__ __forceinline__ void load_weights(float (&w)[VEC], const RmsArgs &g, uint32_t c) {
+  if (!g.weight) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) w[e] = 1.0f;
+  } else if (g.weight_f32) {
+#pragma unroll
+    for (int p = 0; p < VEC; p += 4) {
+      RowPiece<float, 4, END> piece;
+      piece.load((const float *)g.weight, c + p, g.dim);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[p + e] = piece.get(e);
+    }
+  } else {
+    RowPiece<T, VEC, END> piece;
+    piece.load((const T *)g.weight, c, g.dim);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) w[e] = piece.get(e);
+  }
+}
+
 // 1 / sqrt(mean + eps) of a row's squares, whose sum over the row `sum` forms of values times a factor: where it leaves fp32's range, of values
 // times 2^-80 once more (all lanes of a row take the same way).
 template <typename Sum>
@@ -80,12 +102,7 @@ __global__ __launch_bounds__(kRmsThreads<LANES>) void rms_kernel(RmsArgs g) {
   const uint32_t lane = threadIdx.x % LANES;
   float w[ITEMS][VEC];
 #pragma unroll
-  for (int it = 0; it < ITEMS; ++it)
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      const uint32_t c = (it * LANES + lane) * VEC + e;
-      w[it][e] = g.weight && c < g.dim ? load_param<T>(g.weight, g.weight_f32, c) : 1.0f;
-    }
+  for (int it = 0; it < ITEMS; ++it) load_weights<T, VEC, END>(w[it], g, (it * LANES + lane) * VEC);
   const float inv_dim = 1.0f / (float)g.dim;
   for (uint64_t row = (uint64_t)blockIdx.x * kGroups + threadIdx.x / LANES; row < g.n; row += (uint64_t)gridDim.x * kGroups) {
     const T *x = (const T *)g.x + row * g.x_stride;
@@ -245,13 +262,11 @@ __global__ __launch_bounds__(kRmsThreads<LANES>) void rms_grad_kernel(RmsArgs g)
   const uint32_t lane = threadIdx.x % LANES;
   float w[ITEMS][VEC], dw[ITEMS][VEC];
 #pragma unroll
-  for (int it = 0; it < ITEMS; ++it)
+  for (int it = 0; it < ITEMS; ++it) {
+    load_weights<T, VEC, END>(w[it], g, (it * LANES + lane) * VEC);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      const uint32_t c = (it * LANES + lane) * VEC + e;
-      w[it][e] = g.weight && c < g.dim ? load_param<T>(g.weight, g.weight_f32, c) : 1.0f;
-      dw[it][e] = 0.0f;
-    }
+    for (int e = 0; e < VEC; ++e) dw[it][e] = 0.0f;
+  }
   const float inv_dim = 1.0f / (float)g.dim;
   for (uint64_t row = (uint64_t)blockIdx.x * kGroups + threadIdx.x / LANES; row < g.n; row += (uint64_t)gridDim.x * kGroups) {
     const T *h = (const T *)g.x + row * g.x_stride, *dy = (const T *)g.dy + row * g.dy_stride;
