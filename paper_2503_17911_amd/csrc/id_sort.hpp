@@ -14,7 +14,7 @@
 
 namespace ann {
 
-constexpr uint32_t kSmallSort = 16384;  // up to so many ids are put in order by counting
+constexpr uint32_t kSmallSort = 12288;  // up to so many ids are put in order by counting (16,000: 33 us, 32 by two passes; 8,290: 16)
 
 // A plan for `n` ids of which those below `rows` count; the others come last, as the id `rows`.
 struct IdSortPlan {
@@ -232,17 +232,19 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortPass p, Be
 }
 
 // Up to kSmallSort entries: an entry's place is the number of entries before it in the order, counted against all of them (one workgroup's
-// radix sort of 5,000 took 16 us, the passes of many some 27).  A workgroup takes 32 entries, two to a lane, so that a key read from LDS serves both; 64 slices of
-// the keys to its lanes, whose counts are joined in LDS.
-constexpr uint32_t kSmallOwn = 32;
+// radix sort of 5,000 took 16 us, the passes of many some 27).  A workgroup takes 16 entries, the keys in LDS; 64 slices of the keys to its lanes, whose
+// counts are joined in LDS.  5,000: 8 us, bound by the comparisons (n^2 of two instructions) and the reads of LDS alike.  (Two entries to a lane halve the reads
+// and the workgroups: 9.2 us; keys through the scalar cache: 13.)
+constexpr uint32_t kSmallOwn = 16;
 template <typename Beside>
 __global__ __launch_bounds__(kSmallThreads) void sort_small_kernel(SortPass p, Beside beside) {
-  constexpr uint32_t kLanes = kSmallOwn / 2, kSlices = kSmallThreads / kLanes;
+  constexpr uint32_t kSlices = kSmallThreads / kSmallOwn;
   __shared__ __attribute__((aligned(16))) uint32_t keys[kSmallSort + 8 * kSlices];
   __shared__ uint32_t counts[kSmallOwn];
   if (blockIdx.x >= p.blocks) return beside(0, blockIdx.x - p.blocks, gridDim.x - p.blocks);
-  const uint32_t slice_keys = ((p.n + kSlices - 1) / kSlices + 3) / 8 * 8 + 4, padded = slice_keys * kSlices;  // (pieces of 16 bytes, an odd number: slices side by side lie in other banks)
-  for (uint32_t i0 = threadIdx.x; i0 < padded; i0 += 8 * kSmallThreads) {  // (eight on their way: one after the other they took longer than all else)
+  // (pieces of 16 bytes, an odd number: slices side by side lie in other banks)
+  const uint32_t slice_keys = ((p.n + kSlices - 1) / kSlices + 3) / 8 * 8 + 4, padded = slice_keys * kSlices;
+  for (uint32_t i0 = threadIdx.x; i0 < padded; i0 += 8 * kSmallThreads) {  // (eight on their way)
     uint32_t k[8];
 #pragma unroll
     for (uint32_t u = 0; u < 8; ++u) k[u] = i0 + u * kSmallThreads < p.n ? sort_key(p, i0 + u * kSmallThreads) : 0xFFFFFFFFu;
@@ -252,40 +254,26 @@ __global__ __launch_bounds__(kSmallThreads) void sort_small_kernel(SortPass p, B
   }
   if (threadIdx.x < kSmallOwn) counts[threadIdx.x] = 0;
   __syncthreads();
-  const uint32_t begin = threadIdx.x / kLanes * slice_keys, end = begin + slice_keys;
-  uint32_t own[2], key[2], before[2] = {0, 0};
-  bool mixed = false;  // a slice with entries before and behind one of the lane's
-#pragma unroll
-  for (int o = 0; o < 2; ++o) {
-    own[o] = blockIdx.x * kSmallOwn + threadIdx.x % kLanes + o * kLanes;
-    key[o] = own[o] < p.n ? keys[own[o]] : 0;
-    mixed |= own[o] >= begin && own[o] < end;
-  }
-  if (!mixed) {
-    const uint32_t below[2] = {key[0] + (own[0] >= end), key[1] + (own[1] >= end)};  // (equal ids before it stay before it; ids are at most 2^31)
+  const uint32_t own = blockIdx.x * kSmallOwn + threadIdx.x % kSmallOwn, begin = threadIdx.x / kSmallOwn * slice_keys, end = begin + slice_keys;
+  const uint32_t key = own < p.n ? keys[own] : 0;
+  uint32_t before = 0;
+  if (own < begin || own >= end) {
+    const uint32_t below = key + (own >= end);  // (equal ids before it stay before it; ids are at most 2^31)
 #pragma unroll 4
     for (uint32_t j = begin; j < end; j += 4) {
       const uint4 k = *(const uint4 *)(keys + j);
-#pragma unroll
-      for (int o = 0; o < 2; ++o) before[o] += (k.x < below[o]) + (k.y < below[o]) + (k.z < below[o]) + (k.w < below[o]);
+      before += (k.x < below) + (k.y < below) + (k.z < below) + (k.w < below);
     }
   } else {
 #pragma unroll 4
     for (uint32_t j = begin; j < end; j += 4) {
       const uint4 k = *(const uint4 *)(keys + j);
-#pragma unroll
-      for (int o = 0; o < 2; ++o)
-        before[o] += (k.x < key[o] + (j < own[o])) + (k.y < key[o] + (j + 1 < own[o])) + (k.z < key[o] + (j + 2 < own[o])) + (k.w < key[o] + (j + 3 < own[o]));
+      before += (k.x < key + (j < own)) + (k.y < key + (j + 1 < own)) + (k.z < key + (j + 2 < own)) + (k.w < key + (j + 3 < own));
     }
   }
-#pragma unroll
-  for (int o = 0; o < 2; ++o) atomicAdd(&counts[threadIdx.x % kLanes + o * kLanes], before[o]);
+  atomicAdd(&counts[threadIdx.x % kSmallOwn], before);
   __syncthreads();
-  const uint32_t i = blockIdx.x * kSmallOwn + threadIdx.x;
-  if (threadIdx.x < kSmallOwn && i < p.n) {
-    const uint32_t to = counts[threadIdx.x];
-    p.out_keys[to] = keys[i], p.out_at[to] = i;
-  }
+  if (threadIdx.x < kSmallOwn && own < p.n) p.out_keys[counts[threadIdx.x]] = key, p.out_at[counts[threadIdx.x]] = own;
 }
 
 template <typename Beside>
