@@ -352,14 +352,22 @@ __global__ __launch_bounds__(256) void grad_rows_sum_kernel(GradArgs a, uint32_t
   const uint64_t all = (uint64_t)rows * g.d, at = (uint64_t)blockIdx.x * 256 + threadIdx.x;
   if (at >= all) return;
   const float by = a.scaling ? g.scale * a.scaling[1] : g.scale;
-  const uint64_t row = row0 + at / g.d;
-  const float more = a.slots ? more_of_row(a, (uint32_t)row, (uint32_t)(at % g.d)) : 0.0f;
+  const uint32_t j = all >> 32 ? (uint32_t)(at / g.d) : (uint32_t)at / g.d, c = (uint32_t)(at - (uint64_t)j * g.d);  // (divisions of 64 bits took longer than the reads)
+  const uint64_t row = row0 + j;
+  const float more = a.slots ? more_of_row(a, (uint32_t)row, c) : 0.0f;
   float sum = 0.0f;
-  for (uint32_t s = 0; s < splits; ++s) sum += part[s * all + at];
+  for (uint32_t s0 = 0; s0 < splits; s0 += 4) {  // (four on their way)
+    float v[4];
+#pragma unroll
+    for (uint32_t u = 0; u < 4; ++u) v[u] = s0 + u < splits ? part[(s0 + u) * all + at] : 0.0f;
+#pragma unroll
+    for (uint32_t u = 0; u < 4; ++u)
+      if (s0 + u < splits) sum += v[u];
+  }
   const bool left_out = g.bias && g.bias[row] == -INFINITY;
   float v = sum * by;
   if (a.slots) v = __builtin_fmaf(g.scale, more, v);
-  out[row * stride + at % g.d] = from_f32<T>(left_out ? 0.0f : v);
+  out[row * stride + c] = from_f32<T>(left_out ? 0.0f : v);
 }
 
 // Adds v with what the last addition lost: over many queries like terms lose with one sign (1.7e-4 of the sum of a million).
@@ -391,6 +399,7 @@ __global__ __launch_bounds__(256) void grad_bias_kernel(GradArgs a, const float 
 // 4,096 x 100,000 x 128 bf16: 290 us for the queries' side, 329 for the rows' (730 and 640 TFLOP/s; 1,097 us with G stored).  Queries' side: vector
 // instructions issue in 50 % of the cycles, LDS works in 39 (44 % of that conflicts), the matrix cores in 34: none of them bounds it alone,
 // two wavefronts to a SIMD wait.  Rows' side: 26, 41 and 29, and 782 workgroups on 512 places.
+// splits: of the passing side; with one, OWN_ROWS writes drows and drow_bias, otherwise part[split][line] (and drow_bias[split][row]: sums over its queries).
 constexpr int kPassing = 64, kOwned = 128;
 constexpr uint32_t kShortTarget = 512;       // workgroups that own queries: two to a compute unit
 constexpr uint64_t kShortStride = 1u << 24;  // row stride up to which offsets within a tile take 32 bits
@@ -413,7 +422,8 @@ __global__ __launch_bounds__(256, 2) void grad_short_kernel(GradArgs a, uint32_t
   const T *own = (const T *)(OWN_ROWS ? g.rows : g.q), *pass = (const T *)(OWN_ROWS ? g.q : g.rows);
   const uint32_t own_tiles = (owned + kOwned - 1) / kOwned;
   // a die takes a run of rows through all queries
-  const uint32_t b8 = blockIdx.x / 8, ot = OWN_ROWS ? blockIdx.x : b8 % own_tiles, split = OWN_ROWS ? 0 : b8 / own_tiles * 8 + blockIdx.x % 8;
+  const uint32_t b8 = blockIdx.x / 8, split = OWN_ROWS ? blockIdx.x / own_tiles : b8 / own_tiles * 8 + blockIdx.x % 8;
+  const uint32_t ot = OWN_ROWS ? blockIdx.x - split * own_tiles : b8 % own_tiles;
   if (split >= splits) return;
   const uint32_t tiles = (passing + kPassing - 1) / kPassing;
   const uint32_t first = (uint32_t)((uint64_t)tiles * split / splits), last = (uint32_t)((uint64_t)tiles * (split + 1) / splits);
@@ -598,12 +608,12 @@ __global__ __launch_bounds__(256, 2) void grad_short_kernel(GradArgs a, uint32_t
     sum = __uint_as_float(p.low) + __uint_as_float(p.high);
     if (lane < 32 && mine < g.n) {
       sum /= scaling;
-      if (a.slots) sum += more_of_row(a, mine, g.d);
-      drow_bias[mine] = sum;
+      if (a.slots && splits == 1) sum += more_of_row(a, mine, g.d);
+      drow_bias[(uint64_t)split * g.n + mine] = sum;
     }
   }
   if (OWN_ROWS && !drows) return;
-  if (OWN_ROWS && a.slots) add_more<KS / 2>(a, own0, g.n, 0, scaling, acc);
+  if (OWN_ROWS && a.slots && splits == 1) add_more<KS / 2>(a, own0, g.n, 0, scaling, acc);
   const float by = a.scaling ? g.scale * a.scaling[1] : g.scale;
 #pragma unroll
   for (int b = 0; b < KS / 2; ++b) {
@@ -612,11 +622,11 @@ __global__ __launch_bounds__(256, 2) void grad_short_kernel(GradArgs a, uint32_t
     for (int r = 0; r < 16; ++r) {
       const uint32_t l = own0 + block_row(r);
       if (l >= owned || column >= g.d) continue;
-      if constexpr (OWN_ROWS) {
+      if (OWN_ROWS && splits == 1) {
         const bool left_out = BIAS && g.bias[l] == -INFINITY;  // (zero, whatever the queries hold)
         drows[l * stride + column] = from_f32<T>(left_out ? 0.0f : acc[b][r] * by);
       } else {
-        part[((uint64_t)split * g.nq + l) * g.d + column] = acc[b][r];
+        part[((uint64_t)split * owned + l) * g.d + column] = acc[b][r];
       }
     }
   }
@@ -639,6 +649,18 @@ static BackwardPlan backward_plan(uint32_t nq, uint64_t n, uint32_t d, uint32_t 
   p.q_tiles = (nq + kTile - 1) / kTile;
   if (type != ANN_F32 && d <= 128) {
     p.slices = d <= 64 ? 4 : d <= 96 ? 6 : 8;
+    if (more) {
+      // Rows' side: few rows leave most places empty, so the queries are split where that is less, with the parts' way through memory (at 4 TB/s) and a launch: a
+      // workgroup takes 0.29 us to a passing tile and slice (4,173 rows, 434 queries: 33 us by 33 workgroups).  Not for the log probabilities' own gradients,
+      // whose sums keep their order.
+      const uint64_t own_tiles = (n + kOwned - 1) / kOwned, q_tiles = (nq + kPassing - 1) / kPassing;
+      double least = INFINITY;
+      for (uint32_t s = 1; s <= 16 && s <= q_tiles; ++s) {
+        const double cost = 0.29 * p.slices * ((own_tiles * s + kShortTarget - 1) / kShortTarget) * ((q_tiles + s - 1) / s) + (s > 1 ? 5.0 + 2e-6 * s * n * d : 0.0);
+        if (cost < least) least = cost, p.row_splits = s;
+      }
+      if (p.row_splits > 1) p.row_part_at = p.parts.take((uint64_t)p.row_splits * n * d * sizeof(float)), p.sums_at = p.parts.take((uint64_t)p.row_splits * n * sizeof(float));
+    }
     const uint32_t tiles = (uint32_t)((n + kPassing - 1) / kPassing), want = ((kShortTarget + p.q_tiles - 1) / p.q_tiles + 7) / 8 * 8;
     p.splits = want < tiles ? want : tiles;
     p.part_at = p.parts.take((uint64_t)(p.splits + more) * nq * d * sizeof(float));
@@ -711,8 +733,10 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
         constexpr bool BIAS = decltype(bias)::value, ENTROPY = decltype(entropy)::value;
         if (o.dq)
           grad_short_kernel<T, KS, false, BIAS, ENTROPY><<<p.q_tiles * ((p.splits + 7) / 8 * 8), 256, 0, st>>>(a, p.splits, part, nullptr, 0, nullptr);
+        const uint32_t row_blocks = (g.n + kOwned - 1) / kOwned * p.row_splits;
         if (o.drows || o.drow_bias)
-          grad_short_kernel<T, KS, true, BIAS, ENTROPY><<<(g.n + kOwned - 1) / kOwned, 256, 0, st>>>(a, 1, nullptr, (T *)o.drows, o.drows_stride, o.drow_bias);
+          grad_short_kernel<T, KS, true, BIAS, ENTROPY><<<row_blocks, 256, 0, st>>>(a, p.row_splits, (float *)(ws + p.row_part_at), (T *)o.drows, o.drows_stride,
+                                                                                    p.row_splits > 1 && o.drow_bias ? sums : o.drow_bias);
       }
     };
     const auto run_entropy = [&](auto slices, auto bias) {
@@ -734,6 +758,14 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
     else
       run_bias(std::integral_constant<int, 8>());
     ANN_HIP(hipGetLastError());
+    if (p.row_splits > 1 && o.drows) {
+      grad_rows_sum_kernel<T><<<(uint32_t)(((uint64_t)g.n * g.d + 255) / 256), 256, 0, st>>>(a, 0, g.n, (const float *)(ws + p.row_part_at), p.row_splits, (T *)o.drows, o.drows_stride);
+      ANN_HIP(hipGetLastError());
+    }
+    if (p.row_splits > 1 && o.drow_bias) {
+      grad_bias_kernel<<<(g.n + 255) / 256, 256, 0, st>>>(a, sums, p.row_splits, g.n, 0, g.n, o.drow_bias);
+      ANN_HIP(hipGetLastError());
+    }
     if (o.dq) {
       // (256 splits of 256 queries: 15.5 us by two wavefronts to a query)
       const uint32_t splits = p.splits + (a.more_part ? 1 : 0);

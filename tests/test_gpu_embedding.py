@@ -63,7 +63,7 @@ def test_forward(n, rows, d, dtype, ttype):
 
 
 SIZES = [(12_288, 3000, 40), (12_289, 3000, 40), (8192, 3000, 40), (8193, 3000, 40), (16_384, 3000, 8), (16_385, 3000, 8), (16_383, 40_000, 24), (40_001, 2047, 12), (40_001, 2048, 12), (1, 1, 8), (1, 200, 768), (2, 2, 1), (31, 5, 3), (32, 9, 100), (33, 1000, 129), (64, 64, 16), (65, 3, 260), (1000, 77, 100), (4096, 3000, 40),
-         (4097, 3000, 40), (4097, 1, 8), (20_000, 70_000, 24), (9000, 100, 1030), (20_000, 900, 768), (150_000, 3000, 8), (300_000, 3, 20), (280_000, 1 << 22, 3)]
+         (4097, 3000, 40), (4097, 1, 8), (20_000, 70_000, 24), (9000, 100, 1030), (20_000, 900, 768), (150_000, 3000, 8), (300_000, 3, 20), (280_000, 1 << 22, 3), (300_000, 3_000_000, 2)]
 
 
 @pytest.mark.parametrize("law", ["zipf", "one", "each", "pads", "even"])
