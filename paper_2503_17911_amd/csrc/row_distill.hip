@@ -23,11 +23,11 @@ namespace ann {
 // Of an entry: its log probability under the student (0: no row is given, -infinity: the row is left out), and of a query: its loss.  16 lanes to an entry.
 template <typename T>
 __global__ __launch_bounds__(256) void distill_loss_kernel(ScoreTable g, uint32_t k, const uint32_t *__restrict__ ids, const float *__restrict__ given,
-                                                           const float *__restrict__ lse, float *__restrict__ loss, float *__restrict__ logprobs) {
+                                                           const double *__restrict__ lse, float *__restrict__ loss, float *__restrict__ logprobs) {
   constexpr int VEC = 16 / (int)sizeof(T);
   __shared__ double terms[ANN_MAX_ALTERNATIVES];
   const uint32_t q = blockIdx.x, lane = threadIdx.x % 16;
-  const float l = lse[q];
+  const double l = lse[q];  // (rounded to fp32 it would move every log probability by up to half a step of lse)
   for (uint32_t e = threadIdx.x / 16; e < k; e += 16) {
     const uint32_t id = ids[(uint64_t)q * k + e];
     const float bias = id < g.n && g.bias ? g.bias[id] : 0.0f;
@@ -43,11 +43,11 @@ __global__ __launch_bounds__(256) void distill_loss_kernel(ScoreTable g, uint32_
     }
     sum = group_sum_f64<16>(sum);
     if (lane != 0) continue;
-    float logp = 0.0f;
-    if (id < g.n) logp = bias == -INFINITY ? -INFINITY : (float)(sum * (double)g.scale + (double)bias - (double)l);
-    logprobs[(uint64_t)q * k + e] = logp;
+    double logp = 0.0;
+    if (id < g.n) logp = bias == -INFINITY ? -INFINITY : sum * (double)g.scale + (double)bias - l;
+    logprobs[(uint64_t)q * k + e] = (float)logp;
     const double t = id < g.n ? (double)given[(uint64_t)q * k + e] : -INFINITY;
-    terms[e] = t == -INFINITY ? 0.0 : exp(t) * (t - (double)logp);
+    terms[e] = t == -INFINITY ? 0.0 : exp(t) * (t - logp);
   }
   __syncthreads();
   if (threadIdx.x != 0) return;
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(256) void distill_whole_kernel(GivenArgs a) {
 }
 
 // An entry's weight and what the rounding of the first part's element left, which is taken once for a row that is given twice; and their sum over the
-// query's entries of more * row: a workgroup to a query, kGivenLanes pieces of columns at a time, kGivenRuns runs of entries side by side.  T: the type
+// query's entries of more * row: a workgroup to a query (and to each gridDim.y-th part of its columns), kGivenLanes pieces of columns at a time, kGivenRuns runs of entries side by side.  T: the type
 // that G is rounded to.  part NULL: the entries alone.  Workgroups behind the queries' only fill the slots.
 constexpr uint32_t kGivenRuns = 8, kGivenLanes = 32;
 template <typename T, RowEnd END>
@@ -103,7 +103,7 @@ __global__ __launch_bounds__(kGivenRuns * kGivenLanes) void distill_more_kernel(
   constexpr int VEC = 16 / (int)sizeof(T), kEach = ANN_MAX_ALTERNATIVES / kGivenRuns;
   __shared__ float more_of[ANN_MAX_ALTERNATIVES], room[kGivenRuns][kGivenLanes * VEC + 4];
   __shared__ uint32_t id_of[ANN_MAX_ALTERNATIVES];
-  if (a.slots)
+  if (a.slots && blockIdx.y == 0)
     for (uint64_t j = (uint64_t)blockIdx.x * 256 + threadIdx.x; j < a.g.n; j += (uint64_t)gridDim.x * 256) a.slots[j] = ANN_PAD_ID;
   const uint32_t q = blockIdx.x, lane = threadIdx.x % kGivenLanes, run = threadIdx.x / kGivenLanes;
   if (q >= a.g.nq) return;
@@ -121,15 +121,15 @@ __global__ __launch_bounds__(kGivenRuns * kGivenLanes) void distill_more_kernel(
         const float v = -(expf(a.logprobs[at]) * (entry.whole * by));
         more = __builtin_fmaf(v - to_f32(from_f32<T>(v)), back, more);
       }
-      a.rows[at] = entry.id, a.weights[at] = entry.weight, a.more[at] = more;
+      if (blockIdx.y == 0) a.rows[at] = entry.id, a.weights[at] = entry.weight, a.more[at] = more;
     }
-    if (e == 0) a.whole[q] = entry.whole;
+    if (e == 0 && blockIdx.y == 0) a.whole[q] = entry.whole;
     more_of[e] = more * by, id_of[e] = entry.id;
   }
   if (!part) return;
   __syncthreads();
   const uint32_t begin = a.k * run / kGivenRuns, end = a.k * (run + 1) / kGivenRuns;
-  for (uint32_t c0 = 0; c0 < a.g.d; c0 += kGivenLanes * VEC) {
+  for (uint32_t c0 = blockIdx.y * (kGivenLanes * VEC); c0 < a.g.d; c0 += gridDim.y * (kGivenLanes * VEC)) {
     const uint32_t c = c0 + lane * VEC;
     RowPiece<T, VEC, END> x[kEach];
 #pragma unroll
@@ -249,7 +249,7 @@ static uint64_t forward_bytes(uint32_t nq, uint64_t n, uint32_t d, uint32_t type
 
 extern "C" uint64_t ann_row_distillation_workspace(uint32_t nq, uint64_t n, uint32_t d, uint32_t type, uint32_t k) {
   if (n > kMaxRows || nq >= kMaxQueries || d == 0 || type > ANN_BF16 || k > ANN_MAX_ALTERNATIVES || nq == 0) return 0;
-  return forward_bytes(nq, n, d, type) + nq * 4ull;
+  return forward_bytes(nq, n, d, type) + nq * 12ull;
 }
 
 extern "C" ann_status ann_row_distillation(const ann_row_scores *scores, uint32_t k, const uint32_t *given_ids, const float *given_logprobs, float *loss,
@@ -258,17 +258,18 @@ extern "C" ann_status ann_row_distillation(const ann_row_scores *scores, uint32_
   const uint32_t nq = scores->nq;
   if (nq == 0) return ANN_OK;
   if (!loss || !lse || !logprobs) return fail(ANN_EINVAL, "ann_row_distillation: loss, lse or logprobs is NULL");
-  const uint64_t need = ann_row_distillation_workspace(nq, scores->n, scores->d, scores->type, k), before = need - nq * 4ull;
+  const uint64_t need = ann_row_distillation_workspace(nq, scores->n, scores->d, scores->type, k), before = need - nq * 12ull;
   if (ann_status s = check_workspace("ann_row_distillation", workspace, workspace_bytes, need)) return s;
-  if (ann_status s = ann_row_logprobs(scores, 0, (float *)((char *)workspace + before), nullptr, lse, nullptr, nullptr, workspace, before, stream)) return s;
+  double *wide_lse = (double *)((char *)workspace + before);
+  if (ann_status s = row_statistics(*scores, (float *)(wide_lse + nq), lse, wide_lse, workspace, (hipStream_t)stream)) return s;
   const ScoreTable g = score_table(*scores);
   const hipStream_t st = (hipStream_t)stream;
   if (scores->type == ANN_F32)
-    distill_loss_kernel<float><<<nq, 256, 0, st>>>(g, k, given_ids, given_logprobs, lse, loss, logprobs);
+    distill_loss_kernel<float><<<nq, 256, 0, st>>>(g, k, given_ids, given_logprobs, wide_lse, loss, logprobs);
   else if (scores->type == ANN_F16)
-    distill_loss_kernel<f16_t><<<nq, 256, 0, st>>>(g, k, given_ids, given_logprobs, lse, loss, logprobs);
+    distill_loss_kernel<f16_t><<<nq, 256, 0, st>>>(g, k, given_ids, given_logprobs, wide_lse, loss, logprobs);
   else
-    distill_loss_kernel<bf16_t><<<nq, 256, 0, st>>>(g, k, given_ids, given_logprobs, lse, loss, logprobs);
+    distill_loss_kernel<bf16_t><<<nq, 256, 0, st>>>(g, k, given_ids, given_logprobs, wide_lse, loss, logprobs);
   ANN_HIP(hipGetLastError());
   return ANN_OK;
 }
@@ -313,10 +314,13 @@ extern "C" ann_status ann_row_distillation_backward(const ann_row_scores *scores
     }
     const auto add_up = [&](auto t) {
       typedef decltype(t) T;
+      // (few queries: a workgroup to a part of the columns)
+      constexpr uint32_t kColumns = kGivenLanes * (16 / sizeof(T));
+      const dim3 grid(blocks, part && nq < 256 ? (scores->d + kColumns - 1) / kColumns : 1);
       if (scores->d % (16 / sizeof(T)) == 0)
-        distill_more_kernel<T, kWholePieces><<<blocks, kGivenRuns * kGivenLanes, 0, st>>>(v, scaling, part);
+        distill_more_kernel<T, kWholePieces><<<grid, kGivenRuns * kGivenLanes, 0, st>>>(v, scaling, part);
       else
-        distill_more_kernel<T, kShifted><<<blocks, kGivenRuns * kGivenLanes, 0, st>>>(v, scaling, part);
+        distill_more_kernel<T, kShifted><<<grid, kGivenRuns * kGivenLanes, 0, st>>>(v, scaling, part);
     };
     if (type == ANN_F32)
       add_up(0.0f);

@@ -185,7 +185,8 @@ __device__ __forceinline__ Stats join_halves(const Stats &s) {
 // BIAS: rows may be left out, or the scale is negative.  MB: blocks of 32 rows to a wavefront; four: the wide product, for 16-bit
 // rows of whole slices where tiles of 256 rows still fill the card (4,000 x 100,003 x 768 fp16, the call: 1,074 us against 1,118 by tiles of 128 with
 // k = 20, 840 against 922 without alternatives, though 29 registers a lane are kept in scratch memory).
-template <typename T, bool BIAS, int GROUP, int MB>
+// APART (fp32): the smaller products of parts are summed apart.
+template <typename T, bool BIAS, int GROUP, int MB, bool APART = false>
 __global__ __launch_bounds__(256, MB == 4 ? 2 : 1) void row_scores_kernel(ScoreTable g, uint32_t q_tiles, uint32_t q_group, uint32_t splits, float4 *__restrict__ stats,
                                                          float *__restrict__ group_max, float *__restrict__ group_second) {
   constexpr int kMore = MB == 4 ? kWideBuffer : 16;
@@ -216,7 +217,7 @@ __global__ __launch_bounds__(256, MB == 4 ? 2 : 1) void row_scores_kernel(ScoreT
     else
       // (fp32: the smaller products apart take so many registers that one workgroup fits where two did: 155 -> 213 us for 513 x 50,000 x 100;
       // with one sum the log probabilities err by 6e-8 there, by 2.8e-7 with 768 columns, about as far as a plain fp32 product's)
-      tile_product<T, kAlong, kAlong>(acc, X, row0, Q, qt * kTile, 0, g.d, lds);
+      tile_product<T, kAlong, kAlong, APART>(acc, X, row0, Q, qt * kTile, 0, g.d, lds);
     if (BIAS || !whole) {
       // (read by the tile before's epilogue: the barriers of the product lie in between; d > 0)
       if (threadIdx.x < kRowTile) row_bias[threadIdx.x] = row0 + threadIdx.x < g.n ? (BIAS && g.bias ? g.bias[row0 + threadIdx.x] : 0.0f) : -INFINITY;
@@ -709,6 +710,7 @@ struct FinishArgs {
   double unit, scale_error;  // natural units to one of the statistics'; how much scale log2 e lacks where the kernels take it rounded, relative
   float *logprob, *entropy, *lse, *alt_logprobs;
   uint32_t *alt_ids;
+  double *wide_lse;  // before it is rounded (NULL where not wanted)
 };
 
 // A row's product with the query (in LDS, zero from d on) in fp64, by LANES lanes.
@@ -850,6 +852,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 5 : 4) void row_finish_ke
       lp = none || bias == -INFINITY ? -INFINITY : (double)g.scale * target_dot + (double)bias - lse;
     }
     a.lse[i] = (float)lse;
+    if (a.wide_lse) a.wide_lse[i] = lse;
     a.logprob[i] = lp > 0.0 ? 0.0f : (float)lp;
     const double h = none ? 0.0 : log_l - t / l;
     if (a.entropy) a.entropy[i] = h < 0.0 ? 0.0f : (float)h;
@@ -1090,7 +1093,7 @@ static uint32_t query_group(uint32_t q_tiles, uint32_t d, uint32_t elem) {
 static uint32_t query_grid(uint32_t q_tiles, uint32_t group, uint32_t splits) { return ((q_tiles + group - 1) / group * splits + 7) / 8 * 8 * group; }
 
 template <typename T>
-static ann_status forward(const ann_row_scores &s, uint32_t k, const ForwardPlan &p, FinishArgs f, char *ws, hipStream_t st) {
+static ann_status forward(const ann_row_scores &s, uint32_t k, const ForwardPlan &p, FinishArgs f, char *ws, hipStream_t st, bool apart = false) {
   const ScoreTable &g = f.g;
   if (s.n) {
     float4 *stats = (float4 *)(ws + p.stats_at);
@@ -1110,6 +1113,8 @@ static ann_status forward(const ann_row_scores &s, uint32_t k, const ForwardPlan
         const uint32_t q_group = query_group(q_tiles, g.d, sizeof(T)), paired = query_grid(q_tiles, q_group, p.splits);
         if (p.wide && wide_operand(g.q, g.q_stride) && wide_operand(g.rows, g.row_stride)) {
           if constexpr (sizeof(T) == 2) row_scores_kernel<T, BIAS, GROUP, 4><<<paired, 256, 0, st>>>(g, q_tiles, q_group, p.splits, stats, groups, seconds);
+        } else if (!is_short && apart) {
+          if constexpr (sizeof(T) == 4 && GROUP == 0) row_scores_kernel<T, BIAS, GROUP, 2, true><<<paired, 256, 0, st>>>(g, q_tiles, q_group, p.splits, stats, groups, seconds);
         } else if (!is_short)
           row_scores_kernel<T, BIAS, GROUP, 2><<<paired, 256, 0, st>>>(g, q_tiles, q_group, p.splits, stats, groups, seconds);
         else if (p.slices == 2)
@@ -1172,6 +1177,15 @@ static ann_status forward(const ann_row_scores &s, uint32_t k, const ForwardPlan
     end(std::integral_constant<int, 64>());
   ANN_HIP(hipGetLastError());
   return ANN_OK;
+}
+
+ann_status row_statistics(const ann_row_scores &s, float *logprob, float *lse, double *wide_lse, void *workspace, hipStream_t st) {
+  const ForwardPlan p = forward_plan(s.nq, s.n, s.d, s.type, 0);
+  FinishArgs f = {};
+  f.g = score_table(s), f.logprob = logprob, f.lse = lse, f.wide_lse = wide_lse;
+  if (s.type == ANN_F32) return forward<float>(s, 0, p, f, (char *)workspace, st, true);
+  if (s.type == ANN_F16) return forward<f16_t>(s, 0, p, f, (char *)workspace, st);
+  return forward<bf16_t>(s, 0, p, f, (char *)workspace, st);
 }
 
 ann_status check_scores(const char *what, const ann_row_scores *s) {

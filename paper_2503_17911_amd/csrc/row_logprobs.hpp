@@ -54,6 +54,11 @@ ann_status launch_grad_scaling(const GradArgs &a, float *scaling, hipStream_t st
 // a.scaling of f16: NULL to have it found (in the workspace).
 ann_status scores_backward(uint32_t type, const GradArgs &a, const GradOut &o, void *workspace, hipStream_t st);
 
+// lse (and logprob: 0) as ann_row_logprobs without targets and alternatives, in a workspace of its size; wide_lse: lse before it is rounded.  fp32 scores
+// are as exact as their gradients': what is taken off lse, a given row's score, is exact, and where that row has nearly all probability their difference is
+// what the scores err by.
+ann_status row_statistics(const ann_row_scores &s, float *logprob, float *lse, double *wide_lse, void *workspace, hipStream_t st);
+
 ann_status check_scores(const char *what, const ann_row_scores *s);
 ann_status check_workspace(const char *what, const void *workspace, uint64_t bytes, uint64_t need);
 

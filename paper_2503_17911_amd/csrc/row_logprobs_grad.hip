@@ -212,7 +212,7 @@ __global__ __launch_bounds__(256, MB == 4 ? 2 : kGradWaves<T>) void grad_queries
 }
 
 // dq[q][c] = scale sum over the splits, and what was left of the given row's element.  A workgroup of THREADS lanes takes one
-// query after LANES * RUNS of them: LANES to its columns, RUNS to runs of its splits, which are added in the runs' order.
+// query after LANES * RUNS of them: LANES to its columns (and those gridDim.y further), RUNS to runs of its splits, which are added in the runs' order.
 // Eight splits' parts are on their way at a time.
 template <typename T, int LANES, int RUNS, int THREADS>
 __global__ __launch_bounds__(THREADS) void grad_queries_sum_kernel(GradArgs a, const float *__restrict__ part, uint32_t splits, T *__restrict__ dq, uint64_t stride) {
@@ -227,7 +227,7 @@ __global__ __launch_bounds__(THREADS) void grad_queries_sum_kernel(GradArgs a, c
   const bool given = target < g.n && !(g.bias && g.bias[target] == -INFINITY);
   const float rest = given ? a.rest[q] : 0.0f;
   const uint32_t run = threadIdx.x / LANES % RUNS, end = (uint32_t)((uint64_t)splits * (run + 1) / RUNS);
-  for (uint32_t c0 = 0; c0 < g.d; c0 += LANES) {
+  for (uint32_t c0 = blockIdx.y * LANES; c0 < g.d; c0 += gridDim.y * LANES) {
     const uint32_t c = c0 + threadIdx.x % LANES;
     float sum = 0.0f;
     if (c < g.d) {
@@ -846,7 +846,9 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
     }
   }
   if (o.dq && g.nq) {
-    grad_queries_sum_kernel<T, 256, 1, 256><<<g.nq, 256, 0, st>>>(a, part, g.n ? p.splits + (a.more_part ? 1 : 0) : 0, (T *)o.dq, o.dq_stride);
+    // (few queries: a workgroup to 256 columns of one; 20 of 960 columns took 23 us by one workgroup to each)
+    grad_queries_sum_kernel<T, 256, 1, 256><<<dim3(g.nq, g.nq < 256 ? (g.d + 255) / 256 : 1), 256, 0, st>>>(a, part, g.n ? p.splits + (a.more_part ? 1 : 0) : 0, (T *)o.dq,
+                                                                                                           o.dq_stride);
     ANN_HIP(hipGetLastError());
   }
   return ANN_OK;

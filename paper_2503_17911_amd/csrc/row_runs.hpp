@@ -11,7 +11,7 @@
 namespace ann {
 
 // Entries that are summed one after the other: few where there are few in all, so that the card has work (5,003 x 100: 28 us by 32 of them).
-inline uint32_t chunk_entries(uint64_t n) { return n <= 8192 ? 8 : n <= 16384 ? 16 : 32; }
+inline uint32_t chunk_entries(uint64_t n) { return n <= 16384 ? 8 : 32; }
 constexpr uint32_t kMostChunks = 1 << 15;  // beyond, chunks are longer
 constexpr uint32_t kFetched = 8;           // rows on their way at a time
 
