@@ -324,6 +324,17 @@ __global__ __launch_bounds__(256, RESTS ? 2 : kGradWaves<T>) void grad_rows_kern
     for (int i = 0; i < 2; ++i) add_more<2>(a, row0 + rt * kTile + wave / 2 * 64 + i * 32, g.n, ct * kTile + wave % 2 * 64, a.scaling ? a.scaling[0] : 1.0f, acc[i]);
   }
   const float by = a.scaling ? g.scale * a.scaling[1] : g.scale;
+  // the rows left out, a bit to each (read before anything is written: beside the writes the reads came one after the other)
+  uint32_t out_of[2] = {0, 0};
+  if (!SPLIT && g.bias) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const uint32_t row = rt * kTile + wave / 2 * 64 + i * 32 + block_row(r);
+        out_of[i] |= (row < rows && g.bias[row0 + row] == -INFINITY ? 1u : 0u) << r;
+      }
+  }
 #pragma unroll
   for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -336,7 +347,7 @@ __global__ __launch_bounds__(256, RESTS ? 2 : kGradWaves<T>) void grad_rows_kern
           if constexpr (SPLIT) {
             part[((uint64_t)split * rows + row) * g.d + c] = acc[i][j][r];
           } else {
-            const bool left_out = g.bias && g.bias[row0 + row] == -INFINITY;  // (zero, whatever the queries hold)
+            const bool left_out = out_of[i] >> r & 1;  // (zero, whatever the queries hold)
             out[(uint64_t)(row0 + row) * stride + c] = from_f32<T>(left_out ? 0.0f : acc[i][j][r] * by);
           }
         }
@@ -615,6 +626,11 @@ __global__ __launch_bounds__(256, 2) void grad_short_kernel(GradArgs a, uint32_t
   if (OWN_ROWS && !drows) return;
   if (OWN_ROWS && a.slots && splits == 1) add_more<KS / 2>(a, own0, g.n, 0, scaling, acc);
   const float by = a.scaling ? g.scale * a.scaling[1] : g.scale;
+  uint32_t out_of = 0;  // the rows left out, a bit to each
+  if (OWN_ROWS && BIAS && splits == 1) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) out_of |= (own0 + block_row(r) < owned && g.bias[own0 + block_row(r)] == -INFINITY ? 1u : 0u) << r;
+  }
 #pragma unroll
   for (int b = 0; b < KS / 2; ++b) {
     const uint32_t column = b * 32 + lane % 32;
@@ -623,7 +639,7 @@ __global__ __launch_bounds__(256, 2) void grad_short_kernel(GradArgs a, uint32_t
       const uint32_t l = own0 + block_row(r);
       if (l >= owned || column >= g.d) continue;
       if (OWN_ROWS && splits == 1) {
-        const bool left_out = BIAS && g.bias[l] == -INFINITY;  // (zero, whatever the queries hold)
+        const bool left_out = BIAS && (out_of >> r & 1);  // (zero, whatever the queries hold)
         drows[l * stride + column] = from_f32<T>(left_out ? 0.0f : acc[b][r] * by);
       } else {
         part[((uint64_t)split * owned + l) * g.d + column] = acc[b][r];
