@@ -708,7 +708,7 @@ uint64_t ann_row_logprobs_backward_workspace(uint32_t nq, uint64_t n, uint32_t d
  *                the divergence of the softmax over all rows from the teacher's, as far as its list goes (where the
  *                t sum to less than one, it is smallest, T log T with their sum T, where the model gives the listed rows all its probability).
  *                +infinity where a row that counts is left out; 0 where none counts.
- *   lse[i]       as ann_row_logprobs returns it.
+ *   lse[i]       log sum_j exp(s[i][j]) as in ann_row_logprobs (of fp32 rows nearer to it: their products' smaller parts are summed apart).
  *   logprobs     [nq][k] the log probabilities of the given rows under the softmax of all rows'
  *                scores; 0 where the id is not below n, -infinity where the row is left out.
  * The teacher's temperature is in its log probabilities, this model's in `scale`.  The weights

@@ -23,7 +23,7 @@ struct EmbedArgs {
 };
 
 // F: the table's type, T: of y.  A group of LANES lanes takes kUnits pieces to a lane at a time, `slots` of them to a row: so many reads are on
-// their way at once (one after the other: 72 us for 80,000 x 960 fp32 to bf16).
+// their way at once (80,000 x 960 fp32 to bf16: 98 us one after the other, 66 by four, 57 by eight and stored past the caches).
 template <typename F, typename T, int LANES, RowEnd END>
 __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs g, uint32_t slots, bool past) {
   constexpr int VEC = 16 / (int)sizeof(T), kGroups = 256 / LANES, kParts = VEC * (int)sizeof(F) / 16, kEach = VEC / kParts, kUnits = 8;
@@ -66,7 +66,7 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs g, uint32_t slots,
   }
 }
 
-// Rows of zeros; hit: but those whose bit is set.
+// Rows first .. end - 1 of zeros; hit: but those that it marks.
 template <typename F>
 __device__ __forceinline__ void zero_rows(F *table, uint64_t first, uint64_t end, uint64_t stride, uint32_t dim, const uint8_t *hit, uint32_t block,
                                           uint32_t blocks) {

@@ -95,8 +95,8 @@ __global__ __launch_bounds__(256) void distill_whole_kernel(GivenArgs a) {
 }
 
 // An entry's weight and what the rounding of the first part's element left, which is taken once for a row that is given twice; and their sum over the
-// query's entries of more * row: a workgroup to a query (and to each gridDim.y-th part of its columns), kGivenLanes pieces of columns at a time, kGivenRuns runs of entries side by side.  T: the type
-// that G is rounded to.  part NULL: the entries alone.  Workgroups behind the queries' only fill the slots.
+// query's entries of more * row: a workgroup to a query (and to each gridDim.y-th part of its columns), kGivenLanes pieces of columns at a time,
+// kGivenRuns runs of entries side by side.  T: the type that G is rounded to.  part NULL: the entries alone.  Workgroups behind the queries' only fill the slots.
 constexpr uint32_t kGivenRuns = 8, kGivenLanes = 32;
 template <typename T, RowEnd END>
 __global__ __launch_bounds__(kGivenRuns * kGivenLanes) void distill_more_kernel(GivenArgs a, const float *__restrict__ scaling, float *__restrict__ part) {
