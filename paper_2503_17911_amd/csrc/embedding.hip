@@ -6,7 +6,7 @@
 // are put in order with their positions (id_sort.hpp), so that a table's row is the sum of a run of entries (row_runs.hpp).  Rows without an id are filled
 // with zeros beside the sorting, which leaves most of the card idle: with few ids the whole table, with many what the first pass over the ids found no id for.
 // Measured: 80,000 x 960 fp32 to bf16 57 us (246 MB of distinct rows and output; frequent rows are read into each die's L2); gradient of 80,000 x 768 bf16 into
-// 50,000 fp32 rows 106 us: order 41 with the zeros beside it, runs 45, their join 10; of 5,003 x 100 fp16 22 us.
+// 50,000 fp32 rows 98 us: order 34 with the zeros beside it, runs 45, their join 10; of 5,003 x 100 fp16 22 us.
 #include "row_runs.hpp"
 
 namespace ann {

@@ -11,7 +11,7 @@
 // probability; it differs by 1e-6 of itself, so that the remainder is another step's in one of some thousand elements, which then errs by a rounding to
 // 16 bits as all others do).  For dq that is a sum of k rows to a query.  For the rows the entries are put in the order of their ids
 // and summed by runs, so that a row that many teachers name costs no more than others.
-// Measured: 4,096 x 100,000 x 128 bf16 with k = 32: 600 us, of which the first part takes 530 (bound as its kernels are), the order of the entries 29, their runs
+// Measured: 4,096 x 100,000 x 128 bf16 with k = 32: 600 us, of which the first part takes 530 (bound as its kernels are), the order of the entries 27, their runs
 // and join 26, the entries and the queries' sums 17; 8 x 1M x 128 forward 55 us, 5 of them for the given rows.
 #include "row_logprobs.hpp"
 #include "row_runs.hpp"

@@ -158,7 +158,7 @@ def test_same_bits_again_on_other_streams_and_in_graphs():
 
 
 def test_many_tokens():
-    """More than the sort's blocks take in eight rounds, and more chunks than there may be of the shortest; ones are summed exactly."""
+    """More than the sort's blocks take in their usual rounds, and more chunks than there may be of the shortest; ones are summed exactly."""
     import paper_2503_17911_amd as ann
     n, rows = 17_500_000, 5000
     g = torch.Generator(device="cuda").manual_seed(1)
