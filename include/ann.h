@@ -713,6 +713,8 @@ uint64_t ann_row_logprobs_backward_workspace(uint32_t nq, uint64_t n, uint32_t d
  *                scores; 0 where the id is not below n, -infinity where the row is left out.
  * The teacher's temperature is in its log probabilities, this model's in `scale`.  The weights
  * t need not sum to one.  A row may be given twice: its weights add.
+ * Of short lists (n <= 256 and nq n <= 2^23; n <= 1024, nq n <= 2^20 and nq n d <= 3 * 2^28) the scores and their
+ * sums are fp64, kept in the workspace (8 bytes each).
  * scores->targets is NULL.  1 <= k <= ANN_MAX_ALTERNATIVES.  What ann_row_logprobs says of scores that
  * are not finite holds here; sums of the loss are fp64.  nq = 0 does nothing.
  * Errors as ann_row_logprobs.

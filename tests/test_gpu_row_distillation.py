@@ -388,3 +388,39 @@ def test_offsets_beyond_32_bits():
                                           workspace_bytes=needb)
         got.append(out + [drows[:, :d].clone()])
     assert all(torch.equal(a, c) for a, c in zip(*got)) and (got[0][4] != 0).any()
+
+
+SHORT = [(1, 1, 1, 1), (1, 16, 8, 2), (17, 15, 7, 3), (16, 17, 33, 20), (3, 64, 5, 64), (300, 256, 96, 10), (33, 255, 961, 20), (40, 257, 300, 5), (20, 1024, 100, 32), (1000, 100, 131, 40)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("nq, n, d, k", SHORT)
+def test_short_lists_are_summed_in_64_bits(nq, n, d, k, dtype):
+    """Of short lists every sum is fp64: the results are off by their own rounding, a small loss too (students near their teacher)."""
+    import paper_2503_17911_amd as ann
+    for bias, pad, scale in (("none", 0, 10.0), ("holes", 1, 8.0), ("plain", 8, -3.0)):
+        q, rows, b, _ = inputs(nq, n, d, dtype, n + d, bias)
+        ids, given = teacher_lists(q, rows, b, scale, k, d, near=0.02)
+        z = R.scores(q, rows, scale, b)
+        lse, logp, loss, t, _ = definition(z, ids, given)
+        got = forward(ann, q, rows, b, ids, given, scale, pad)
+        # fp64: d + n additions and a few functions, of scores up to |scale| |q| |x| + |bias|; times what a loss sums.  2 ** -24 of a result: its rounding
+        most = abs(scale) * q.double().norm(dim=1) * rows.double().norm(dim=1).max() + (0.0 if b is None else b[b > -math.inf].abs().max())
+        wide = (2 * d + n + 64) * 2.0 ** -53 * (1 + most + lse.abs())
+        for f, want, slack in (("lse", lse, wide), ("logprobs", logp, 2 * wide[:, None]), ("loss", loss, 2 * wide * t.sum(1) + 64 * 2.0 ** -53 * (t * (given.double() - logp).nan_to_num()).abs().sum(1))):
+            there = want.abs() < math.inf
+            assert torch.equal(got[f].double()[~there], want[~there]), f
+            assert ((got[f].double() - want).abs() <= R.U32 * want.abs() + slack + 2.0 ** -149)[there].all(), f
+
+
+def test_short_list_spoilt_in_its_left_out_rows():
+    """What lies in rows left out has no part in any result; of more scores than the kernels of short lists take, the others' do the same."""
+    import paper_2503_17911_amd as ann
+    for nq, n in ((50, 200), (40000, 250), (1100, 1000)):
+        q, rows, b, _ = inputs(nq, n, 40, "bf16", 7, "holes")
+        ids, given = teacher_lists(q, rows, b, 10.0, 8, 3)
+        first = check_forward(ann, q, rows, b, ids, given, 10.0)
+        spoilt = rows.clone()
+        spoilt[b == -math.inf] = float("nan")
+        second = forward(ann, q, spoilt, b, ids, given, 10.0)
+        assert all(torch.equal(first[f], second[f]) for f in first)
