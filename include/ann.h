@@ -733,8 +733,9 @@ uint64_t ann_row_distillation_workspace(uint32_t nq, uint64_t n, uint32_t d, uin
  * The part of G that all rows have is rounded and multiplied as ann_row_logprobs_backward
  * does it (power of two of f16: by the largest finite |g_loss T|); that of the given rows is added in fp32,
  * with what the rounding left at these rows.  Rows left out get zero, a query whose lse is -infinity too.
- * The workspace holds a number to a row and sums of fp32 rows for the smaller of n and nq * k of them,
- * beside what ann_row_logprobs_backward asks for.  Errors as ann_row_distillation.
+ * Of short lists (as above, and at most 4,096 queries) G and its products are fp64 and rounded once, at the end,
+ * with 8 bytes of workspace to a score.  Otherwise the workspace holds a number to a row and sums of fp32 rows for the
+ * smaller of n and nq * k of them, beside what ann_row_logprobs_backward asks for.  Errors as ann_row_distillation.
  */
 ann_status ann_row_distillation_backward(const ann_row_scores *scores, uint32_t k, const uint32_t *given_ids,
                                          const float *given_logprobs, const float *lse, const float *logprobs,

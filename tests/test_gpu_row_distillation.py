@@ -424,3 +424,55 @@ def test_short_list_spoilt_in_its_left_out_rows():
         spoilt[b == -math.inf] = float("nan")
         second = forward(ann, q, spoilt, b, ids, given, 10.0)
         assert all(torch.equal(first[f], second[f]) for f in first)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("nq, n, d, k", SHORT)
+def test_gradients_over_short_lists_are_summed_in_64_bits(nq, n, d, k, dtype):
+    """The gradients are off by lse's rounding to fp32, which they take the probabilities from, and by their own."""
+    import paper_2503_17911_amd as ann
+    gen = torch.Generator().manual_seed(nq)
+    for bias, pad, scale in (("none", 0, 10.0), ("holes", 1, 8.0), ("plain", 8, -3.0)):
+        q, rows, b, _ = inputs(nq, n, d, dtype, n + d, bias)
+        ids, given = teacher_lists(q, rows, b, scale, k, d, near=0.02)
+        z = R.scores(q, rows, scale, b)
+        lse, _, _, t, B = definition(z, ids, given)
+        g = 0.5 + torch.rand(nq, generator=gen)
+        lse32 = torch.where(torch.rand(nq, generator=gen) < 0.5, lse, lse + 0.3).float()   # (of more rows than these, as with rows on several cards)
+        got = backward(ann, q, rows, b, ids, given, scale, lse32, torch.zeros(nq, k), g, pad)
+        A = (g.double() * t.sum(1))[:, None] * torch.where(z == -math.inf, 0.0, (z - lse32.double()[:, None]).exp())
+        G = A + g.double()[:, None] * B
+        x, qq = rows.double(), q.double()
+        if b is not None:
+            x = torch.where((b == -math.inf)[:, None], 0.0, x)
+        # fp64: a score as above, an exponential of it, k subtractions, the products' n or nq additions; 2 ** -24 and half a step: the roundings at the end
+        most = abs(scale) * q.double().norm(dim=1) * rows.double().norm(dim=1).max() + (0.0 if b is None else b[b > -math.inf].abs().max())
+        wide = ((2 * d + k + 64) * 2.0 ** -53 * (1 + most + lse.abs()))[:, None] * (A + g.double()[:, None] * B.abs())
+        many = (n + nq + 64) * 2.0 ** -53
+        terms = A + g.double()[:, None] * B.abs()
+        for f, want, slack in (("dq", G @ x, wide @ x.abs() + many * (terms @ x.abs())), ("drows", G.T @ qq, wide.T @ qq.abs() + many * (terms.T @ qq.abs()))):
+            tol = (abs(scale) * (want.abs() * R.U32 + slack) + R.half_step(q.dtype) * abs(scale) * want.abs()) * (1 + 2 * R.half_step(q.dtype)) + R.smallest_step(q.dtype)
+            assert ((got[f].double() - scale * want).abs() <= tol).all(), f
+        assert ((got["drow_bias"].double() - G.sum(0)).abs() <= R.U32 * G.sum(0).abs() + wide.sum(0) + many * terms.sum(0) + 2.0 ** -149).all()
+        # each by itself, and again: the same bits
+        for only in (dict(drows=False, dbias=False), dict(dq=False, dbias=False), dict(dq=False, drows=False), dict()):
+            again = backward(ann, q, rows, b, ids, given, scale, lse32, torch.zeros(nq, k), g, pad, **only)
+            assert all(torch.equal(again[f], got[f]) for f in again)
+
+
+def test_gradients_over_short_lists_with_spoilt_rows_left_out_and_queries_without_rows():
+    import paper_2503_17911_amd as ann
+    q, rows, b, _ = inputs(50, 200, 41, "bf16", 7, "holes")
+    ids, given = teacher_lists(q, rows, b, 10.0, 8, 3)
+    g = torch.ones(50)
+    z = R.scores(q, rows, 10.0, b)
+    lse = definition(z, ids, given)[0].float()
+    first = backward(ann, q, rows, b, ids, given, 10.0, lse, torch.zeros(50, 8), g)
+    spoilt = rows.clone()
+    spoilt[b == -math.inf] = float("nan")
+    second = backward(ann, q, spoilt, b, ids, given, 10.0, lse, torch.zeros(50, 8), g)
+    assert all(torch.equal(first[f], second[f]) for f in first)
+    assert (first["drows"][:, :41][b == -math.inf] == 0).all() and (first["drow_bias"][b == -math.inf] == 0).all()
+    out = torch.full((200,), -math.inf)
+    none = backward(ann, q, rows, out, ids, given, 10.0, torch.full((50,), -math.inf), torch.full((50, 8), -math.inf), g)
+    assert all((none[f][:, :41] == 0).all() for f in ("dq", "drows")) and (none["drow_bias"] == 0).all()
