@@ -3,6 +3,7 @@
 //   t_ie = exp(given_ie),  loss_i = sum_e t_ie (given_ie - log p_i[id_ie]),  T_i = sum_e t_ie
 //   G[i][j] = g_i (T_i p_ij - sum of t_ie over the entries e with id_ie = j),   dq = scale G X,  dX = scale G^T Q,  dbias = sum_i G_i
 //
+// (Short lists have kernels of their own, below.)
 // Forward: the log of the softmax' sum over all rows is that of the rows' log probabilities; the given rows' scores are formed again (fp64 sums).
 // Backward: G has a part at all rows and one at k rows of each query.  The first is what the rows' log probabilities have, with the weight
 // -g_i T_i: its kernels.  The second is added in fp32 to the products' results before these are rounded, together with what the

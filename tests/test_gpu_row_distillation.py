@@ -476,3 +476,43 @@ def test_gradients_over_short_lists_with_spoilt_rows_left_out_and_queries_withou
     out = torch.full((200,), -math.inf)
     none = backward(ann, q, rows, out, ids, given, 10.0, torch.full((50,), -math.inf), torch.full((50, 8), -math.inf), g)
     assert all((none[f][:, :41] == 0).all() for f in ("dq", "drows")) and (none["drow_bias"] == 0).all()
+
+
+def test_short_lists_in_a_graph():
+    """Forward and backward captured over one workspace and replayed with other contents, with eager work between: each replay gives the eager calls' bits."""
+    import paper_2503_17911_amd as ann
+    nq, n, d, k, t = 37, 200, 100, 8, types(ann)[torch.bfloat16]
+    cases = []
+    for seed in (1, 2, 3):
+        q, rows, b, _ = inputs(nq, n, d, "bf16", seed, "holes")
+        cases.append((q.cuda(), rows.cuda(), b.cuda(), *(x.cuda() for x in teacher_lists(q, rows, b, 10.0, k, seed))))
+    held = [x.clone() if x.dtype != torch.int64 else x.to(torch.int32) for x in cases[0]]
+    q, rows, b, ids, given = held
+    need = max(ann.ann_row_distillation_workspace(nq, n, d, t, k), ann.ann_row_distillation_backward_workspace(nq, n, d, t, k))
+    ws = dirty(need)
+    loss, lse, logprobs, g = torch.empty(nq, device="cuda"), torch.empty(nq, device="cuda"), torch.empty(nq, k, device="cuda"), torch.full((nq,), 0.5, device="cuda")
+    dq, drows, dbias = torch.empty_like(q), torch.empty_like(rows), torch.empty(n, device="cuda")
+
+    def both():
+        what = dict(q=q, nq=nq, q_stride=d, rows=rows, n=n, row_stride=d, d=d, type=t, scale=10.0, row_bias=b, k=k, given_ids=ids, given_logprobs=given, workspace=ws,
+                    workspace_bytes=need, stream=stream())
+        ann.ann_row_distillation(**what, loss=loss, lse=lse, logprobs=logprobs)
+        ann.ann_row_distillation_backward(**what, lse=lse, logprobs=logprobs, g_loss=g, dq=dq, dq_stride=d, drows=drows, drows_stride=d, drow_bias=dbias)
+
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        both()
+    side.synchronize()
+    with torch.cuda.graph(graph):
+        both()
+    for case in cases + cases:
+        for to, x in zip(held, case):
+            to.copy_(x)
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = [x.clone() for x in (loss, lse, logprobs, dq, drows, dbias)]
+        ws.fill_(0xFF)
+        both()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(replayed, (loss, lse, logprobs, dq, drows, dbias)))
