@@ -702,8 +702,8 @@ uint64_t ann_row_logprobs_backward_workspace(uint32_t nq, uint64_t n, uint32_t d
  * Distillation: the loss that a model is trained with where another, its teacher, says what it
  * answers: k rows and their log probabilities for every query, such as the alternatives
  * that ann_row_logprobs gives for the teacher's queries (over the teacher's rows, the same in number and order).
- *   given_ids, given_logprobs  [nq][k]; entries whose id is not below n (ANN_PAD_ID)
- *                or whose log probability is -infinity do not count.
+ *   given_ids, given_logprobs  [nq][k]; entries whose id is not below n (ANN_PAD_ID) or whose
+ *                weight exp(given_logprobs) is zero in fp64 (-infinity, and below some -745) do not count.
  *   loss[i]      = sum_e t_ie (given_logprobs[i][e] - logprobs[i][e]),  t = exp(given_logprobs);
  *                the divergence of the softmax over all rows from the teacher's, as far as its list goes (where the
  *                t sum to less than one, it is smallest, T log T with their sum T, where the model gives the listed rows all its probability).

@@ -47,8 +47,8 @@ __global__ __launch_bounds__(256) void distill_loss_kernel(ScoreTable g, uint32_
     double logp = 0.0;
     if (id < g.n) logp = bias == -INFINITY ? -INFINITY : sum * (double)g.scale + (double)bias - l;
     logprobs[(uint64_t)q * k + e] = (float)logp;
-    const double t = id < g.n ? (double)given[(uint64_t)q * k + e] : -INFINITY;
-    terms[e] = t == -INFINITY ? 0.0 : exp(t) * (t - logp);
+    const double t = id < g.n ? (double)given[(uint64_t)q * k + e] : -INFINITY, weight = exp(t);
+    terms[e] = weight == 0.0 ? 0.0 : weight * (t - logp);  // (without a weight nothing counts, also where logp is -infinity)
   }
   __syncthreads();
   if (threadIdx.x != 0) return;
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(256) void distill_short_loss_kernel(uint32_t nq, ui
   const double *s = scores + (uint64_t)q * n;
   const uint64_t at = (uint64_t)q * k + lane;
   const uint32_t id = lane < k ? ids[at] : ANN_PAD_ID;
-  const float weight = id < n ? given[at] : -INFINITY;
+  const double t = id < n ? (double)given[at] : -INFINITY, weight = exp(t);
   const double own = id < n ? s[id] : 0.0;
   float top = -INFINITY;
   for (uint32_t j = lane; j < n; j += kWave) top = fmaxf(top, (float)s[j]);
@@ -130,8 +130,8 @@ __global__ __launch_bounds__(256) void distill_short_loss_kernel(uint32_t nq, ui
   for (uint32_t j = lane; j < n; j += kWave) sum += exp(s[j] - (double)top);
   sum = group_sum_f64<kWave>(sum);
   const double lse = sum == 0.0 ? -INFINITY : (double)top + log(sum);
-  const double logp = id >= n ? 0.0 : own == -INFINITY ? -INFINITY : own - lse, t = (double)weight;
-  const double all = group_sum_f64<kWave>(weight == -INFINITY ? 0.0 : exp(t) * (t - logp));
+  const double logp = id >= n ? 0.0 : own == -INFINITY ? -INFINITY : own - lse;
+  const double all = group_sum_f64<kWave>(weight == 0.0 ? 0.0 : weight * (t - logp));  // (without a weight nothing counts, also where logp is -infinity)
   if (lane < k) logprobs[at] = (float)logp;
   if (lane == 0) loss[q] = (float)all, lse_out[q] = (float)lse;
 }
