@@ -575,7 +575,9 @@ uint64_t ann_embedding_backward_workspace(uint64_t n, uint64_t rows, uint32_t di
  *                NULL where not wanted, and without a residual.
  *   rstd         [n] fp32, for the backward pass; NULL allowed.
  * sum may be x or residual, y may be x or residual (same strides); sum and y are not
- * the same rows.  Squares may leave fp32's range: every row of finite elements has its rstd (a row with an infinite element: 0).
+ * the same rows.  Squares may leave fp32's range at either end, also with eps = 0: y is that of every row of finite elements, and rstd is +infinity where fp32
+ * has no number for it (eps = 0 and a root mean square below 2^-128).  A row with an infinite element: rstd 0.  A row of zeros with eps = 0 has no
+ * norm: rstd +infinity, y NaN.
  * n = 0 does nothing.  dim <= ANN_MAX_NORM_DIM.
  * Errors: ANN_EINVAL (NULL x or y, dim == 0, types, strides, sum without residual or over y, eps negative
  * or NaN), ANN_ECAPACITY.

@@ -76,14 +76,24 @@ __device__ __forceinline__ void load_weights(float (&w)[VEC], const RmsArgs &g, 
   }
 }
 
-// 1 / sqrt(mean + eps) of a row's squares, whose sum over the row `sum` forms of values times a factor: where it leaves fp32's range, of values
-// times 2^-80 once more (all lanes of a row take the same way).
+// 1 / sqrt(mean + eps) of a row's squares, whose sum over the row `sum` forms of values times a factor (all lanes of a row take the same way).  Where the
+// sum leaves fp32's range, of values times 2^-80 once more.  Where mean + eps is below 2^-100, so that squares below fp32's normal numbers (each off by up to
+// 2^-126, were they left out) would be seen, of values times 2^100: they are at most 2^-50 sqrt(dim), and their squares 2^-98 at least.  1 / rms itself is above
+// fp32's range below 2^-128: the row's values times `by` and the result `of_scaled` are in it, and rstd = by * of_scaled where that has a number.
+struct RowScale {
+  float by, of_scaled;  // h * rstd = (h * by) * of_scaled; by is 1 or 2^100
+};
 template <typename Sum>
-__device__ __forceinline__ float row_rstd(Sum sum, float inv_dim, float eps) {
+__device__ __forceinline__ RowScale row_rstd(Sum sum, float inv_dim, float eps) {
   float sq = sum(1.0f);
-  if (sq < INFINITY || sq != sq) return 1.0f / sqrtf(__builtin_fmaf(sq, inv_dim, eps));
+  const float mean = __builtin_fmaf(sq, inv_dim, eps);
+  if (mean < 0x1p-100f) {
+    sq = sum(0x1p100f);
+    return {0x1p100f, 1.0f / sqrtf(__builtin_fmaf(sq, inv_dim, eps * 0x1p100f * 0x1p100f))};
+  }
+  if (sq < INFINITY || sq != sq) return {1.0f, 1.0f / sqrtf(mean)};
   sq = sum(0x1p-80f);
-  return 0x1p-80f / sqrtf(sq * inv_dim);  // (eps is nothing beside it)
+  return {1.0f, 0x1p-80f / sqrtf(sq * inv_dim)};  // (eps is nothing beside it)
 }
 
 // x + residual, rounded once to T.
@@ -124,7 +134,7 @@ __global__ __launch_bounds__(kRmsThreads<LANES>) void rms_kernel(RmsArgs g) {
         for (int it = 0; it < ITEMS; ++it) p[it].store(sum, (it * LANES + lane) * VEC, g.dim);
       }
     }
-    const float rstd = row_rstd(
+    const RowScale scale_of = row_rstd(
         [&](float by) {
           float sq = 0.0f;
 #pragma unroll
@@ -134,7 +144,17 @@ __global__ __launch_bounds__(kRmsThreads<LANES>) void rms_kernel(RmsArgs g) {
           return row_sum<LANES>(sq, room);
         },
         inv_dim, g.eps);
-    if (lane == 0 && g.rstd) g.rstd[row] = rstd;
+    const float rstd = scale_of.of_scaled;
+    if (lane == 0 && g.rstd) g.rstd[row] = scale_of.by * rstd;
+    if (scale_of.by != 1.0f) {  // (exact: tiny values, of types with fp32's range, or zeros)
+#pragma unroll
+      for (int it = 0; it < ITEMS; ++it) {
+        float v[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[e] = p[it].get(e) * scale_of.by;
+        p[it].set(v);
+      }
+    }
     if constexpr (!E4M3) {
       T *y = (T *)g.y + row * g.y_stride;
 #pragma unroll
@@ -200,7 +220,7 @@ __global__ __launch_bounds__(1024) void rms_long_kernel(RmsArgs g) {
       }
       return p;
     };
-    const float rstd = row_rstd(
+    const RowScale scale_of = row_rstd(
         [&](float by) {
           float sq = 0.0f;
           for (uint32_t c = threadIdx.x * VEC; c < g.dim; c += 1024 * VEC) {
@@ -211,9 +231,9 @@ __global__ __launch_bounds__(1024) void rms_long_kernel(RmsArgs g) {
           return row_sum<1024>(sq, room);
         },
         inv_dim, g.eps);
-    if (threadIdx.x == 0 && g.rstd) g.rstd[row] = rstd;
+    if (threadIdx.x == 0 && g.rstd) g.rstd[row] = scale_of.by * scale_of.of_scaled;
     const auto value = [&](const P &p, uint32_t c, int e) {
-      return p.get(e) * rstd * (g.weight && c + e < g.dim ? load_param<T>(g.weight, g.weight_f32, c + e) : 1.0f);
+      return p.get(e) * scale_of.by * scale_of.of_scaled * (g.weight && c + e < g.dim ? load_param<T>(g.weight, g.weight_f32, c + e) : 1.0f);
     };
     if constexpr (!E4M3) {
       T *y = (T *)g.y + row * g.y_stride;
