@@ -590,7 +590,8 @@ ann_status ann_rms_norm(const void *x, uint64_t n, uint32_t dim, uint64_t x_stri
  * The same with y in 8 bits, for products of 8-bit elements: codes e4m3 (4 bits of
  * exponent, 3 of mantissa, largest value 448, no infinities) with a scale to
  * every `group` columns of a row:
- *   scale = max(largest |v| of the group, 2^-100) / 448,  code = v / scale rounded once,  v = h * rstd * weight in fp32.
+ *   scale = max(largest |v| of the group, 2^-100) / 448,  code = v / scale,  v = h * rstd * weight,
+ * all in fp32; the quotient, correctly rounded to fp32, is rounded to 8 bits once (to nearest, ties to the even code).
  *   group        32, 64 or 128 columns (the last group of a row may be shorter), or 0: one scale to a row.
  *   scales       [n] rows of ceil(dim / group) (group 0: one) fp32.
  * y is not x or residual.  Values that are not numbers get the code for that and do not

@@ -4,7 +4,7 @@
 //   dx = rstd * (a - xh * mean(a * xh)) + dsum,  a = dy * w,  xh = h * rstd;   dw = sum over rows of dy * xh
 //
 // The norm is that of h as it is kept, so that the gradient, which reads h again, is that of the values returned.
-// In 8 bits (e4m3): v = h * rstd * w in fp32, scale = max |v| / 448 over a group of columns (or the row), code = v / scale, rounded once.
+// In 8 bits (e4m3): v = h * rstd * w in fp32, scale = max |v| / 448 over a group of columns (or the row), code = fp32's quotient v / scale, rounded to 8 bits.
 //
 // Bound by memory: every row is read once and stays in the registers of 16 to 512 lanes as the pieces that were loaded (of 16 bytes with any
 // alignment: rows of odd strides are read as wide as the others), one to four to a lane; sums are fp32.  A group of columns that
@@ -37,13 +37,14 @@ template <int LANES>
 constexpr int kRmsThreads = LANES > 256 ? LANES : 256;
 
 // The codes of v / scale, of the VEC values from column c on: 448 is the largest that there is, v / scale is not above it but for its rounding.
+// (A division: times 1 / scale, which is rounded itself, values halfway between two codes leave their place: 175 of a scale of 7.)
 template <int VEC>
-__device__ __forceinline__ void store_codes(const float (&v)[VEC], float inv, uint8_t *row, uint32_t c, uint32_t columns) {
+__device__ __forceinline__ void store_codes(const float (&v)[VEC], float scale, uint8_t *row, uint32_t c, uint32_t columns) {
   Words<VEC / 4, 1> o;
 #pragma unroll
   for (int w = 0; w < VEC / 4; ++w) {
-    const int low = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * w] * inv, v[4 * w + 1] * inv, 0, false);
-    o.v[w] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * w + 2] * inv, v[4 * w + 3] * inv, low, true);
+    const int low = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * w] / scale, v[4 * w + 1] / scale, 0, false);
+    o.v[w] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * w + 2] / scale, v[4 * w + 3] / scale, low, true);
   }
   if (c + VEC <= columns) {
     *(Words<VEC / 4, 1> *)(row + c) = o;
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(kRmsThreads<LANES>) void rms_kernel(RmsArgs g) {
         const uint32_t c = (it * LANES + lane) * VEC;
         const float scale = fmaxf(g.group ? lanes_max(most[it], g.group / VEC) : whole, kSmallestMax) / kE4m3Max;
         if (g.group ? c < g.dim && c % g.group == 0 : c == 0) scales[g.group ? c / g.group : 0] = scale;
-        store_codes(v[it], 1.0f / scale, y, c, g.dim);
+        store_codes(v[it], scale, y, c, g.dim);
       }
     }
   }
@@ -269,7 +270,7 @@ __global__ __launch_bounds__(1024) void rms_long_kernel(RmsArgs g) {
         }
         const float scale = fmaxf(g.group ? lanes_max(most, g.group / VEC) : whole, kSmallestMax) / kE4m3Max;
         if (in && (g.group ? c % g.group == 0 : c == 0)) scales[g.group ? c / g.group : 0] = scale;
-        if (in) store_codes(v, 1.0f / scale, y, c, g.dim);
+        if (in) store_codes(v, scale, y, c, g.dim);
       }
     }
   }
