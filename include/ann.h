@@ -733,9 +733,12 @@ uint64_t ann_row_distillation_workspace(uint32_t nq, uint64_t n, uint32_t d, uin
  *   dq[i]    = scale * sum_j G[i][j] x_j         drows[j] = scale * sum_i G[i][j] q_i
  *   drow_bias[j] = sum_i G[i][j]
  * dq, drows (of `type`, with their strides) and drow_bias ([n] fp32) each may be NULL where not wanted.
- * The part of G that all rows have is rounded and multiplied as ann_row_logprobs_backward
- * does it (power of two of f16: by the largest finite |g_loss T|); that of the given rows is added in fp32,
- * with what the rounding left at these rows.  Rows left out get zero, a query whose lse is -infinity too.
+ * The part of G that all rows have is multiplied as ann_row_logprobs_backward does it (power of two of f16: by the largest
+ * finite |g_loss T|), with 16-bit rows in two parts of 16 bits: what the rounding of an element leaves is taken along wherever its
+ * probability is above 2^-10, in drows of up to 256 queries always (of smaller ones it may stay: a query's are less than 1/32 of half a
+ * step of |g_loss T| together, as a root of the sum of squares).  The part of the given rows is added in fp32.  The results
+ * are off by their own rounding and by what the scores and sums in fp32 are.  Rows left out get zero, a query whose lse is -infinity too.
+ * logprobs is what the forward pass wrote (it must be there; today's kernels take all they need from lse).
  * Of short lists (as above, and at most 4,096 queries) G and its products are fp64 and rounded once, at the end,
  * with 8 bytes of workspace to a score.  Otherwise the workspace holds a number to a row and sums of fp32 rows for the
  * smaller of n and nq * k of them, beside what ann_row_logprobs_backward asks for.  Errors as ann_row_distillation.

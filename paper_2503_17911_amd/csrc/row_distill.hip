@@ -6,12 +6,10 @@
 // (Short lists have kernels of their own, below.)
 // Forward: the log of the softmax' sum over all rows is that of the rows' log probabilities; the given rows' scores are formed again (fp64 sums).
 // Backward: G has a part at all rows and one at k rows of each query.  The first is what the rows' log probabilities have, with the weight
-// -g_i T_i: its kernels.  The second is added in fp32 to the products' results before these are rounded, together with what the
-// rounding of the first part's elements to 16 bits left at the same rows: where the student is near the teacher the two nearly cancel, and the
-// rounding of g T p alone would be all that is left (the element as the product took it is formed again from the forward pass' log
-// probability; it differs by 1e-6 of itself, so that the remainder is another step's in one of some thousand elements, which then errs by a rounding to
-// 16 bits as all others do).  For dq that is a sum of k rows to a query.  For the rows the entries are put in the order of their ids
-// and summed by runs, so that a row that many teachers name costs no more than others.
+// -g_i T_i: its kernels, with G of 16-bit rows in two parts of 16 bits (2^-18 of an element is left in bf16, 2^-24 in f16): where the student is near the
+// teacher, or its likely rows are alike, the products are small differences, and the rounding of g T p to 16 bits would be seen in them.  The second is
+// added in fp32 to the products' results before these are rounded.  For dq that is a sum of k rows to a query.  For the rows the entries are put in the
+// order of their ids and summed by runs, so that a row that many teachers name costs no more than others.
 // Measured: 4,096 x 100,000 x 128 bf16 with k = 32: 600 us, of which the first part takes 530 (bound as its kernels are), the order of the entries 27, their runs
 // and join 26, the entries and the queries' sums 17; 8 x 1M x 128 forward 55 us, 5 of them for the given rows.
 #include "row_logprobs.hpp"
@@ -283,11 +281,10 @@ struct GivenArgs {
   ScoreTable g;
   uint32_t k;
   const uint32_t *ids;
-  const float *given, *logprobs, *lse, *g_loss;
+  const float *given, *lse, *g_loss;
   float *whole;     // [nq]: -g T
   uint32_t *rows;   // [nq][k]: the entries' ids; ANN_PAD_ID where none counts
   float *weights;   // [nq][k]: -g t
-  float *more;      // [nq][k]: that and what the rounding left
   uint32_t *slots;  // [n]: filled with ANN_PAD_ID (NULL where not wanted)
 };
 
@@ -317,37 +314,27 @@ __global__ __launch_bounds__(256) void distill_whole_kernel(GivenArgs a) {
   if (lane_id() == 0) a.whole[q] = entry.whole;
 }
 
-// An entry's weight and what the rounding of the first part's element left, which is taken once for a row that is given twice; and their sum over the
-// query's entries of more * row: a workgroup to a query (and to each gridDim.y-th part of its columns), kGivenLanes pieces of columns at a time,
-// kGivenRuns runs of entries side by side.  T: the type that G is rounded to.  part NULL: the entries alone.  Workgroups behind the queries' only fill the slots.
+// The entries' weights, and the sum over a query's entries of weight * row: a workgroup to a query (and to each gridDim.y-th part of its columns),
+// kGivenLanes pieces of columns at a time, kGivenRuns runs of entries side by side.  T: of the rows.  part NULL: the entries alone.  Workgroups behind
+// the queries' only fill the slots.
 constexpr uint32_t kGivenRuns = 8, kGivenLanes = 32;
 template <typename T, RowEnd END>
 __global__ __launch_bounds__(kGivenRuns * kGivenLanes) void distill_more_kernel(GivenArgs a, const float *__restrict__ scaling, float *__restrict__ part) {
   constexpr int VEC = 16 / (int)sizeof(T), kEach = ANN_MAX_ALTERNATIVES / kGivenRuns;
-  __shared__ float more_of[ANN_MAX_ALTERNATIVES], room[kGivenRuns][kGivenLanes * VEC + 4];
+  __shared__ float weight_of[ANN_MAX_ALTERNATIVES], room[kGivenRuns][kGivenLanes * VEC + 4];
   __shared__ uint32_t id_of[ANN_MAX_ALTERNATIVES];
   if (a.slots && blockIdx.y == 0)
     for (uint64_t j = (uint64_t)blockIdx.x * 256 + threadIdx.x; j < a.g.n; j += (uint64_t)gridDim.x * 256) a.slots[j] = ANN_PAD_ID;
   const uint32_t q = blockIdx.x, lane = threadIdx.x % kGivenLanes, run = threadIdx.x / kGivenLanes;
   if (q >= a.g.nq) return;
-  const float by = scaling ? scaling[0] : 1.0f, back = scaling ? scaling[1] : 1.0f;
+  const float by = scaling ? scaling[0] : 1.0f;
   if (threadIdx.x < kWave) {
     const uint32_t e = threadIdx.x;
     const uint64_t at = (uint64_t)q * a.k + e;
     const Entry entry = given_entry(a, q, e);
-    bool again = false;
-    for (uint32_t o = 0; o < a.k; ++o) again |= (uint32_t)__builtin_amdgcn_readlane((int)entry.id, (int)o) == entry.id && o < e;
-    float more = 0.0f;
-    if (e < a.k) {
-      more = entry.weight;
-      if (sizeof(T) == 2 && entry.id < a.g.n && !again) {
-        const float v = -(expf(a.logprobs[at]) * (entry.whole * by));
-        more = __builtin_fmaf(v - to_f32(from_f32<T>(v)), back, more);
-      }
-      if (blockIdx.y == 0) a.rows[at] = entry.id, a.weights[at] = entry.weight, a.more[at] = more;
-    }
+    if (e < a.k && blockIdx.y == 0) a.rows[at] = entry.id, a.weights[at] = entry.weight;
     if (e == 0 && blockIdx.y == 0) a.whole[q] = entry.whole;
-    more_of[e] = more * by, id_of[e] = entry.id;
+    weight_of[e] = entry.weight * by, id_of[e] = entry.id;
   }
   if (!part) return;
   __syncthreads();
@@ -366,9 +353,9 @@ __global__ __launch_bounds__(kGivenRuns * kGivenLanes) void distill_more_kernel(
 #pragma unroll
     for (int u = 0; u < kEach; ++u) {
       const uint32_t id = begin + u < end ? id_of[begin + u] : ANN_PAD_ID;
-      const float more = begin + u < end ? more_of[begin + u] : 0.0f;
+      const float weight = begin + u < end ? weight_of[begin + u] : 0.0f;
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) sum[v] = id < a.g.n ? __builtin_fmaf(more, x[u].get(v), sum[v]) : sum[v];
+      for (int v = 0; v < VEC; ++v) sum[v] = id < a.g.n ? __builtin_fmaf(weight, x[u].get(v), sum[v]) : sum[v];
     }
     __syncthreads();  // (the columns before have been read)
 #pragma unroll
@@ -389,13 +376,13 @@ struct GivenSums {
   static constexpr bool kWeighted = true, kScalar = true;
   const T *q;
   uint64_t q_stride;
-  const float *more, *weights;
+  const float *weights;
   uint32_t *slots;
   float *sums;
   uint32_t k, ld, dim, d;
   bool by_row;  // a sum lies at its row's number; otherwise at that of the run's first entry
   __device__ __forceinline__ const T *row(uint32_t position) const { return q + position / k * q_stride; }
-  __device__ __forceinline__ float weight(uint32_t position) const { return more[position]; }
+  __device__ __forceinline__ float weight(uint32_t position) const { return weights[position]; }
   __device__ __forceinline__ float scalar(uint32_t position) const { return weights[position]; }
   __device__ __forceinline__ float *at(uint32_t id, uint32_t start) const { return sums + (uint64_t)(by_row ? id : start) * ld; }
   __device__ __forceinline__ void write_scalar(uint32_t id, uint32_t start, float sum) const {
@@ -417,7 +404,7 @@ struct DistillPlan {
   RunsPlan runs;
   bool by_row = false;
   uint32_t ld = 0;  // of the sums and their parts: d + 1, in pieces of 16 bytes
-  uint64_t backward_bytes = 0, whole_at = 0, rows_at = 0, weights_at = 0, more_at = 0, scaling_at = 0, slots_at = 0, sort_at = 0, part_at = 0, sums_at = 0;
+  uint64_t backward_bytes = 0, whole_at = 0, rows_at = 0, weights_at = 0, scaling_at = 0, slots_at = 0, sort_at = 0, part_at = 0, sums_at = 0;
   Parts parts;
 };
 
@@ -429,7 +416,7 @@ static DistillPlan distill_plan(uint32_t nq, uint64_t n, uint32_t d, uint32_t ty
   p.backward_bytes = scores_backward_bytes(nq, n, d, type, true);
   p.parts.take(p.backward_bytes);
   p.whole_at = p.parts.take(nq * 4ull);
-  p.rows_at = p.parts.take(entries * 4), p.weights_at = p.parts.take(entries * 4), p.more_at = p.parts.take(entries * 4);
+  p.rows_at = p.parts.take(entries * 4), p.weights_at = p.parts.take(entries * 4);
   p.scaling_at = p.parts.take(2 * sizeof(float));
   p.slots_at = p.parts.take(n * 4);
   p.sort = id_sort_plan(entries, n);
@@ -443,13 +430,12 @@ static DistillPlan distill_plan(uint32_t nq, uint64_t n, uint32_t d, uint32_t ty
 }
 
 template <typename T>
-static ann_status distill_rows(const DistillPlan &p, const GivenArgs &a, bool rows, bool few, char *ws, GradArgs &to, hipStream_t st) {
+static ann_status distill_rows(const DistillPlan &p, const GivenArgs &a, bool rows, char *ws, GradArgs &to, hipStream_t st) {
   SortedIds sorted;
   if (ann_status s = sort_ids(p.sort, a.rows, ws + p.sort_at, nullptr, NothingBeside(), st, sorted)) return s;
   const uint32_t dim = rows ? a.g.d : 0;
   const Runs runs = {sorted.keys, sorted.positions, a.g.nq * a.k, a.g.n, p.runs.chunk, p.runs.chunks, dim, (float *)(ws + p.part_at), p.ld};
-  // (few queries: the product takes along what G's rounding left)
-  const GivenSums<T> work = {(const T *)a.g.q, a.g.q_stride, few ? a.weights : a.more, a.weights, a.slots, (float *)(ws + p.sums_at), a.k, p.ld, dim, a.g.d, p.by_row};
+  const GivenSums<T> work = {(const T *)a.g.q, a.g.q_stride, a.weights, a.slots, (float *)(ws + p.sums_at), a.k, p.ld, dim, a.g.d, p.by_row};
   if (ann_status s = sum_runs<T>(runs, work, 0, st)) return s;
   to.slots = a.slots, to.sums = work.sums, to.more_ld = p.ld;
   return ANN_OK;
@@ -544,8 +530,8 @@ extern "C" ann_status ann_row_distillation_backward(const ann_row_scores *scores
   if (nq && scores->n) {
     const bool rows_side = drows || drow_bias;
     GivenArgs v = {};
-    v.g = a.g, v.k = k, v.ids = given_ids, v.given = given_logprobs, v.logprobs = logprobs, v.lse = lse, v.g_loss = g_loss;
-    v.whole = (float *)(ws + p.whole_at), v.rows = (uint32_t *)(ws + p.rows_at), v.weights = (float *)(ws + p.weights_at), v.more = (float *)(ws + p.more_at);
+    v.g = a.g, v.k = k, v.ids = given_ids, v.given = given_logprobs, v.lse = lse, v.g_loss = g_loss;
+    v.whole = (float *)(ws + p.whole_at), v.rows = (uint32_t *)(ws + p.rows_at), v.weights = (float *)(ws + p.weights_at);
     v.slots = rows_side ? (uint32_t *)(ws + p.slots_at) : nullptr;
     const uint32_t filling = rows_side ? (uint32_t)((scores->n + 4095) / 4096 < 2048 ? (scores->n + 4095) / 4096 : 2048) : 0, blocks = nq > filling ? nq : filling;
     a.g_logprob = v.whole;
@@ -576,10 +562,9 @@ extern "C" ann_status ann_row_distillation_backward(const ann_row_scores *scores
     ANN_HIP(hipGetLastError());
     a.more_part = true;
     if (rows_side) {
-      const bool few = type == ANN_F32 || nq <= kFewGradQueries;
-      ann_status s = type == ANN_F32   ? distill_rows<float>(p, v, drows, few, ws, a, st)
-                     : type == ANN_F16 ? distill_rows<f16_t>(p, v, drows, few, ws, a, st)
-                                       : distill_rows<bf16_t>(p, v, drows, few, ws, a, st);
+      ann_status s = type == ANN_F32   ? distill_rows<float>(p, v, drows, ws, a, st)
+                     : type == ANN_F16 ? distill_rows<f16_t>(p, v, drows, ws, a, st)
+                                       : distill_rows<bf16_t>(p, v, drows, ws, a, st);
       if (s) return s;
     }
   }

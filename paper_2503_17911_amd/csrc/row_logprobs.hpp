@@ -24,7 +24,7 @@ inline ScoreTable score_table(const ann_row_scores &s) {
 }
 
 // What the gradients of the scores are asked for.  With `every`, g_logprob is a weight of every query's probabilities, whether a row is given
-// or not (targets: NULL), and what more there is to single elements of G, after its rounding, is added in fp32:
+// or not (targets, g_entropy: NULL), G of 16-bit rows is multiplied in two parts of 16 bits, and what more there is to single elements of it is added in fp32:
 //   more_part    to dq: another part of its sums, which is in the workspace already (times what G is multiplied by)
 //   slots        to drows[j] (and drow_bias[j], its column d): sums[slots[j]] of more_ld elements, where slots[j] is not ANN_PAD_ID
 struct GradArgs {

@@ -22,6 +22,11 @@
 // 0.17 % in bf16).  So what it leaves is taken along: where queries are few (kFewGradQueries) of every element, in 16 bits more, otherwise of the
 // given rows' elements.  Where no given row's element outweighs the others (the entropy's gradient alone) G's rounding stays in the
 // results: up to 0.20 % in dq and 0.22 % in the rows' gradient in bf16, 2.4e-4 and 2.9e-4 in f16.
+// With `every` (distillation) what the rounding leaves goes to both products, as 16 bits more: no single element outweighs the others there, and where a few
+// likely rows are alike, or the student is near its teacher, dq is a small difference of them (0.43 to 1.3 % in bf16 without, 5 % of the worst query).
+// Blocks (of 32 x 32 elements, or 64 x 64 where G is stored) without a probability above kSmallShare are left with 16 bits: the roundings of elements that
+// small are at most sqrt(kSmallShare) = 1/32 of half a step of the query's weight times a row, all together as roots of sums of squares (p^2 <= kSmallShare p).
+// (The rows' gradient of few queries takes all remainders here too.)
 #include "row_logprobs.hpp"
 
 #include <math.h>
@@ -31,6 +36,7 @@ namespace ann {
 constexpr uint64_t kChunkBytes = 512ull << 20;  // of G at a time
 constexpr uint32_t kGradTarget = 768;           // workgroups of a product: three to a compute unit
 constexpr uint32_t kWideSlots = 512;            // of a wide one: two
+constexpr float kSmallShare = 0x1p-10f;         // a probability whose rounding to 16 bits may stay
 
 // Wavefronts to a SIMD of the gradients' products by tiles of 128 (three instead of two: 303 -> 237 and 282 -> 255 us with 2,048 x 50,000 x 768).
 template <typename T>
@@ -84,10 +90,11 @@ __global__ __launch_bounds__(1024) void grad_scaling_kernel(GradArgs a, float *_
 }
 
 // G of rows row0 .. row0 + rows (of this chunk), [nq][ld], zero from row n on.  m runs over rows, n over queries, so that a lane holds runs of
-// four rows of one query.  BIAS: biases and rows left out.  SUMS: row_sums[2 q_tile + half][ld] gets sums over 64 queries.
+// four rows of one query.  BIAS: biases and rows left out.  SUMS: row_sums[2 q_tile + half][ld] gets sums over 64 queries.  large[64 queries][64 rows] (NULL
+// where not wanted): whether a probability there is above kSmallShare; without all_rests, rests are written of the tiles that have such a block only.
 template <typename T, bool BIAS, bool ENTROPY, bool SUMS>
 __global__ __launch_bounds__(256) void grad_scores_kernel(GradArgs a, uint32_t row0, uint32_t q_tiles, uint32_t ld, T *__restrict__ G,
-                                                          T *__restrict__ rests, float *__restrict__ row_sums) {
+                                                          T *__restrict__ rests, bool all_rests, uint8_t *__restrict__ large, float *__restrict__ row_sums) {
   __shared__ __attribute__((aligned(16))) char lds[kTileBytes<T, kAlong, kAlong>];
   __shared__ float row_bias[kTile];
   const ScoreTable &g = a.g;
@@ -103,6 +110,7 @@ __global__ __launch_bounds__(256) void grad_scores_kernel(GradArgs a, uint32_t r
   tile_product<T, kAlong, kAlong, sizeof(T) == 4>(acc, X, first, Q, qt * kTile, 0, g.d, lds);  // (its barriers stand between row_bias and its use)
   const bool whole = first + kTile <= g.n;
   const float scaling = sizeof(T) == 2 && a.scaling ? a.scaling[0] : 1.0f;
+  bool any_large = false;
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     const uint32_t q = qt * kTile + nw + j * 32 + lane % 32;
@@ -130,6 +138,12 @@ __global__ __launch_bounds__(256) void grad_scores_kernel(GradArgs a, uint32_t r
         if ((BIAS || !whole) && bias == -INFINITY) v = 0.0f;
         acc[i][j][r] = none ? 0.0f : v;
       }
+      if (sizeof(T) == 2 && large) {
+        float most = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(acc[i][j][r]));
+        any_large |= most > kSmallShare * fabsf(gl);
+      }
       if (there) {
         T *out = G + (uint64_t)q * ld + rt * kTile + mw + i * 32 + lane / 32 * 4;
 #pragma unroll
@@ -138,12 +152,33 @@ __global__ __launch_bounds__(256) void grad_scores_kernel(GradArgs a, uint32_t r
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             o.v[e] = from_f32<T>(acc[i][j][r + e] * scaling);
-            if (sizeof(T) == 2 && rests) left.v[e] = from_f32<T>(__builtin_fmaf(acc[i][j][r + e], scaling, -to_f32(o.v[e])));
+            if (sizeof(T) == 2 && all_rests) left.v[e] = from_f32<T>(__builtin_fmaf(acc[i][j][r + e], scaling, -to_f32(o.v[e])));
             if (sizeof(T) == 2 && (uint32_t)(i * 32 + block_row(r + e)) == hit) a.rest[q] = __builtin_fmaf(acc[i][j][r + e], scaling, -to_f32(o.v[e]));
           }
           *(Piece<T, 4> *)(out + r * 2) = o;
-          if (sizeof(T) == 2 && rests) *(Piece<T, 4> *)(rests + (out - G) + r * 2) = left;
+          if (sizeof(T) == 2 && all_rests) *(Piece<T, 4> *)(rests + (out - G) + r * 2) = left;
         }
+      }
+    }
+  }
+  if (sizeof(T) == 2 && large) {
+    const bool with = __any(any_large);
+    if (lane == 0) large[(uint64_t)(qt * 2 + wave % 2) * (ld / 64) + rt * 2 + wave / 2] = with;
+    if (__syncthreads_or(with) && !all_rests) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t q = qt * kTile + nw + j * 32 + lane % 32;
+        if (q >= g.nq) continue;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; r += 4) {
+            Piece<T, 4> left;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              left.v[e] = from_f32<T>(__builtin_fmaf(acc[i][j][r + e], scaling, -to_f32(from_f32<T>(acc[i][j][r + e] * scaling))));
+            *(Piece<T, 4> *)(rests + (uint64_t)q * ld + rt * kTile + mw + i * 32 + lane / 32 * 4 + r * 2) = left;
+          }
       }
     }
   }
@@ -167,12 +202,48 @@ __global__ __launch_bounds__(256) void grad_scores_kernel(GradArgs a, uint32_t r
   }
 }
 
+// The runs of k in begin .. end, in steps of 64, whose blocks are marked for the same of HALVES halves of `lines` lines of 64 (of 2 each but for the last):
+// run(first, end, halves), by all lanes, a bit of halves to each that is marked.
+template <int HALVES, typename Run>
+__device__ __forceinline__ void marked_runs(const uint8_t *marks, uint32_t lines, uint64_t line_stride, uint64_t k_stride, uint32_t begin, uint32_t end, Run run) {
+  for (uint32_t b0 = begin / 64; b0 * 64 < end; b0 += 64) {
+    const uint32_t b = b0 + lane_id();
+    uint64_t of[HALVES], left = 0;
+#pragma unroll
+    for (uint32_t h = 0; h < HALVES; ++h) {
+      bool with = false;
+      if ((uint64_t)b * 64 < end)
+        for (uint32_t l = 2 * h; l < lines && l < 2 * h + 2; ++l) with |= marks[l * line_stride + b * k_stride] != 0;
+      of[h] = __ballot(with);  // (alike in all wavefronts)
+      left |= of[h];
+    }
+    while (left) {
+      const uint32_t first = __builtin_ctzll(left);
+      uint64_t other = ~left;  // blocks that are not as the first
+      uint32_t halves = 0;
+#pragma unroll
+      for (uint32_t h = 0; h < HALVES; ++h) {
+        const bool is = of[h] >> first & 1;
+        other |= is ? ~of[h] : of[h];
+        halves |= (is ? 1u : 0u) << h;
+      }
+      other &= ~0ull << first;
+      const uint32_t last = other ? __builtin_ctzll(other) : 64;
+      const uint32_t k0 = (b0 + first) * 64, k1 = (b0 + last) * 64;
+      run(k0 > begin ? k0 : begin, k1 < end ? k1 : end, halves);
+      left &= other ? ~0ull << last : 0;
+    }
+  }
+}
+
 // part[split][q][c] (+)= sum over the split's rows of the chunk of G[q][j] x[j][c]  (rows left out may hold anything: read as zeros, or,
 // MB == 4, there are none)
-// MB == 4: tiles of 256 queries by the wide product (2,048 x 50,000 x 768 fp16: 183 us, 860 TFLOP/s; by tiles of 128: 240).
-template <typename T, int MB>
+// MB == 4: tiles of 256 queries by the wide product (2,048 x 50,000 x 768 fp16: 183 us, 860 TFLOP/s; by tiles of 128: 240).  RESTS: also of what G's rounding left, in the
+// blocks that `large` names.
+template <typename T, int MB, bool RESTS>
 __global__ __launch_bounds__(256, MB == 4 ? 2 : kGradWaves<T>) void grad_queries_kernel(ScoreTable g, uint32_t row0, uint32_t rows, uint32_t ld, const T *__restrict__ G,
-                                                                                        uint32_t splits, float *__restrict__ part, bool add) {
+                                                                                        const T *__restrict__ rests, const uint8_t *__restrict__ large, uint32_t splits,
+                                                                                        float *__restrict__ part, bool add) {
   constexpr int kQueryTile = MB * 64, kMore = MB == 4 ? kWideBuffer : 16, kSlice = MB == 4 ? kWideSlice : Operand16<T>::kSlice;
   __shared__ __attribute__((aligned(16))) char lds[MB == 4 ? kWideBuffer : kTileBytes<T, kAlong, kAcross>], lds1[kMore], lds2[kMore];
   const uint32_t c_tiles = (g.d + kTile - 1) / kTile, q_tiles = (g.nq + kQueryTile - 1) / kQueryTile;
@@ -185,14 +256,30 @@ __global__ __launch_bounds__(256, MB == 4 ? 2 : kGradWaves<T>) void grad_queries
   uint32_t end = (uint32_t)((uint64_t)slices * (split + 1) / splits) * kSlice;
   f32x16 acc[MB][2];
   clear(acc);
+  // the tile's 64s of queries
+  const uint32_t lines = (g.nq - qt * kQueryTile + 63) / 64 < MB ? (g.nq - qt * kQueryTile + 63) / 64 : MB;
+  const uint8_t *marks = RESTS ? large + (uint64_t)qt * MB * (ld / 64) : nullptr;
   if constexpr (MB == 4) {
     // (G is zero behind the last row)
     const Lines<T> A = {G, ld, g.nq, ld}, B = {(const T *)g.rows + row0 * g.row_stride, g.row_stride, g.d, rows};
     wide_product<T, kAlong, kAcross>(acc, A, qt * kQueryTile, B, ct * kTile, begin, end, lds, lds1, lds2);
+    if constexpr (RESTS) {
+      const Lines<T> R = {rests, ld, g.nq, ld};
+      // (a tile of 128 queries that is not marked has no rests: its two wavefronts sit out)
+      marked_runs<2>(marks, lines, ld / 64, 1, begin, end, [&](uint32_t k0, uint32_t k1, uint32_t halves) {
+        wide_product<T, kAlong, kAcross, true>(acc, R, qt * kQueryTile, B, ct * kTile, k0, k1, lds, lds1, lds2,
+                                                __builtin_amdgcn_readfirstlane(halves >> (threadIdx.x / kWave / 2)) & 1);
+      });
+    }
   } else {
     if (end > rows) end = rows;
     const Lines<T> A = {G, ld, g.nq, rows}, B = {(const T *)g.rows + row0 * g.row_stride, g.row_stride, g.d, rows, g.bias ? g.bias + row0 : nullptr};
     tile_product<T, kAlong, kAcross>(acc, A, qt * kQueryTile, B, ct * kTile, begin, end, lds);
+    if constexpr (RESTS) {
+      const Lines<T> R = {rests, ld, g.nq, rows};
+      marked_runs<1>(marks, lines, ld / 64, 1, begin, end,
+                     [&](uint32_t k0, uint32_t k1, uint32_t) { tile_product<T, kAlong, kAcross>(acc, R, qt * kQueryTile, B, ct * kTile, k0, k1, lds); });
+    }
   }
   const int wave = (int)threadIdx.x / kWave, lane = lane_id();
 #pragma unroll
@@ -257,10 +344,11 @@ __global__ __launch_bounds__(THREADS) void grad_queries_sum_kernel(GradArgs a, c
 }
 
 // drows[row0 + j][c] = scale sum over the queries of G[q][j] q[q][c].  SPLIT: part[split][row][c] instead, of a split's queries.
-// RESTS: also of what G's rounding left; else what that of the given rows' elements did.
-template <typename T, bool SPLIT, bool RESTS>
-__global__ __launch_bounds__(256, RESTS ? 2 : kGradWaves<T>) void grad_rows_kernel(GradArgs a, uint32_t row0, uint32_t rows, uint32_t ld, const T *__restrict__ G, const T *__restrict__ rests,
-                                                        T *__restrict__ out, uint64_t stride, float *__restrict__ part, uint32_t splits) {
+// RESTS: also of what G's rounding left, of all elements or of the blocks that `large` names; else what that of the given rows' elements did.
+enum Rests { kNoRests, kAllRests, kLargeRests };
+template <typename T, bool SPLIT, Rests RESTS>
+__global__ __launch_bounds__(256, RESTS == kAllRests ? 2 : kGradWaves<T>) void grad_rows_kernel(GradArgs a, uint32_t row0, uint32_t rows, uint32_t ld, const T *__restrict__ G, const T *__restrict__ rests,
+                                                        const uint8_t *__restrict__ large, T *__restrict__ out, uint64_t stride, float *__restrict__ part, uint32_t splits) {
   const ScoreTable &g = a.g;
   __shared__ __attribute__((aligned(16))) char lds[kTileBytes<T, kAcross, kAcross>];
   const uint32_t c_tiles = (g.d + kTile - 1) / kTile, b8 = blockIdx.x / 8, split = SPLIT ? b8 % splits : 0, at = SPLIT ? b8 / splits : b8;
@@ -277,13 +365,14 @@ __global__ __launch_bounds__(256, RESTS ? 2 : kGradWaves<T>) void grad_rows_kern
   f32x16 acc[2][2];
   clear(acc);
   tile_product<T, kAcross, kAcross>(acc, A, rt * kTile, B, ct * kTile, begin, end, lds);
-  if constexpr (RESTS) {
-    const Lines<T> R = {rests, ld, ld, g.nq};
-    tile_product<T, kAcross, kAcross>(acc, R, rt * kTile, B, ct * kTile, begin, end, lds);
-  }
+  const Lines<T> R = {rests, ld, ld, g.nq};
+  if constexpr (RESTS == kAllRests) tile_product<T, kAcross, kAcross>(acc, R, rt * kTile, B, ct * kTile, begin, end, lds);
+  if constexpr (RESTS == kLargeRests)
+    marked_runs<1>(large + rt * 2, 2, 1, ld / 64, begin, end,
+                   [&](uint32_t k0, uint32_t k1, uint32_t) { tile_product<T, kAcross, kAcross>(acc, R, rt * kTile, B, ct * kTile, k0, k1, lds); });
   const int wave = (int)threadIdx.x / kWave, lane = lane_id();
   if constexpr (sizeof(T) == 2) {
-    if (!RESTS && a.targets) {
+    if (RESTS == kNoRests && a.targets) {
       // the queries whose given row is one of the tile's, in their order, 256 at a time
       uint32_t *list = (uint32_t *)lds;  // [256] queries, [256] rows of the tile, [4] counts
       const uint32_t tile0 = row0 + rt * kTile;
@@ -410,12 +499,14 @@ __global__ __launch_bounds__(256) void grad_bias_kernel(GradArgs a, const float 
 // 4,096 x 100,000 x 128 bf16: 290 us for the queries' side, 329 for the rows' (730 and 640 TFLOP/s; 1,097 us with G stored).  Queries' side: vector
 // instructions issue in 50 % of the cycles, LDS works in 39 (44 % of that conflicts), the matrix cores in 34: none of them bounds it alone,
 // two wavefronts to a SIMD wait.  Rows' side: 26, 41 and 29, and 782 workgroups on 512 places.
+// REST: what the rounding of G leaves is multiplied too where a block has a probability above kSmallShare (else that of the given rows' blocks); with few
+// queries, on the rows' side, in every block.
 // splits: of the passing side; with one, OWN_ROWS writes drows and drow_bias, otherwise part[split][line] (and drow_bias[split][row]: sums over its queries).
 constexpr int kPassing = 64, kOwned = 128;
 constexpr uint32_t kShortTarget = 512;       // workgroups that own queries: two to a compute unit
 constexpr uint64_t kShortStride = 1u << 24;  // row stride up to which offsets within a tile take 32 bits
 
-template <typename T, int KS, bool OWN_ROWS, bool BIAS, bool ENTROPY>
+template <typename T, int KS, bool OWN_ROWS, bool BIAS, bool ENTROPY, bool REST>
 __global__ __launch_bounds__(256, 2) void grad_short_kernel(GradArgs a, uint32_t splits, float *__restrict__ part, T *__restrict__ drows, uint64_t stride,
                                                             float *__restrict__ drow_bias) {
   typedef typename Operand16<T>::E E;
@@ -533,6 +624,7 @@ __global__ __launch_bounds__(256, 2) void grad_short_kernel(GradArgs a, uint32_t
       for (int kk = 0; kk < KS; ++kk) s = matrix_step(*(const E *)(x + kk * 32), line[kk], s);
       // G, times the scaling
       const uint32_t line0 = tile * kPassing + half * 32;
+      float most = 0.0f;  // of the probabilities
 #pragma unroll
       for (int r = 0; r < 16; r += 4) {
         const int l = half * 32 + block_row(r);
@@ -550,6 +642,7 @@ __global__ __launch_bounds__(256, 2) void grad_short_kernel(GradArgs a, uint32_t
           float y = OWN_ROWS ? lse2[e] : own_lse2;
           y = BIAS ? (__builtin_fmaf(s[r + e], g.scale, b) + y) * kLog2e : __builtin_fmaf(s[r + e], c, y);
           const float p = __builtin_amdgcn_exp2f(y);
+          if (REST) most = fmaxf(most, p);
           float slope = OWN_ROWS ? gl[e] : own_gl;
           if (ENTROPY) slope = __builtin_fmaf(OWN_ROWS ? gh[e] : own_gh, __builtin_fmaf(y, kLn2, OWN_ROWS ? h[e] : own_h), slope);
           float v = p * slope;
@@ -607,7 +700,7 @@ __global__ __launch_bounds__(256, 2) void grad_short_kernel(GradArgs a, uint32_t
           }
       };
       multiply(G);
-      if (OWN_ROWS && (hits || g.nq <= kFewGradQueries)) {  // what the rounding left, in 16 bits more
+      if ((OWN_ROWS && g.nq <= kFewGradQueries) || (REST ? __any(most > kSmallShare) : OWN_ROWS && hits)) {  // what the rounding left, in 16 bits more
 #pragma unroll
         for (int r = 0; r < 16; ++r) G[r / 8][r % 8] = from_f32<T>(s[r] - to_f32((T)G[r / 8][r % 8]));
         multiply(G);
@@ -654,11 +747,11 @@ struct BackwardPlan {
   uint32_t row_splits = 1;                      // of the queries, in the rows' product
   int slices = 0;                               // of 16 columns, if G stays in registers
   bool wide = false;                            // the queries' product: tiles of 256 of them
-  uint64_t g_at = 0, rests_at = 0, part_at = 0, row_part_at = 0, sums_at = 0, scaling_at = 0, rest_at = 0;
+  uint64_t g_at = 0, rests_at = 0, large_at = 0, part_at = 0, row_part_at = 0, sums_at = 0, scaling_at = 0, rest_at = 0;
   Parts parts;
 };
 
-// more: room for another part of the queries' sums, behind the splits'.
+// more: room for another part of the queries' sums, behind the splits', and for what the rounding of all of G leaves.
 static BackwardPlan backward_plan(uint32_t nq, uint64_t n, uint32_t d, uint32_t type, bool more) {
   BackwardPlan p;
   if (nq == 0 || n == 0) return p;
@@ -684,8 +777,9 @@ static BackwardPlan backward_plan(uint32_t nq, uint64_t n, uint32_t d, uint32_t 
     p.rest_at = p.parts.take(nq * sizeof(float));
     return p;
   }
+  const bool rests = type != ANN_F32 && (more || nq <= kFewGradQueries);
   const uint64_t row_bytes = (uint64_t)nq * type_bytes(type), all = (n + kTile - 1) / kTile * kTile;
-  uint64_t chunk = kChunkBytes / row_bytes / kTile * kTile;
+  uint64_t chunk = kChunkBytes / (more && rests ? 2 : 1) / row_bytes / kTile * kTile;
   if (chunk < kTile) chunk = kTile;
   if (chunk > all) chunk = all;
   // chunks of like sizes
@@ -707,7 +801,8 @@ static BackwardPlan backward_plan(uint32_t nq, uint64_t n, uint32_t d, uint32_t 
     if (p.splits > most) p.splits = most;
   }
   p.g_at = p.parts.take(p.chunk * row_bytes);
-  if (type != ANN_F32 && nq <= kFewGradQueries) p.rests_at = p.parts.take(p.chunk * row_bytes);
+  if (rests) p.rests_at = p.parts.take(p.chunk * row_bytes);
+  if (rests && more) p.large_at = p.parts.take((uint64_t)p.q_tiles * 2 * (p.chunk / 64));
   p.part_at = p.parts.take((uint64_t)(p.splits + more) * nq * d * sizeof(float));
   // (one chunk whose tiles leave compute units with one workgroup or none: runs of queries, of 64 at least)
   const uint32_t row_tiles = p.chunk / kTile * c_tiles;
@@ -734,7 +829,9 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
   GradArgs a = args;
   const ScoreTable &g = a.g;
   const uint32_t c_tiles = (g.d + kTile - 1) / kTile;
-  T *G = (T *)(ws + p.g_at), *rests = sizeof(T) == 2 && g.nq && g.nq <= kFewGradQueries && o.drows ? (T *)(ws + p.rests_at) : nullptr;
+  T *G = (T *)(ws + p.g_at), *rests = sizeof(T) == 2 && g.nq && (a.every || (g.nq <= kFewGradQueries && o.drows)) ? (T *)(ws + p.rests_at) : nullptr;
+  const bool all_rests = rests && o.drows && g.nq <= kFewGradQueries;
+  uint8_t *large = sizeof(T) == 2 && a.every && g.nq ? (uint8_t *)(ws + p.large_at) : nullptr;
   float *part = (float *)(ws + p.part_at), *sums = (float *)(ws + p.sums_at);
   a.rest = (float *)(ws + p.rest_at);
   if (std::is_same<T, f16_t>::value && g.nq && g.n && !a.scaling) {
@@ -743,23 +840,25 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
     a.scaling = scaling;
   }
   if (p.slices) {
-    const auto run = [&](auto slices, auto bias, auto entropy) {
+    const auto run = [&](auto slices, auto bias, auto entropy, auto every) {
       if constexpr (sizeof(T) == 2) {
         constexpr int KS = decltype(slices)::value;
-        constexpr bool BIAS = decltype(bias)::value, ENTROPY = decltype(entropy)::value;
+        constexpr bool BIAS = decltype(bias)::value, ENTROPY = decltype(entropy)::value, REST = decltype(every)::value;
         if (o.dq)
-          grad_short_kernel<T, KS, false, BIAS, ENTROPY><<<p.q_tiles * ((p.splits + 7) / 8 * 8), 256, 0, st>>>(a, p.splits, part, nullptr, 0, nullptr);
+          grad_short_kernel<T, KS, false, BIAS, ENTROPY, REST><<<p.q_tiles * ((p.splits + 7) / 8 * 8), 256, 0, st>>>(a, p.splits, part, nullptr, 0, nullptr);
         const uint32_t row_blocks = (g.n + kOwned - 1) / kOwned * p.row_splits;
         if (o.drows || o.drow_bias)
-          grad_short_kernel<T, KS, true, BIAS, ENTROPY><<<row_blocks, 256, 0, st>>>(a, p.row_splits, (float *)(ws + p.row_part_at), (T *)o.drows, o.drows_stride,
-                                                                                    p.row_splits > 1 && o.drow_bias ? sums : o.drow_bias);
+          grad_short_kernel<T, KS, true, BIAS, ENTROPY, REST><<<row_blocks, 256, 0, st>>>(a, p.row_splits, (float *)(ws + p.row_part_at), (T *)o.drows, o.drows_stride,
+                                                                                          p.row_splits > 1 && o.drow_bias ? sums : o.drow_bias);
       }
     };
     const auto run_entropy = [&](auto slices, auto bias) {
-      if (a.g_entropy)
-        run(slices, bias, std::true_type());
+      if (a.every)  // (there is no entropy's gradient then)
+        run(slices, bias, std::false_type(), std::true_type());
+      else if (a.g_entropy)
+        run(slices, bias, std::true_type(), std::false_type());
       else
-        run(slices, bias, std::false_type());
+        run(slices, bias, std::false_type(), std::false_type());
     };
     const auto run_bias = [&](auto slices) {
       if (g.bias)
@@ -800,7 +899,7 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
     if (g.nq) {
       const uint32_t grid = p.q_tiles * ((ld / kTile + 7) / 8 * 8);
       const auto run = [&](auto bias, auto entropy, auto row_sums) {
-        grad_scores_kernel<T, decltype(bias)::value, decltype(entropy)::value, decltype(row_sums)::value><<<grid, 256, 0, st>>>(a, row0, p.q_tiles, ld, G, rests, sums);
+        grad_scores_kernel<T, decltype(bias)::value, decltype(entropy)::value, decltype(row_sums)::value><<<grid, 256, 0, st>>>(a, row0, p.q_tiles, ld, G, rests, all_rests, large, sums);
       };
       const auto run_sums = [&](auto bias, auto entropy) {
         if (o.drow_bias)
@@ -823,7 +922,13 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
         const auto product = [&](auto blocks) {
           constexpr int MB = decltype(blocks)::value;
           const uint32_t tiles = c_tiles * ((g.nq + MB * 64 - 1) / (MB * 64)) * p.splits;
-          grad_queries_kernel<T, MB><<<(tiles + 7) / 8 * 8, 256, 0, st>>>(g, row0, rows, ld, G, p.splits, part, row0 != 0);
+          if constexpr (sizeof(T) == 2) {
+            if (a.every) {
+              grad_queries_kernel<T, MB, true><<<(tiles + 7) / 8 * 8, 256, 0, st>>>(g, row0, rows, ld, G, rests, large, p.splits, part, row0 != 0);
+              return;
+            }
+          }
+          grad_queries_kernel<T, MB, false><<<(tiles + 7) / 8 * 8, 256, 0, st>>>(g, row0, rows, ld, G, nullptr, nullptr, p.splits, part, row0 != 0);
         };
         // (biases: rows left out may hold anything, which the wide product does not look for)
         if (p.wide && !g.bias && wide_operand(g.rows, g.row_stride)) {
@@ -839,13 +944,15 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
       float *row_part = (float *)(ws + p.row_part_at);
       const auto product = [&](auto split, auto with_rests) {
         grad_rows_kernel<T, decltype(split)::value, decltype(with_rests)::value>
-            <<<grid, 256, 0, st>>>(a, row0, rows, ld, G, rests, (T *)o.drows, o.drows_stride, row_part, p.row_splits);
+            <<<grid, 256, 0, st>>>(a, row0, rows, ld, G, rests, large, (T *)o.drows, o.drows_stride, row_part, p.row_splits);
       };
       const auto with_split = [&](auto split) {
-        if (sizeof(T) == 2 && rests)
-          product(split, std::integral_constant<bool, sizeof(T) == 2>());
+        if (sizeof(T) == 2 && all_rests)
+          product(split, std::integral_constant<Rests, sizeof(T) == 2 ? kAllRests : kNoRests>());
+        else if (sizeof(T) == 2 && large)
+          product(split, std::integral_constant<Rests, sizeof(T) == 2 ? kLargeRests : kNoRests>());
         else
-          product(split, std::false_type());
+          product(split, std::integral_constant<Rests, kNoRests>());
       };
       if (p.row_splits > 1) {
         with_split(std::true_type());

@@ -345,10 +345,11 @@ __device__ __forceinline__ void wide_barrier() {
 
 // acc[i][j]: 32 x 32 block (m block 4 (wave / 2) + i, n block 2 (wave % 2) + j).  k_begin and the depths: see WideSide.  The three
 // buffers of kWideBuffer bytes are variables of their own (so that the compiler can tell reads of one from what is on its way into
-// another) and free when the call begins after a barrier.  All 256 lanes take part.
-template <typename T, Order OA, Order OB>
+// another) and free when the call begins after a barrier.  All 256 lanes take part.  SOME: wavefronts for which `mine` is false add nothing (what A holds of
+// their lines is not looked at).
+template <typename T, Order OA, Order OB, bool SOME = false>
 __device__ __forceinline__ void wide_product(f32x16 (&acc)[4][2], const Lines<T> &A, uint32_t m0, const Lines<T> &B, uint32_t n0, uint32_t k_begin,
-                                             uint32_t k_end, char *lds0, char *lds1, char *lds2) {
+                                             uint32_t k_end, char *lds0, char *lds1, char *lds2, bool mine = true) {
   typedef WideSide<T, OA, kWideM> SA;
   typedef WideSide<T, OB, kWideN> SB;
   typedef typename Operand16<T>::E E;
@@ -368,6 +369,7 @@ __device__ __forceinline__ void wide_product(f32x16 (&acc)[4][2], const Lines<T>
     for (int j = 0; j < 2; ++j) fb[kk][j] = SB::fragment(at + SA::kBytes, nw + j, kk);
   };
   const auto multiply = [&](int kk) {
+    if (SOME && !mine) return;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
