@@ -713,7 +713,7 @@ uint64_t ann_row_logprobs_backward_workspace(uint32_t nq, uint64_t n, uint32_t d
  *                +infinity where a row that counts is left out; 0 where none counts.
  *   lse[i]       log sum_j exp(s[i][j]) as in ann_row_logprobs (of fp32 rows nearer to it: their products' smaller parts are summed apart).
  *   logprobs     [nq][k] the log probabilities of the given rows under the softmax of all rows'
- *                scores; 0 where the id is not below n, -infinity where the row is left out.
+ *                scores, at most 0; 0 where the id is not below n, -infinity where the row is left out.
  * The teacher's temperature is in its log probabilities, this model's in `scale`.  The weights
  * t need not sum to one.  A row may be given twice: its weights add.
  * Of short lists (n <= 256 and nq n <= 2^23; n <= 1024, nq n <= 2^20 and nq n d <= 3 * 2^28) the scores and their

@@ -44,6 +44,7 @@ __global__ __launch_bounds__(256) void distill_loss_kernel(ScoreTable g, uint32_
     if (lane != 0) continue;
     double logp = 0.0;
     if (id < g.n) logp = bias == -INFINITY ? -INFINITY : sum * (double)g.scale + (double)bias - l;
+    logp = logp > 0.0 ? 0.0 : logp;  // (what lse is off, where the row has all probability)
     logprobs[(uint64_t)q * k + e] = (float)logp;
     const double t = id < g.n ? (double)given[(uint64_t)q * k + e] : -INFINITY, weight = exp(t);
     terms[e] = weight == 0.0 ? 0.0 : weight * (t - logp);  // (without a weight nothing counts, also where logp is -infinity)
@@ -128,7 +129,7 @@ __global__ __launch_bounds__(256) void distill_short_loss_kernel(uint32_t nq, ui
   for (uint32_t j = lane; j < n; j += kWave) sum += exp(s[j] - (double)top);
   sum = group_sum_f64<kWave>(sum);
   const double lse = sum == 0.0 ? -INFINITY : (double)top + log(sum);
-  const double logp = id >= n ? 0.0 : own == -INFINITY ? -INFINITY : own - lse;
+  const double above = id >= n ? 0.0 : own == -INFINITY ? -INFINITY : own - lse, logp = above > 0.0 ? 0.0 : above;  // (what lse is off)
   const double all = group_sum_f64<kWave>(weight == 0.0 ? 0.0 : weight * (t - logp));  // (without a weight nothing counts, also where logp is -infinity)
   if (lane < k) logprobs[at] = (float)logp;
   if (lane == 0) loss[q] = (float)all, lse_out[q] = (float)lse;
