@@ -740,8 +740,10 @@ uint64_t ann_row_distillation_workspace(uint32_t nq, uint64_t n, uint32_t d, uin
  * are off by their own rounding and by what the scores and sums in fp32 are.  Rows left out get zero, a query whose lse is -infinity too.
  * logprobs is what the forward pass wrote (it must be there; today's kernels take all they need from lse).
  * Of short lists (as above, and at most 4,096 queries) G and its products are fp64 and rounded once, at the end,
- * with 8 bytes of workspace to a score.  Otherwise the workspace holds a number to a row and sums of fp32 rows for the
- * smaller of n and nq * k of them, beside what ann_row_logprobs_backward asks for.  Errors as ann_row_distillation.
+ * with 8 bytes of workspace to a score.  Otherwise the workspace holds, beside what ann_row_logprobs_backward asks for: a number to a
+ * row; one more [nq][d] of fp32; for each of the nq * k entries some 30 bytes, for every 8 of them (32 where they are more than 16,384; at most 32,768 times) two
+ * fp32 rows, and fp32 rows for the smaller of n and nq * k; with 16-bit elements and d <= 128 parts of the rows' sums, at most 256 MiB; with longer rows of
+ * 16 bits what the rounding leaves of G (G and that are 512 MiB at a time at most, as G alone is there).  Errors as ann_row_distillation.
  */
 ann_status ann_row_distillation_backward(const ann_row_scores *scores, uint32_t k, const uint32_t *given_ids,
                                          const float *given_logprobs, const float *lse, const float *logprobs,

@@ -36,6 +36,7 @@ namespace ann {
 constexpr uint64_t kChunkBytes = 512ull << 20;  // of G at a time
 constexpr uint32_t kGradTarget = 768;           // workgroups of a product: three to a compute unit
 constexpr uint32_t kWideSlots = 512;            // of a wide one: two
+constexpr uint64_t kRowPartBytes = 256ull << 20;  // of parts of short rows' sums (4,096 x 70,000 x 128 takes 143 MB: 467 us, 508 without)
 constexpr float kSmallShare = 0x1p-10f;         // a probability whose rounding to 16 bits may stay
 
 // Wavefronts to a SIMD of the gradients' products by tiles of 128 (three instead of two: 303 -> 237 and 282 -> 255 us with 2,048 x 50,000 x 768).
@@ -765,6 +766,7 @@ static BackwardPlan backward_plan(uint32_t nq, uint64_t n, uint32_t d, uint32_t 
       const uint64_t own_tiles = (n + kOwned - 1) / kOwned, q_tiles = (nq + kPassing - 1) / kPassing;
       double least = INFINITY;
       for (uint32_t s = 1; s <= 16 && s <= q_tiles; ++s) {
+        if (s > 1 && (uint64_t)s * n * (d + 1) * sizeof(float) > kRowPartBytes) break;
         const double cost = 0.29 * p.slices * ((own_tiles * s + kShortTarget - 1) / kShortTarget) * ((q_tiles + s - 1) / s) + (s > 1 ? 5.0 + 2e-6 * s * n * d : 0.0);
         if (cost < least) least = cost, p.row_splits = s;
       }
