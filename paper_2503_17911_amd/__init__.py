@@ -9,16 +9,10 @@ is no CPU fallback.
 from __future__ import annotations
 
 import ctypes
-from pathlib import Path
-
+import importlib.util
 import os
-
-# PyTorch brings a HIP runtime of its own.  Where it is there, it is loaded first and the library uses the same one: with the library first, a process
-# holds two, and calls on torch's tensors find no device.
-try:
-    import torch  # noqa: F401
-except ImportError:
-    pass
+import sys
+from pathlib import Path
 
 _PKG = Path(__file__).resolve().parent
 # ANN_LIBRARY_PATH selects another build of the same library (e.g. one compiled
@@ -82,10 +76,28 @@ class RowScores(ctypes.Structure):
                 ("scale", ctypes.c_float), ("row_bias", ctypes.c_void_p), ("targets", ctypes.c_void_p)]
 
 
+def _share_hip_runtime() -> None:
+    """PyTorch brings a HIP runtime of its own, which a program that uses both has to share: with two in a process, calls on torch's tensors
+    find no device.  So where torch is installed its runtime, a file beside it, is loaded before the library asks for one of the same
+    name, whichever the program imports first.  (torch itself is not imported: that takes seconds, and who only searches needs none of it.)"""
+    if "torch" in sys.modules:
+        return
+    try:
+        spec = importlib.util.find_spec("torch")
+        for place in (spec.submodule_search_locations or []) if spec else []:
+            runtime = Path(place) / "lib" / "libamdhip64.so"
+            if runtime.exists():
+                ctypes.CDLL(str(runtime))
+                return
+    except (ImportError, ValueError, OSError):
+        pass  # a torch that cannot be found or loaded brings no tensors
+
+
 def _load_library() -> ctypes.CDLL:
     if not LIB_PATH.exists():
         raise ImportError(f"{LIB_PATH} is missing: build the HIP library first "
                           f"(python -m paper_2503_17911_amd.build); there is no fallback path")
+    _share_hip_runtime()
     lib = ctypes.CDLL(str(LIB_PATH))
     vp, u32, u64, i32 = ctypes.c_void_p, ctypes.c_uint32, ctypes.c_uint64, ctypes.c_int
     lib.ann_sq_train.argtypes = [vp, u64, u32, u32, vp, vp, vp]
