@@ -831,9 +831,10 @@ static ann_status backward(const GradArgs &args, const BackwardPlan &p, const Gr
   GradArgs a = args;
   const ScoreTable &g = a.g;
   const uint32_t c_tiles = (g.d + kTile - 1) / kTile;
-  T *G = (T *)(ws + p.g_at), *rests = sizeof(T) == 2 && g.nq && (a.every || (g.nq <= kFewGradQueries && o.drows)) ? (T *)(ws + p.rests_at) : nullptr;
+  const bool every = a.every && (o.dq || o.drows);  // (the bias' gradient takes G as it is before its rounding)
+  T *G = (T *)(ws + p.g_at), *rests = sizeof(T) == 2 && g.nq && (every || (g.nq <= kFewGradQueries && o.drows)) ? (T *)(ws + p.rests_at) : nullptr;
   const bool all_rests = rests && o.drows && g.nq <= kFewGradQueries;
-  uint8_t *large = sizeof(T) == 2 && a.every && g.nq ? (uint8_t *)(ws + p.large_at) : nullptr;
+  uint8_t *large = sizeof(T) == 2 && every && g.nq ? (uint8_t *)(ws + p.large_at) : nullptr;
   float *part = (float *)(ws + p.part_at), *sums = (float *)(ws + p.sums_at);
   a.rest = (float *)(ws + p.rest_at);
   if (std::is_same<T, f16_t>::value && g.nq && g.n && !a.scaling) {
