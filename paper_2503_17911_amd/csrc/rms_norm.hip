@@ -9,8 +9,8 @@
 // Bound by memory: every row is read once and stays in the registers of 16 to 512 lanes as the pieces that were loaded (of 16 bytes with any
 // alignment: rows of odd strides are read as wide as the others), one to four to a lane; sums are fp32.  A group of columns that
 // shares a scale is 4 to 32 lanes side by side: its maximum takes two to five lane exchanges.  Gradients of the weights collect in registers, one
-// part per workgroup, added in a fixed order by a second kernel.  Measured: 80,000 x 768 bf16 with the residual in e4m3 83 us (5.2 TB/s; a large copy reaches
-// 5.1), the gradient 99 us (5.0 TB/s, of which 4.8 are the second kernel; 226 us by 64 lanes of four pieces, a third of them idle, with elements instead of
+// part per workgroup, added in a fixed order by a second kernel.  Measured: 80,000 x 768 bf16 with the residual in e4m3 84 us (5.1 TB/s, as a large copy
+// reaches; 83 with a multiplication in the place of the codes' division), the gradient 99 us (5.0 TB/s, of which 4.8 are the second kernel; 226 us by 64 lanes of four pieces, a third of them idle, with elements instead of
 // words in registers); rows of 769: 115 us in bf16, gradient 180; one row 3 us.
 #include "row_pieces.hpp"
 

@@ -10,8 +10,10 @@
 // teacher, or its likely rows are alike, the products are small differences, and the rounding of g T p to 16 bits would be seen in them.  The second is
 // added in fp32 to the products' results before these are rounded.  For dq that is a sum of k rows to a query.  For the rows the entries are put in the
 // order of their ids and summed by runs, so that a row that many teachers name costs no more than others.
-// Measured: 4,096 x 100,000 x 128 bf16 with k = 32: 600 us, of which the first part takes 530 (bound as its kernels are), the order of the entries 27, their runs
-// and join 26, the entries and the queries' sums 17; 8 x 1M x 128 forward 55 us, 5 of them for the given rows.
+// Measured: gradients of 4,096 x 100,000 x 128 bf16 with k = 32: 619 us, of which the first part takes 570 (bound as its kernels are; 714 the call where every
+// block has a likely row), the order of the entries 27, their runs and join 25, the entries and the queries' sums 13.  Forward: 8 x 1M x 128 55 us, 5 of them
+// for the given rows; 4,096 x 100,000 x 128 221 us in bf16, 217 in f16, 1,011 in fp32, whose scores take the smaller products of their parts apart (the rows'
+// log probabilities, which do not, 690): losses are differences of log probabilities, off by 2.6e-8 so, and small where the student is near its teacher.
 #include "row_logprobs.hpp"
 #include "row_runs.hpp"
 
@@ -138,9 +140,9 @@ __global__ __launch_bounds__(256) void distill_short_loss_kernel(uint32_t nq, ui
 // Backward of short lists: the scores in fp64 as above, G from them in their place (both parts together, so nothing is left to add), and both products by the fp64 matrix
 // instructions: G X and G^T Q in one launch.  A workgroup makes 16 rows of 64 columns, each of its eight wavefronts along every eighth block of four of the sum; it reads
 // a block of 16 ahead (without: 63 us in the place of 43 for 3,000 x 64 x 96, where eight workgroups make all of G^T Q; with more queries than 4,096 that is too few).
-// Measured, us, here against the kernels for long lists (k = 20, bf16 / fp32): 8 x 256 x 960 18 / 18 against 60 / 113; 300 x 256 x 960 30 / 31 against 81 / 145;
-// 3,000 x 128 x 768 70 / 76 against 113 / 187; 3,000 x 64 x 96 53 / 53 against 65 / 96; 4,096 x 256 x 960 156 / 170 against 146 / 262 (k = 1, bf16: 155 against 116;
-// k = 64: 159 against 199); 300 x 1,024 x 960 71 / 75 against 91 / 153.
+// Measured, us, here against the kernels for long lists (k = 20, bf16 / fp32): 8 x 256 x 960 18 / 19 against 66 / 115; 300 x 256 x 960 30 / 31 against 91 / 146;
+// 3,000 x 128 x 768 71 / 75 against 124 / 187; 3,000 x 64 x 96 52 / 54 against 64 / 96; 4,096 x 256 x 960 162 / 168 against 164 / 261 (k = 1, bf16: 155 against 135;
+// k = 64: 159 against 197); 300 x 1,024 x 960 71 / 75 against 100 / 153.
 static bool short_gradient(uint64_t nq, uint64_t n, uint32_t d) { return nq && nq <= 4096 && short_list(nq, n, d); }
 
 __global__ __launch_bounds__(256) void distill_short_weights_kernel(uint32_t nq, uint32_t n, double *__restrict__ scores, uint32_t k, const uint32_t *__restrict__ ids,

@@ -216,7 +216,8 @@ __global__ __launch_bounds__(256, MB == 4 ? 2 : 1) void row_scores_kernel(ScoreT
       wide_product<T, kAlong, kAlong>(acc, X, row0, Q, qt * kTile, 0, g.d, lds, lds1, lds2);
     else
       // (fp32: the smaller products apart take so many registers that one workgroup fits where two did: 155 -> 213 us for 513 x 50,000 x 100;
-      // with one sum the log probabilities err by 6e-8 there, by 2.8e-7 with 768 columns, about as far as a plain fp32 product's)
+      // with one sum the log probabilities err by 6e-8 there, by 2.8e-7 with 768 columns, about as far as a plain fp32 product's.  Distillation, whose
+      // losses are differences of them, has them apart: 105 -> 167 us for that size, 690 -> 1,010 for 4,096 x 100,000 x 128)
       tile_product<T, kAlong, kAlong, APART>(acc, X, row0, Q, qt * kTile, 0, g.d, lds);
     if (BIAS || !whole) {
       // (read by the tile before's epilogue: the barriers of the product lie in between; d > 0)
