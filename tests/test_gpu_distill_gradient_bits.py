@@ -44,8 +44,9 @@ def test_sums_that_cancel(nq, n, d, dtype):
         b = None
         if bias:
             b = torch.zeros(n)
-            b[torch.randperm(n)[:n // 5]] = -math.inf
-            b[live] = torch.randint(-4, 5, (8,)) / 8.0
+            gen = torch.Generator().manual_seed(n)
+            b[torch.randperm(n, generator=gen)[:n // 5]] = -math.inf
+            b[live] = torch.randint(-4, 5, (8,), generator=gen) / 8.0
         z = R.scores(q, rows, scale, b)
         lse, logp, _, t, B = definition(z, ids, given)
         lse32 = lse.float()
